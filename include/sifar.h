@@ -483,6 +483,93 @@ int sifar_litmus(int32_t protocol, int32_t placement, int32_t pairs, int32_t tri
 int sifar_allreduce_noalloc(const void *src, int64_t src_rank_stride, int32_t nranks,
                             int32_t tokens, int32_t hidden, void *out, void *stream);
 
+/* ---- Row operators of a decode step ------------------------------------------
+ * What a decode step computes, row by row, around its all-reduces: the norms
+ * around a block (sifar_block_norm), the experts of a token (sifar_route) and,
+ * at its end, the next token (sifar_sample). The paper runs its all-reduces
+ * inside such steps (Sec. 2.4, 6.1) and does not describe these operators.
+ *
+ * In tensor-parallel decode every rank holds the same rows after an all-reduce
+ * and repeats these operators; ranks that disagreed on an expert or a token
+ * would diverge. So results are functions of the inputs alone: equal inputs
+ * give equal bits on every call, ties go to the lowest index, and no
+ * floating-point sum depends on the order in which workgroups arrive.
+ *
+ * They need no handle and allocate nothing, and may be called under HIP graph
+ * capture. Conventions as above, and:
+ *  - Element types: SIFAR_BF16, SIFAR_FP16, SIFAR_FP32. Sums are kept in 32 bits
+ *    or more and rounded once, where an output is stored.
+ *  - Rows are `..._stride` elements apart, elements of a row adjacent.
+ *  - tokens = 0 is no work: SIFAR_OK, nothing is enqueued, and row pointers
+ *    may be NULL. A bad argument is SIFAR_EINVAL before anything is enqueued.
+ *  - Rows behind the last token are neither read nor written.
+ */
+#define SIFAR_BF16 0
+#define SIFAR_FP16 1
+#define SIFAR_FP32 2
+
+/* Largest sizes of the row operators. */
+#define SIFAR_ROWS_MAX_TOKENS 1048576
+
+/* Norms before and after a block, fused with its gate and the residual stream
+ * (layers that normalise a block's output before adding it, then normalise the
+ * sum for the next block). Per token t and element h:
+ *
+ *   a  = x_0 + x_1 + ... + x_(parts-1)          fp32, ascending
+ *   b  = a / sqrt(mean_h(a^2) + eps) * (weight_offset + post_weight[h])
+ *   r' = residual_scale * residual + branch_scale * gate * b
+ *   residual_out = r'                            rounded to residual_dtype
+ *   y  = r' / sqrt(mean_h(r'^2) + eps) * (weight_offset + norm_weight[h])
+ *
+ * with r' unrounded in y (sifar_reduce_rmsnorm, whose epilogue is the plain
+ * pre-norm case, normalises the rounded one). Left out where its pointer is
+ * NULL: post_weight (b = a), gate (1), residual (0), norm_weight and y (both or
+ * neither). weight_offset 1 takes norm weights stored as w - 1.
+ *
+ *   x             [parts][tokens][hidden] dtype, partials part_stride apart: the
+ *                 block's output, or the ranks' partials of it (summed in
+ *                 ascending rank order, as an all-reduce sums them)
+ *   gate          [tokens][hidden] dtype; gate_stride 0: one row for all
+ *   post_weight,
+ *   norm_weight   [hidden] dtype
+ *   residual, residual_out  [tokens][hidden] residual_dtype (dtype or SIFAR_FP32)
+ *   y             [tokens][hidden] dtype
+ *
+ * Limits: hidden a multiple of 8 in 8..65536; 0 <= tokens <=
+ * SIFAR_ROWS_MAX_TOKENS; 1 <= parts <= 8; row strides, where there is more than
+ * one token, multiples of 8 elements and at least hidden (gate_stride may be 0);
+ * part_stride, where there is more than one partial, a multiple of 8 and not
+ * negative; pointers 16-byte aligned. residual_out and y may each be, row for row, x (its first
+ * partial), the residual or the gate (same address, stride and element size).
+ * Any other overlap of an output with an input or the other output is refused,
+ * and so are outputs whose rows interleave with another operand's at another
+ * stride. One launch. */
+typedef struct {
+    int32_t dtype;
+    int32_t residual_dtype;
+    int32_t tokens;
+    int32_t hidden;
+    int32_t parts;
+    float branch_scale;
+    float residual_scale;
+    float weight_offset;
+    float eps;
+    const void *x;
+    int64_t x_stride;
+    int64_t part_stride;
+    const void *post_weight;
+    const void *gate;
+    int64_t gate_stride;
+    const void *residual;
+    int64_t residual_stride;
+    void *residual_out;
+    int64_t residual_out_stride;
+    const void *norm_weight;
+    void *y;
+    int64_t y_stride;
+} sifar_block_norm_args;
+int sifar_block_norm(const sifar_block_norm_args *a, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

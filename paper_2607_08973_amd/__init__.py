@@ -18,6 +18,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 from typing import Optional, Sequence
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -66,6 +67,12 @@ SIFAR_NOALLOC_MAX_TOKENS = 64
 SIFAR_NOALLOC_MAX_ELEMS = 262144
 SIFAR_NOALLOC_SCRATCH_BYTES = 8437248
 
+# the row operators: element types and largest sizes
+SIFAR_BF16 = 0
+SIFAR_FP16 = 1
+SIFAR_FP32 = 2
+SIFAR_ROWS_MAX_TOKENS = 1048576
+
 CHUNK = 512  # elements per chunk (one 64-lane wave, 16 bytes per lane)
 
 # every symbol include/sifar.h declares
@@ -75,7 +82,7 @@ EXPORTS = (
     "sifar_step", "sifar_step_plan", "sifar_set_injection", "sifar_log_geometry",
     "sifar_read_log", "sifar_read_stamp_log", "sifar_read_placement",
     "sifar_epochs", "sifar_status", "sifar_error_info", "sifar_strerror", "sifar_floor",
-    "sifar_litmus", "sifar_allreduce_noalloc",
+    "sifar_litmus", "sifar_allreduce_noalloc", "sifar_block_norm",
 )
 
 
@@ -123,6 +130,33 @@ class sifar_step_buffers(ctypes.Structure):
         ("residual", ctypes.c_void_p),
         ("weight", ctypes.c_void_p),
         ("y_ring", ctypes.c_void_p),
+    ]
+
+
+class sifar_block_norm_args(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("residual_dtype", ctypes.c_int32),
+        ("tokens", ctypes.c_int32),
+        ("hidden", ctypes.c_int32),
+        ("parts", ctypes.c_int32),
+        ("branch_scale", ctypes.c_float),
+        ("residual_scale", ctypes.c_float),
+        ("weight_offset", ctypes.c_float),
+        ("eps", ctypes.c_float),
+        ("x", ctypes.c_void_p),
+        ("x_stride", ctypes.c_int64),
+        ("part_stride", ctypes.c_int64),
+        ("post_weight", ctypes.c_void_p),
+        ("gate", ctypes.c_void_p),
+        ("gate_stride", ctypes.c_int64),
+        ("residual", ctypes.c_void_p),
+        ("residual_stride", ctypes.c_int64),
+        ("residual_out", ctypes.c_void_p),
+        ("residual_out_stride", ctypes.c_int64),
+        ("norm_weight", ctypes.c_void_p),
+        ("y", ctypes.c_void_p),
+        ("y_stride", ctypes.c_int64),
     ]
 
 
@@ -178,6 +212,7 @@ def load(path: str = LIB_PATH):
         "sifar_litmus": (ctypes.c_int, [I32, I32, I32, I32, P,
                                         ctypes.POINTER(sifar_litmus_result)]),
         "sifar_allreduce_noalloc": (ctypes.c_int, [P, I64, I32, I32, I32, P, P]),
+        "sifar_block_norm": (ctypes.c_int, [P, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -363,6 +398,108 @@ def sifar_allreduce_noalloc(src, src_rank_stride: int, nranks: int, tokens: int,
     """One all-reduce on the library's static scratch (no allocation)."""
     _check("sifar_allreduce_noalloc", load().sifar_allreduce_noalloc(
         _ptr(src), src_rank_stride, nranks, tokens, hidden, _ptr(out), _stream(stream)))
+
+
+# ---- row operators: tensors in, shapes and strides taken from them ----------
+# Their arguments are packed in one call each (the structs above, in native
+# layout): filling a ctypes structure of 22 fields takes longer than the launch.
+
+_BLOCK_NORM = struct.Struct("@5i4fP2q2PqPqPq2Pq")
+_DTYPES = None  # torch dtype -> SIFAR_* element type
+
+
+def _refuse(fn: str, why: str):
+    e = SifarError(fn, SIFAR_EINVAL)
+    e.args = (f"{e.args[0]}: {why}",)
+    raise e
+
+
+def _dtype(fn: str, dtype) -> int:
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.bfloat16: SIFAR_BF16, torch.float16: SIFAR_FP16,
+                   torch.float32: SIFAR_FP32}
+    code = _DTYPES.get(dtype)
+    if code is None:
+        _refuse(fn, f"no element type for {dtype}")
+    return code
+
+
+def _gpu(fn: str, name: str, t) -> int:
+    """The current device, which has to hold t."""
+    dev = t.get_device()
+    if dev < 0 or dev != _current_device():
+        _refuse(fn, f"{name} is on {t.device}, not on the current GPU")
+    return dev
+
+
+def _current_device() -> int:
+    import torch
+    return torch._C._cuda_getDevice()  # a GPU tensor exists: PyTorch has initialised the GPU
+
+
+def _operand(fn: str, name: str, t, dtype, shape, dev: int):
+    """Address and leading stride of t, which has to be `dtype` of `shape` on
+    device `dev` with adjacent elements: the library sees addresses only."""
+    at = t.stride()
+    if (t.dtype is not dtype or t.shape != shape or t.get_device() != dev
+            or (at[-1] != 1 and shape[-1] > 1)):
+        _refuse(fn, f"{name} is {t.dtype} {tuple(t.shape)} on {t.device} at strides {at}, not "
+                    f"{dtype} {tuple(shape)} on the current GPU with adjacent elements")
+    return t.data_ptr(), at[0]
+
+
+def sifar_block_norm(x, residual, residual_out, post_weight=None, gate=None, norm_weight=None,
+                     y=None, branch_scale=1.0, residual_scale=1.0, weight_offset=0.0, eps=1e-6,
+                     stream=None) -> None:
+    """x [tokens][hidden], or [parts][tokens][hidden] to be summed; gate [tokens][hidden], or
+    [hidden] or [1][hidden] for all tokens; residual (or None) and residual_out
+    [tokens][hidden] in x's type or float32; norm_weight and y together or neither."""
+    fn = "sifar_block_norm"
+    shape, at = x.shape, x.stride()
+    if len(shape) == 2:
+        parts, part_stride = 1, 0
+    elif len(shape) == 3:
+        parts, part_stride = shape[0], at[0]
+        shape, at = shape[1:], at[1:]
+    else:
+        _refuse(fn, f"x has {len(shape)} dimensions, not 2 or 3")
+    T, H = shape
+    if T > SIFAR_ROWS_MAX_TOKENS or H > 65536 or parts > 8:
+        _refuse(fn, f"{parts} x {T} x {H} is too large")
+    if at[1] != 1 and H > 1:
+        _refuse(fn, "the elements of x's rows are not adjacent")
+    if residual_out is None:
+        _refuse(fn, "no residual_out")
+    dev = _gpu(fn, "x", x)
+    dt, rdt, vec = x.dtype, residual_out.dtype, shape[1:]
+    out, out_stride = _operand(fn, "residual_out", residual_out, rdt, shape, dev)
+    res = res_stride = g = g_stride = post = norm = yp = y_stride = 0
+    if residual is not None:
+        res, res_stride = _operand(fn, "residual", residual, rdt, shape, dev)
+    if gate is not None:
+        if gate.shape == shape:
+            g, g_stride = _operand(fn, "gate", gate, dt, shape, dev)
+        else:
+            row = gate[0] if gate.dim() == 2 and gate.shape[0] == 1 else gate
+            g, _ = _operand(fn, "gate", row, dt, vec, dev)
+    if post_weight is not None:
+        post, _ = _operand(fn, "post_weight", post_weight, dt, vec, dev)
+    if norm_weight is not None:
+        norm, _ = _operand(fn, "norm_weight", norm_weight, dt, vec, dev)
+    if y is not None:
+        yp, y_stride = _operand(fn, "y", y, dt, shape, dev)
+    if (norm_weight is None) != (y is None):
+        _refuse(fn, "norm_weight and y go together")
+    code = _dtype(fn, dt)
+    rc = load().sifar_block_norm(
+        _BLOCK_NORM.pack(code, code if rdt is dt else _dtype(fn, rdt), T, H, parts, branch_scale,
+                         residual_scale, weight_offset, eps, x.data_ptr(), at[0], part_stride,
+                         post, g, g_stride, res, res_stride, out, out_stride, norm, yp, y_stride),
+        _stream(stream))
+    if rc:
+        _check(fn, rc)
 
 
 def sifar_status(h: int) -> int:

@@ -1,0 +1,165 @@
+"""sifar_block_norm refuses, on the host and before any device call, what its
+contract leaves out. No GPU is used."""
+from __future__ import annotations
+
+import ctypes
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+import torch
+
+import paper_2607_08973_amd as S
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include",
+                      "sifar.h")
+T, H = 4, 64
+BASE = 1 << 20  # addresses that a refused call never touches
+
+
+def args(**kw):
+    a = S.sifar_block_norm_args(
+        dtype=S.SIFAR_BF16, residual_dtype=S.SIFAR_BF16, tokens=T, hidden=H, parts=1,
+        branch_scale=1.0, residual_scale=1.0, weight_offset=0.0, eps=1e-6, x=BASE, x_stride=H,
+        part_stride=0, post_weight=2 * BASE, gate=3 * BASE, gate_stride=H, residual=4 * BASE,
+        residual_stride=H, residual_out=5 * BASE, residual_out_stride=H, norm_weight=6 * BASE,
+        y=7 * BASE, y_stride=H)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+BAD = [
+    dict(dtype=3), dict(dtype=-1), dict(residual_dtype=S.SIFAR_FP16), dict(residual_dtype=3),
+    dict(dtype=S.SIFAR_FP32, residual_dtype=S.SIFAR_BF16),
+    dict(tokens=-1), dict(tokens=S.SIFAR_ROWS_MAX_TOKENS + 1),
+    dict(hidden=0), dict(hidden=12), dict(hidden=65544), dict(parts=0), dict(parts=9),
+    dict(eps=-1.0), dict(eps=float("nan")),
+    dict(norm_weight=None), dict(y=None),                       # both or neither
+    dict(x=None), dict(residual_out=None),
+    dict(x=BASE + 8), dict(post_weight=2 * BASE + 2), dict(gate=3 * BASE + 8),
+    dict(residual=4 * BASE + 4), dict(residual_out=5 * BASE + 8), dict(norm_weight=6 * BASE + 8),
+    dict(y=7 * BASE + 8),
+    dict(x_stride=H - 8), dict(x_stride=H + 4), dict(x_stride=-H), dict(gate_stride=H - 8),
+    dict(residual_stride=0), dict(residual_out_stride=0), dict(y_stride=H - 8),
+    dict(parts=2, part_stride=-8), dict(parts=2, part_stride=4),
+    # outputs over inputs, over each other, over the weights
+    dict(y=5 * BASE), dict(y=5 * BASE + 2 * H), dict(residual_out=BASE + 2 * H),
+    dict(residual_out=4 * BASE + 2 * H), dict(y=BASE, y_stride=2 * H),
+    dict(residual_out=6 * BASE), dict(y=2 * BASE),
+    dict(residual_dtype=S.SIFAR_FP32, residual_out=BASE),       # x's rows, but longer
+    dict(parts=2, part_stride=T * H, y=BASE + 2 * T * H),       # a later partial
+    dict(parts=2, part_stride=0, y=BASE),
+    dict(gate_stride=0, y=3 * BASE),                            # every token reads that row
+]
+
+
+@pytest.mark.parametrize("kw", BAD, ids=lambda kw: ",".join(f"{k}={v}" for k, v in kw.items()))
+def test_refused_by_the_library(kw):
+    assert S.load().sifar_block_norm(ctypes.byref(args(**kw)), None) == S.SIFAR_EINVAL
+
+
+def test_null_and_empty_calls():
+    L = S.load()
+    assert L.sifar_block_norm(None, None) == S.SIFAR_EINVAL
+    a = args(tokens=0, x=None, residual=None, residual_out=None)
+    assert L.sifar_block_norm(ctypes.byref(a), None) == S.SIFAR_OK
+
+
+def test_layout_matches_a_c_compiler(tmp_path):
+    cc = shutil.which("gcc") or shutil.which("cc")
+    if cc is None:
+        pytest.skip("no C compiler")
+    cls = S.sifar_block_norm_args
+    body = re.search(r"typedef struct \{([^{}]*)\} sifar_block_norm_args;",
+                     open(HEADER).read()).group(1)
+    assert re.findall(r"\b(\w+);", body) == [f for f, _ in cls._fields_]
+    lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "sifar.h"', "int main(void) {",
+             '    printf("size %zu\\n", sizeof(sifar_block_norm_args));']
+    lines += [f'    printf("{f} %zu\\n", offsetof(sifar_block_norm_args, {f}));'
+              for f, _ in cls._fields_]
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text("\n".join(lines + ["    return 0;", "}"]) + "\n")
+    subprocess.run([cc, "-std=c11", "-I", os.path.dirname(HEADER), str(src), "-o", str(exe)],
+                   check=True)
+    for line in subprocess.run([str(exe)], check=True, capture_output=True,
+                               text=True).stdout.split("\n")[:-1]:
+        what, value = line.split()
+        assert int(value) == (ctypes.sizeof(cls) if what == "size" else getattr(cls, what).offset)
+
+
+class Recorder:
+    """Stands in for the library where host tensors play device tensors."""
+
+    def __init__(self):
+        self.calls = []
+
+    def sifar_block_norm(self, packed, stream):
+        self.calls.append(S.sifar_block_norm_args.from_buffer_copy(packed))
+        return 0
+
+    def sifar_strerror(self, code):
+        return b""
+
+
+@pytest.fixture
+def recorder(monkeypatch):
+    r = Recorder()
+    monkeypatch.setattr(S, "_lib", r)
+    monkeypatch.setattr(S, "_gpu", lambda fn, name, t: -1)   # a host tensor's device
+    monkeypatch.setattr(S, "_current_stream", lambda: 0)
+    return r
+
+
+def tensors(**kw):
+    z = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
+    a = dict(x=z(2, T, H), residual=torch.zeros(T, H), residual_out=torch.zeros(T, 2 * H)[:, :H],
+             post_weight=z(H), gate=z(1, H), norm_weight=z(H), y=z(T, H))
+    a.update(kw)
+    return a
+
+
+def test_marshalling(recorder):
+    t = tensors()
+    S.sifar_block_norm(**t, branch_scale=0.5, residual_scale=2.0, weight_offset=1.0, eps=1e-5)
+    c = recorder.calls[0]
+    assert (c.dtype, c.residual_dtype, c.tokens, c.hidden, c.parts) == (
+        S.SIFAR_BF16, S.SIFAR_FP32, T, H, 2)
+    assert (c.branch_scale, c.residual_scale, c.weight_offset) == (0.5, 2.0, 1.0)
+    assert abs(c.eps - 1e-5) < 1e-11
+    for name in ("x", "post_weight", "gate", "residual", "residual_out", "norm_weight", "y"):
+        assert getattr(c, name) == t[name].data_ptr(), name
+    assert (c.x_stride, c.part_stride, c.gate_stride, c.residual_stride, c.residual_out_stride,
+            c.y_stride) == (H, T * H, 0, H, 2 * H, H)
+    S.sifar_block_norm(**tensors(x=t["x"][0], gate=torch.zeros(T, H, dtype=torch.bfloat16),
+                                 residual=None, norm_weight=None, y=None, post_weight=None))
+    c = recorder.calls[1]
+    assert (c.parts, c.gate_stride, c.residual, c.norm_weight, c.y, c.post_weight) == (
+        1, H, None, None, None, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(x=torch.zeros(T, H, dtype=torch.float64)), dict(x=torch.zeros(H)),
+    dict(x=torch.zeros(2, 2, T, H)), dict(x=torch.zeros(9, T, H, dtype=torch.bfloat16)),
+    dict(x=torch.zeros(T, H)),                                       # the others are bf16
+    dict(x=torch.zeros(T, 2 * H, dtype=torch.bfloat16)[:, ::2]),
+    dict(residual_out=torch.zeros(T, H + 8)), dict(residual_out=None),
+    dict(residual_out=torch.zeros(H, T).t()),
+    dict(residual=torch.zeros(T, H, dtype=torch.bfloat16)),          # not residual_out's type
+    dict(gate=torch.zeros(T + 1, H, dtype=torch.bfloat16)),
+    dict(gate=torch.zeros(1, T, H, dtype=torch.bfloat16)),
+    dict(norm_weight=torch.zeros(T, H, dtype=torch.bfloat16)), dict(norm_weight=None),
+    dict(y=None), dict(post_weight=torch.zeros(H + 8, dtype=torch.bfloat16)),
+], ids=range(16))
+def test_refused_by_the_binding(recorder, kw):
+    with pytest.raises(S.SifarError) as e:
+        S.sifar_block_norm(**tensors(**kw))
+    assert e.value.code == S.SIFAR_EINVAL and not recorder.calls
+
+
+def test_host_tensors_are_refused():
+    with pytest.raises(S.SifarError) as e:
+        S.sifar_block_norm(**tensors())
+    assert e.value.code == S.SIFAR_EINVAL
