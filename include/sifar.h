@@ -570,6 +570,59 @@ typedef struct {
 } sifar_block_norm_args;
 int sifar_block_norm(const sifar_block_norm_args *a, void *stream);
 
+/* Routing to experts. Per token t, with x its logits:
+ *
+ *   s_e = softmax(x)_e, or 1 / (1 + exp(-x_e))     (0 below 2^-1000)
+ *   c_e = s_e + bias_e                      in 64 bits; bias NULL: 0
+ *   a group's worth = its best c, or (group_top 2) the sum of its best two;
+ *     only experts of the top_groups best groups stay
+ *   ids      = the topk best experts that stay, by c, best first; without a bias
+ *              by x (the same order, also where s saturates)
+ *   weights  = s of the chosen (without the bias), divided by their sum if
+ *              renorm (0 where the sum is 0), times scale
+ *
+ * Ties go to the lowest index, of experts and of groups (values of c that agree
+ * to 2^-42 of themselves count as equal). An expert is not there for a token
+ * whose logit is -inf or NaN, or whose c is -inf or NaN: it is never chosen,
+ * and its group's worth counts the others (best two: the one, if there is only
+ * one). Where fewer than topk are left, the rest of ids is -1 with weight 0.
+ * Logits of the type's lowest finite value are ordinary logits. Where logits are
+ * +inf, softmax shares 1 among them.
+ *
+ *   logits   [tokens][experts] dtype, rows logits_stride elements apart
+ *   bias     [experts] fp32, or NULL
+ *   ids, weights  [tokens][topk] int32 and fp32, contiguous
+ *
+ * Experts are grouped in equal runs of adjacent indices; groups = 1 (then
+ * top_groups = 1) for none. Limits: experts 1..SIFAR_ROUTE_MAX_EXPERTS and a
+ * multiple of groups; groups 1..SIFAR_ROUTE_MAX_GROUPS; topk
+ * 1..SIFAR_ROUTE_MAX_TOPK and at most experts; 0 <= tokens <=
+ * SIFAR_ROWS_MAX_TOKENS; group_top 1 or 2; pointers aligned to their elements.
+ * Outputs that overlap each other or an input are refused. One launch. */
+#define SIFAR_ROUTE_SOFTMAX 0
+#define SIFAR_ROUTE_SIGMOID 1
+#define SIFAR_ROUTE_MAX_EXPERTS 1024
+#define SIFAR_ROUTE_MAX_GROUPS 32
+#define SIFAR_ROUTE_MAX_TOPK 32
+typedef struct {
+    int32_t dtype;
+    int32_t tokens;
+    int32_t experts;
+    int32_t topk;
+    int32_t score;
+    int32_t groups;
+    int32_t top_groups;
+    int32_t group_top;
+    int32_t renorm;
+    float scale;
+    const void *logits;
+    int64_t logits_stride;
+    const float *bias;
+    int32_t *ids;
+    float *weights;
+} sifar_route_args;
+int sifar_route(const sifar_route_args *a, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -72,6 +72,12 @@ SIFAR_BF16 = 0
 SIFAR_FP16 = 1
 SIFAR_FP32 = 2
 SIFAR_ROWS_MAX_TOKENS = 1048576
+SIFAR_ROUTE_SOFTMAX = 0
+SIFAR_ROUTE_SIGMOID = 1
+SIFAR_ROUTE_MAX_EXPERTS = 1024
+SIFAR_ROUTE_MAX_GROUPS = 32
+SIFAR_ROUTE_MAX_TOPK = 32
+ROUTE_SCORE = {"softmax": 0, "sigmoid": 1}
 
 CHUNK = 512  # elements per chunk (one 64-lane wave, 16 bytes per lane)
 
@@ -83,6 +89,7 @@ EXPORTS = (
     "sifar_read_log", "sifar_read_stamp_log", "sifar_read_placement",
     "sifar_epochs", "sifar_status", "sifar_error_info", "sifar_strerror", "sifar_floor",
     "sifar_litmus", "sifar_allreduce_noalloc", "sifar_block_norm",
+    "sifar_route",
 )
 
 
@@ -160,6 +167,26 @@ class sifar_block_norm_args(ctypes.Structure):
     ]
 
 
+class sifar_route_args(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("tokens", ctypes.c_int32),
+        ("experts", ctypes.c_int32),
+        ("topk", ctypes.c_int32),
+        ("score", ctypes.c_int32),
+        ("groups", ctypes.c_int32),
+        ("top_groups", ctypes.c_int32),
+        ("group_top", ctypes.c_int32),
+        ("renorm", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("logits", ctypes.c_void_p),
+        ("logits_stride", ctypes.c_int64),
+        ("bias", ctypes.c_void_p),
+        ("ids", ctypes.c_void_p),
+        ("weights", ctypes.c_void_p),
+    ]
+
+
 class SifarError(RuntimeError):
     def __init__(self, fn: str, code: int, info=None):
         msg = f"{fn} failed: {code} ({strerror(code)})"
@@ -213,6 +240,7 @@ def load(path: str = LIB_PATH):
                                         ctypes.POINTER(sifar_litmus_result)]),
         "sifar_allreduce_noalloc": (ctypes.c_int, [P, I64, I32, I32, I32, P, P]),
         "sifar_block_norm": (ctypes.c_int, [P, P]),
+        "sifar_route": (ctypes.c_int, [P, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -405,6 +433,7 @@ def sifar_allreduce_noalloc(src, src_rank_stride: int, nranks: int, tokens: int,
 # layout): filling a ctypes structure of 22 fields takes longer than the launch.
 
 _BLOCK_NORM = struct.Struct("@5i4fP2q2PqPqPq2Pq")
+_ROUTE = struct.Struct("@9if1Pq3P")
 _DTYPES = None  # torch dtype -> SIFAR_* element type
 
 
@@ -498,6 +527,37 @@ def sifar_block_norm(x, residual, residual_out, post_weight=None, gate=None, nor
                          residual_scale, weight_offset, eps, x.data_ptr(), at[0], part_stride,
                          post, g, g_stride, res, res_stride, out, out_stride, norm, yp, y_stride),
         _stream(stream))
+    if rc:
+        _check(fn, rc)
+
+
+def sifar_route(logits, ids, weights, score="softmax", bias=None, groups=1, top_groups=1,
+                group_top=1, renorm=True, scale=1.0, stream=None) -> None:
+    """logits [tokens][experts]; ids (int32) and weights (float32) [tokens][topk], contiguous;
+    bias [experts] float32; score "softmax" or "sigmoid"."""
+    import torch
+    fn = "sifar_route"
+    if logits.dim() != 2 or ids.dim() != 2:
+        _refuse(fn, "logits or ids do not have 2 dimensions")
+    T, E = logits.shape
+    out, k = ids.shape, ids.shape[1]
+    if T > SIFAR_ROWS_MAX_TOKENS or E > SIFAR_ROUTE_MAX_EXPERTS or k > SIFAR_ROUTE_MAX_TOPK:
+        _refuse(fn, f"{T} x {E}, top {k}, is too large")
+    if out[0] != T:
+        _refuse(fn, f"ids has {out[0]} rows, logits {T}")
+    dev = _gpu(fn, "logits", logits)
+    x, x_stride = _operand(fn, "logits", logits, logits.dtype, logits.shape, dev)
+    i, i_stride = _operand(fn, "ids", ids, torch.int32, out, dev)
+    w, w_stride = _operand(fn, "weights", weights, torch.float32, out, dev)
+    if T > 1 and (i_stride != k or w_stride != k):
+        _refuse(fn, "the rows of ids or weights are not adjacent")
+    b = 0 if bias is None else _operand(fn, "bias", bias, torch.float32, logits.shape[1:], dev)[0]
+    mode = ROUTE_SCORE.get(score, score)
+    if mode not in (SIFAR_ROUTE_SOFTMAX, SIFAR_ROUTE_SIGMOID):
+        _refuse(fn, f"no score {score!r}")
+    rc = load().sifar_route(
+        _ROUTE.pack(_dtype(fn, logits.dtype), T, E, k, mode, groups, top_groups, group_top,
+                    1 if renorm else 0, scale, x, x_stride, b, i, w), _stream(stream))
     if rc:
         _check(fn, rc)
 

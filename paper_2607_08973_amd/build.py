@@ -16,7 +16,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libsifar.so")
 SOURCES = [os.path.join(CSRC, "kernels.hip"), os.path.join(CSRC, "floors.hip"),
            os.path.join(CSRC, "litmus.hip"), os.path.join(CSRC, "noalloc.hip"),
-           os.path.join(CSRC, "block_norm.hip"), os.path.join(CSRC, "api.cpp")]
+           os.path.join(CSRC, "block_norm.hip"), os.path.join(CSRC, "route.hip"),
+           os.path.join(CSRC, "api.cpp")]
 ARCH = "gfx950"
 
 FLAGS = [

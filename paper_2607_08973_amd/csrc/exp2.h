@@ -1,0 +1,41 @@
+// 2^t in 64 bits, for the row operators that rank scores or add up weights where
+// 32 bits would let a neighbour win. Plain C++ for host and device.
+//
+// t = i + f with i the nearest integer: 2^t = 2^i (1 + f q(f)), |f| <= 1/2. q
+// interpolates (2^f - 1) / f at Chebyshev nodes; its degree sets the error
+// (tests/test_exp2.py measures both against 80-bit arithmetic). f = 0 gives 1
+// exactly. One fma per degree: on gfx950 a 64-bit fma issues at the rate of an
+// unpacked 32-bit one, so 64 bits cost the longer polynomial and nothing else.
+#pragma once
+
+#if defined(__HIPCC__)
+#define SIFAR_HD __host__ __device__ __forceinline__
+#else
+#define SIFAR_HD inline
+#endif
+
+namespace sifar {
+
+// 1 + f q(f), relative error below 3e-16.
+SIFAR_HD double exp2_fraction(double f) {
+    double q = 0x1.e9d4d5f786506p-32;
+    q = __builtin_fma(q, f, 0x1.e606425df1ca8p-28);
+    q = __builtin_fma(q, f, 0x1.b524fa5b1918cp-24);
+    q = __builtin_fma(q, f, 0x1.62bfd475ca6bdp-20);
+    q = __builtin_fma(q, f, 0x1.ffcbfc674abbep-17);
+    q = __builtin_fma(q, f, 0x1.43091309706fcp-13);
+    q = __builtin_fma(q, f, 0x1.5d87fe78a51d0p-10);
+    q = __builtin_fma(q, f, 0x1.3b2ab6fba1dd8p-7);
+    q = __builtin_fma(q, f, 0x1.c6b08d704a0c2p-5);
+    q = __builtin_fma(q, f, 0x1.ebfbdff82c598p-3);
+    q = __builtin_fma(q, f, 0x1.62e42fefa39efp-1);
+    return __builtin_fma(q, f, 1.0);
+}
+
+// 2^t for |t| <= 1020.
+SIFAR_HD double exp2_64(double t) {
+    const double i = __builtin_rint(t);
+    return __builtin_ldexp(exp2_fraction(t - i), static_cast<int>(i));
+}
+
+}  // namespace sifar

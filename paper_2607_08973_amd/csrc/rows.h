@@ -149,6 +149,22 @@ __device__ __forceinline__ T wave_reduce(T v, Op op) {
     return v;
 }
 
+// Lane `from`'s value (the same lane for the whole wave), in scalar registers.
+template <class T>
+__device__ __forceinline__ T lane_value(T x, int from) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(
+            T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), from));
+    } else {
+        const uint64_t b = __builtin_bit_cast(uint64_t, x);
+        const uint32_t lo = static_cast<uint32_t>(
+            __builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(b)), from));
+        const uint32_t hi = static_cast<uint32_t>(
+            __builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(b >> 32)), from));
+        return __builtin_bit_cast(T, (static_cast<uint64_t>(hi) << 32) | lo);
+    }
+}
+
 struct Add {
     template <class T>
     __device__ __forceinline__ T operator()(T a, T b) const { return a + b; }

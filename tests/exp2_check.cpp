@@ -1,0 +1,29 @@
+// Host-side check of exp2.h against 80-bit arithmetic. Built and run by
+// tests/test_exp2.py on the CPU.
+#include <cmath>
+#include <cstdio>
+#include <random>
+
+#include "exp2.h"
+
+int main() {
+    std::mt19937_64 rng(260708973);
+    std::uniform_real_distribution<double> frac(-0.5, 0.5), wide(-1020.0, 1020.0);
+    long double worst = 0;
+    const auto see = [&](double t) {
+        const long double want = exp2l(static_cast<long double>(t));
+        const long double e = fabsl(static_cast<long double>(sifar::exp2_64(t)) / want - 1);
+        if (e > worst) worst = e;
+    };
+    for (int i = 0; i < 2000000; ++i) {
+        see(frac(rng));
+        see(wide(rng));
+    }
+    for (int i = -1020; i <= 1020; ++i) {
+        if (sifar::exp2_64(i) != std::ldexp(1.0, i)) return std::printf("2^%d\n", i), 1;
+        see(i + 0.5);
+        see(std::nextafter(i + 0.5, 0.0));
+    }
+    std::printf("%.3Le\n", worst);
+    return worst < 3e-16L ? 0 : 1;
+}
