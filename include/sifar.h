@@ -623,6 +623,64 @@ typedef struct {
 } sifar_route_args;
 int sifar_route(const sifar_route_args *a, void *stream);
 
+/* Sampling. Per row t, with x its logits and T its temperature:
+ *
+ *   w_i = exp((x_i - max x) / T), 0 below 2^-60 (a token 2^60 times less likely
+ *         than the likeliest is never drawn)
+ *   order: by x, best first, equal ones by index
+ *   top-k   keeps the first top_k                          (top_k <= 0: all)
+ *   top-p   of these, the fewest whose weight is at least top_p times theirs,
+ *           one at least                                   (not < 1: all)
+ *   min-p   of these, those with w >= min_p                (not > 0: all; above 1
+ *           counts as 1)
+ *   token   the first, in index order over what is kept, at which the running sum
+ *           of w exceeds uniform times the kept weight
+ *   prob    w_token / kept weight
+ *
+ * A temperature that is not above 0 takes the first token in the order, with
+ * prob 1. A logit of -inf or NaN is not there; a row without any other gives
+ * token -1 and prob 0. Masks of the type's lowest finite value are as good as
+ * -inf at ordinary temperatures (below 1000 with fp16's -65504). Where logits
+ * are +inf, they share the weight. uniform belongs in [0, 1); below 0 or NaN
+ * counts as 0, and 1 or above draws the last token kept.
+ *
+ * Sums are exact integers in units of 2^-42 of the largest weight, so the token
+ * does not depend on the order of addition: ranks that hold equal logits draw
+ * equal tokens from equal random numbers.
+ *
+ *   logits    [tokens][vocab] dtype, rows logits_stride elements apart
+ *   uniform, temperature, top_k, top_p, min_p   [tokens] fp32 (top_k: int32);
+ *             all but uniform may be NULL: temperature 1, no filter
+ *   out       [tokens] int32;  probs  [tokens] fp32, or NULL
+ *   workspace at least sifar_sample_workspace(tokens, vocab) bytes, 16-byte
+ *             aligned, caller-owned, in any state before and after. Calls that
+ *             may run at the same time need one each.
+ *
+ * Limits: 1 <= vocab <= SIFAR_SAMPLE_MAX_VOCAB; 0 <= tokens <=
+ * SIFAR_ROWS_MAX_TOKENS; pointers aligned to their elements. Outputs and
+ * workspace that overlap each other or an input are refused. Two launches. */
+#define SIFAR_SAMPLE_MAX_VOCAB 1048576
+typedef struct {
+    int32_t dtype;
+    int32_t tokens;
+    int32_t vocab;
+    const void *logits;
+    int64_t logits_stride;
+    const float *uniform;
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p;
+    const float *min_p;
+    int32_t *out;
+    float *probs;
+    void *workspace;
+    int64_t workspace_bytes;
+} sifar_sample_args;
+int sifar_sample(const sifar_sample_args *a, void *stream);
+
+/* Bytes of workspace that sifar_sample needs, or SIFAR_EINVAL. */
+int64_t sifar_sample_workspace(int32_t tokens, int32_t vocab);
+
 #ifdef __cplusplus
 }
 #endif

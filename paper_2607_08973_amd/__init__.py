@@ -77,6 +77,7 @@ SIFAR_ROUTE_SIGMOID = 1
 SIFAR_ROUTE_MAX_EXPERTS = 1024
 SIFAR_ROUTE_MAX_GROUPS = 32
 SIFAR_ROUTE_MAX_TOPK = 32
+SIFAR_SAMPLE_MAX_VOCAB = 1048576
 ROUTE_SCORE = {"softmax": 0, "sigmoid": 1}
 
 CHUNK = 512  # elements per chunk (one 64-lane wave, 16 bytes per lane)
@@ -89,7 +90,7 @@ EXPORTS = (
     "sifar_read_log", "sifar_read_stamp_log", "sifar_read_placement",
     "sifar_epochs", "sifar_status", "sifar_error_info", "sifar_strerror", "sifar_floor",
     "sifar_litmus", "sifar_allreduce_noalloc", "sifar_block_norm",
-    "sifar_route",
+    "sifar_route", "sifar_sample", "sifar_sample_workspace",
 )
 
 
@@ -187,6 +188,25 @@ class sifar_route_args(ctypes.Structure):
     ]
 
 
+class sifar_sample_args(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("tokens", ctypes.c_int32),
+        ("vocab", ctypes.c_int32),
+        ("logits", ctypes.c_void_p),
+        ("logits_stride", ctypes.c_int64),
+        ("uniform", ctypes.c_void_p),
+        ("temperature", ctypes.c_void_p),
+        ("top_k", ctypes.c_void_p),
+        ("top_p", ctypes.c_void_p),
+        ("min_p", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("probs", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
 class SifarError(RuntimeError):
     def __init__(self, fn: str, code: int, info=None):
         msg = f"{fn} failed: {code} ({strerror(code)})"
@@ -241,6 +261,8 @@ def load(path: str = LIB_PATH):
         "sifar_allreduce_noalloc": (ctypes.c_int, [P, I64, I32, I32, I32, P, P]),
         "sifar_block_norm": (ctypes.c_int, [P, P]),
         "sifar_route": (ctypes.c_int, [P, P]),
+        "sifar_sample": (ctypes.c_int, [P, P]),
+        "sifar_sample_workspace": (I64, [I32, I32]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -434,6 +456,7 @@ def sifar_allreduce_noalloc(src, src_rank_stride: int, nranks: int, tokens: int,
 
 _BLOCK_NORM = struct.Struct("@5i4fP2q2PqPqPq2Pq")
 _ROUTE = struct.Struct("@9if1Pq3P")
+_SAMPLE = struct.Struct("@3iPq8Pq")
 _DTYPES = None  # torch dtype -> SIFAR_* element type
 
 
@@ -558,6 +581,47 @@ def sifar_route(logits, ids, weights, score="softmax", bias=None, groups=1, top_
     rc = load().sifar_route(
         _ROUTE.pack(_dtype(fn, logits.dtype), T, E, k, mode, groups, top_groups, group_top,
                     1 if renorm else 0, scale, x, x_stride, b, i, w), _stream(stream))
+    if rc:
+        _check(fn, rc)
+
+
+def sifar_sample_workspace(tokens: int, vocab: int) -> int:
+    """Bytes of workspace that sifar_sample needs."""
+    fn = "sifar_sample_workspace"
+    if tokens > SIFAR_ROWS_MAX_TOKENS or vocab > SIFAR_SAMPLE_MAX_VOCAB:
+        _refuse(fn, f"{tokens} x {vocab} is too large")
+    n = load().sifar_sample_workspace(tokens, vocab)
+    if n < 0:
+        _check(fn, n)
+    return n
+
+
+def sifar_sample(logits, uniform, out, workspace, probs=None, temperature=None, top_k=None,
+                 top_p=None, min_p=None, stream=None) -> None:
+    """logits [tokens][vocab]; uniform, temperature, top_p, min_p float32 [tokens], top_k and out
+    int32 [tokens], probs float32 [tokens]; workspace: a contiguous uint8 tensor of
+    sifar_sample_workspace(tokens, vocab) bytes, not shared by calls that may overlap."""
+    import torch
+    fn = "sifar_sample"
+    if logits.dim() != 2:
+        _refuse(fn, f"logits has {logits.dim()} dimensions, not 2")
+    T, V = logits.shape
+    if T > SIFAR_ROWS_MAX_TOKENS or V > SIFAR_SAMPLE_MAX_VOCAB:
+        _refuse(fn, f"{T} x {V} is too large")
+    dev = _gpu(fn, "logits", logits)
+    rows, f32, i32 = logits.shape[:1], torch.float32, torch.int32
+    x, x_stride = _operand(fn, "logits", logits, logits.dtype, logits.shape, dev)
+    u, _ = _operand(fn, "uniform", uniform, f32, rows, dev)
+    o, _ = _operand(fn, "out", out, i32, rows, dev)
+    ws, _ = _operand(fn, "workspace", workspace, torch.uint8, workspace.shape[:1], dev)
+    p = 0 if probs is None else _operand(fn, "probs", probs, f32, rows, dev)[0]
+    t = 0 if temperature is None else _operand(fn, "temperature", temperature, f32, rows, dev)[0]
+    k = 0 if top_k is None else _operand(fn, "top_k", top_k, i32, rows, dev)[0]
+    tp = 0 if top_p is None else _operand(fn, "top_p", top_p, f32, rows, dev)[0]
+    mp = 0 if min_p is None else _operand(fn, "min_p", min_p, f32, rows, dev)[0]
+    rc = load().sifar_sample(
+        _SAMPLE.pack(_dtype(fn, logits.dtype), T, V, x, x_stride, u, t, k, tp, mp, o, p, ws,
+                     workspace.shape[0]), _stream(stream))
     if rc:
         _check(fn, rc)
 
