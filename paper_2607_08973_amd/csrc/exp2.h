@@ -32,6 +32,20 @@ SIFAR_HD double exp2_fraction(double f) {
     return __builtin_fma(q, f, 1.0);
 }
 
+// The same with a relative error below 4e-14: for sums in units of 2^-42.
+SIFAR_HD double exp2_fraction9(double f) {
+    double q = 0x1.b638808675ca6p-24;
+    q = __builtin_fma(q, f, 0x1.63d136355f669p-20);
+    q = __builtin_fma(q, f, 0x1.ffcb9515c8f1ap-17);
+    q = __builtin_fma(q, f, 0x1.4308ac85abb17p-13);
+    q = __builtin_fma(q, f, 0x1.5d87fe86fe7ccp-10);
+    q = __builtin_fma(q, f, 0x1.3b2ab7181b74ap-7);
+    q = __builtin_fma(q, f, 0x1.c6b08d7047e52p-5);
+    q = __builtin_fma(q, f, 0x1.ebfbdff823cedp-3);
+    q = __builtin_fma(q, f, 0x1.62e42fefa39efp-1);
+    return __builtin_fma(q, f, 1.0);
+}
+
 // 2^t for |t| <= 1020.
 SIFAR_HD double exp2_64(double t) {
     const double i = __builtin_rint(t);

@@ -30,8 +30,11 @@ constexpr int kThreads = 1024;                 // of a pick workgroup
 constexpr int kPickWaves = kThreads / kRowWave;
 constexpr int kMaxChunks = SIFAR_SAMPLE_MAX_VOCAB / kChunkElems;
 constexpr int kBins = 64 + 26 * 64;            // log-linear bins of a 32-bit distance
-constexpr int kList = 4096;                    // candidates kept in LDS
+constexpr int kList = 8192;                    // candidates kept in LDS
+constexpr int kSmall = 256;                    // most candidates that are ranked by counting
 constexpr int kNucleus = 64;                   // chunk maxima a nucleus is first sought above
+constexpr int kNucleusMass = 128;              // most p * sum / largest weight of such a row
+constexpr int kPerBit = 64;                    // bins of a halving of the weight
 constexpr int kUnitBits = 42;                  // a weight of 1 in units
 constexpr double kLog2e = 1.4426950408889634;
 constexpr double kLn2 = 0.6931471805599453;
@@ -132,6 +135,24 @@ __device__ __forceinline__ double log2_weight(float x, float max, double c) {
     return x == max ? 0.0 : z > -1100.0 ? z : -1100.0;
 }
 
+// The weight of a finite logit under a finite maximum, times 2^bits. Garbage, but
+// finite, for logits far below the cut; -inf and NaN come out as the lowest
+// finite logit.
+__device__ __forceinline__ double weight(float x, double max, double scale, int bits) {
+    const float y = fmaxf(x, -3.402823466e38f);
+    const double z = (static_cast<double>(y) - max) * scale;
+    const double i = __builtin_rint(z);
+    return __builtin_ldexp(exp2_fraction9(z - i), static_cast<int>(i) + bits);
+}
+
+__device__ __forceinline__ double max64(double a, double b) {
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+
+// A chunk's maximum and, where the row needs it, the sum of its weights. What
+// top-k keeps is summed when it is known, and so is what min-p alone keeps.
 template <int D>
 __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const SampleArgs n) {
     const sifar_sample_args &a = n.a;
@@ -149,12 +170,18 @@ __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const Sample
     for (int i = 0; i < kPer; ++i) m = fmaxf(m, x[i]);
     m = wave_reduce(m, Max{});
     double mass = 0.0;
-    // top-k rows add up their own few weights, min-p rows those above a known logit
-    if (!d.greedy && d.top_k <= 0 && !(d.min_p > 0.0f && !(d.top_p < 1.0f)) && m > none) {
+    if (!d.greedy && d.top_k <= 0 && (d.top_p < 1.0f || !(d.min_p > 0.0f)) && m > none) {
         const double scale = kLog2e / static_cast<double>(d.temperature);
+        if (m < __builtin_inff()) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            mass += x[i] > none ? exp2_64(log2_weight(x[i], m, scale)) : 0.0;
+            for (int i = 0; i < kPer; ++i) {
+                const double w = weight(x[i], m, scale, 0);
+                mass += x[i] > none ? w : 0.0;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) mass += x[i] == m ? 1.0 : 0.0;
+        }
         mass = wave_reduce(mass, Add{});
     }
     if (lane == 0)
@@ -164,20 +191,23 @@ __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const Sample
 // ---- pick_kernel -----------------------------------------------------------------
 
 struct Shared {
-    uint64_t hist[kBins];
+    uint64_t hist[kBins];                // also the candidates in order, or the chunks' ranks
     uint64_t chunk_units[kMaxChunks];
     uint32_t chunk_ties[kMaxChunks];
-    uint32_t chunk_key[kMaxChunks];  // of the chunk's maximum
-    uint32_t list_key[kList];
+    uint32_t chunk_key[kMaxChunks];      // of the chunk's maximum
+    uint32_t queue[kMaxChunks];          // chunks to be read
+    uint32_t list_key[kList];            // candidates
     uint32_t list_at[kList];
+    uint32_t rank[kThreads];
+    uint64_t sums[kSmall];
     uint64_t wave_sum[kPickWaves];
     uint32_t wave_max[kPickWaves];
     uint64_t found_before;
     uint32_t found_bin;
-    uint32_t list_size;
-    uint32_t bound;      // of the candidates
-    uint32_t chosen;     // the token's chunk,
-    uint64_t chosen_at;  // the units before the token in it
+    uint32_t list_size, queue_size;
+    uint32_t bound;        // of the candidates
+    uint32_t chosen;       // the token's chunk,
+    uint64_t chosen_at;    // the units before the token in it
     uint64_t chosen_ties;  // and the ties before the chunk
 };
 
@@ -185,25 +215,35 @@ __device__ __forceinline__ void add(uint64_t &sum, uint64_t x) {  // in LDS
     atomicAdd(reinterpret_cast<unsigned long long *>(&sum), static_cast<unsigned long long>(x));
 }
 
-__device__ __forceinline__ uint64_t shuffle_up(uint64_t x, int by) {
-    return __shfl_up(static_cast<unsigned long long>(x), by);
+// Inclusive sum over the lanes below: DPP moves within rows of 16, then the last
+// lane of a row, and of the lower half, to the rows above. (Shuffles through LDS
+// took six times as long, and a row's walk has a dozen of these.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t add_from(uint64_t x) {
+    const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(static_cast<uint32_t>(x)), CTRL,
+                                               ROWS, 0xF, false);
+    const int hi = __builtin_amdgcn_update_dpp(
+        0, static_cast<int>(static_cast<uint32_t>(x >> 32)), CTRL, ROWS, 0xF, false);
+    return x + ((static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32) |
+                static_cast<uint32_t>(lo));
 }
 
-__device__ __forceinline__ uint64_t wave_scan(uint64_t x, int lane) {  // inclusive
-#pragma unroll
-    for (int by = 1; by < kRowWave; by *= 2) {
-        const uint64_t y = shuffle_up(x, by);
-        if (lane >= by) x += y;
-    }
+__device__ __forceinline__ uint64_t wave_scan(uint64_t x) {
+    x = add_from<0x111, 0xF>(x);  // row_shr:1
+    x = add_from<0x112, 0xF>(x);
+    x = add_from<0x114, 0xF>(x);
+    x = add_from<0x118, 0xF>(x);
+    x = add_from<0x142, 0xA>(x);  // row_bcast:15 into rows 1 and 3
+    x = add_from<0x143, 0xC>(x);  // row_bcast:31 into rows 2 and 3
     return x;
 }
 
 // Exclusive sum over the workgroup's threads, and the whole sum.
 __device__ __forceinline__ uint64_t block_scan(Shared &s, uint64_t x, uint64_t &total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t inc = wave_scan(x, lane);
+    const int wave = threadIdx.x >> 6;
+    const uint64_t inc = wave_scan(x);
     __syncthreads();  // wave_sum may still be read from the call before
-    if (lane == 63) s.wave_sum[wave] = inc;
+    if ((threadIdx.x & 63) == 63) s.wave_sum[wave] = inc;
     __syncthreads();
     uint64_t before = 0;
     total = 0;
@@ -214,6 +254,12 @@ __device__ __forceinline__ uint64_t block_scan(Shared &s, uint64_t x, uint64_t &
         total += v;
     }
     return before + inc - x;
+}
+
+__device__ __forceinline__ uint64_t block_sum(Shared &s, uint64_t x) {
+    uint64_t total;
+    block_scan(s, x, total);
+    return total;
 }
 
 __device__ __forceinline__ uint32_t block_max(Shared &s, uint32_t x) {
@@ -227,6 +273,31 @@ __device__ __forceinline__ uint32_t block_max(Shared &s, uint32_t x) {
     return m;
 }
 
+// Key, then lower index: sorts as the order of the draw.
+__device__ __forceinline__ uint64_t order_of(uint32_t key, uint32_t at) {
+    return (static_cast<uint64_t>(key) << 32) | static_cast<uint32_t>(~at);
+}
+
+// Into s.rank[e]: how many of the first n values of `order` are above the e-th. Up
+// to 256 values the workgroup splits each one's comparisons four ways.
+__device__ __forceinline__ void rank_all(Shared &s, const uint64_t *order, int n) {
+    const int span = n <= kThreads / 4 ? kThreads / 4 : n <= kThreads / 2 ? kThreads / 2 : kThreads;
+    const int parts = kThreads / span;
+    const int e = threadIdx.x & (span - 1), part = threadIdx.x / span;
+    s.rank[threadIdx.x] = 0;
+    __syncthreads();
+    if (e < n) {
+        const int each = (n + parts - 1) / parts;
+        const int end = each * (part + 1) < n ? each * (part + 1) : n;
+        const uint64_t mine = order[e];
+        uint32_t above = 0;
+#pragma unroll 4
+        for (int j = each * part; j < end; ++j) above += order[j] > mine;
+        atomicAdd(&s.rank[e], above);
+    }
+    __syncthreads();
+}
+
 // A row in pick_kernel.
 template <int D>
 struct Row {
@@ -234,36 +305,69 @@ struct Row {
     int vocab, chunks;
     float max;
     double scale;  // log2(e) / temperature
+    bool finite;   // the maximum is; otherwise the infinite logits share the weight
 
     // a weight in units; at least one, so that what may be drawn can be
+    __device__ __forceinline__ double units_of(float x) const {
+        return __builtin_rint(max64(weight(x, max, scale, kUnitBits), 1.0));
+    }
     __device__ __forceinline__ uint64_t units(uint32_t key) const {
-        const double t = log2_weight(value_of(key), max, scale);
-        const double i = __builtin_rint(t);
-        const double w =
-            __builtin_ldexp(exp2_fraction(t - i), static_cast<int>(i) + kUnitBits);
-        const uint64_t u = __builtin_bit_cast(uint64_t, w + 0x1p52) & ((uint64_t{1} << 52) - 1);
-        return u > 0 ? u : 1;
+        return finite ? static_cast<uint64_t>(units_of(value_of(key))) : uint64_t{1} << kUnitBits;
     }
 };
+
+// The chunks whose maximum reaches `least`, in no order.
+__device__ __forceinline__ uint32_t queue_chunks(Shared &s, int chunks, uint32_t least) {
+    __syncthreads();
+    if (threadIdx.x == 0) s.queue_size = 0;
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) < chunks && s.chunk_key[threadIdx.x] >= least)
+        s.queue[atomicAdd(&s.queue_size, 1u)] = threadIdx.x;
+    __syncthreads();
+    return s.queue_size;
+}
+
+// f(logits of a lane, chunk) over the queued chunks, a wave a chunk, the next one
+// loaded while one is worked on.
+template <int D, class F>
+__device__ __forceinline__ void each_chunk(const Shared &s, const Row<D> &r, uint32_t size, F f) {
+    const int lane = threadIdx.x & 63;
+    uint32_t q = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (q >= size) return;
+    float x[kPer], next[kPer];
+    int c = __builtin_amdgcn_readfirstlane(s.queue[q]);
+    load_chunk<D>(r.logits, r.vocab, c, lane, next);
+    while (true) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) x[i] = next[i];
+        const int at = c;
+        q += kPickWaves;
+        const bool more = q < size;
+        if (more) {
+            c = __builtin_amdgcn_readfirstlane(s.queue[q]);
+            load_chunk<D>(r.logits, r.vocab, c, lane, next);
+        }
+        f(x, at);
+        if (!more) return;
+    }
+}
 
 // Where weights are sought: the row's chunks whose maximum reaches `least`...
 template <int D>
 struct InRow {
-    const Shared &s;
+    Shared &s;
     const Row<D> &r;
     template <class F>
     __device__ __forceinline__ void each(uint32_t least, F f) const {
         const int lane = threadIdx.x & 63;
-        for (int c = threadIdx.x >> 6; c < r.chunks; c += kPickWaves) {
-            if (s.chunk_key[c] < least) continue;
-            float x[kPer];
-            load_chunk<D>(r.logits, r.vocab, c, lane, x);
+        const uint32_t size = queue_chunks(s, r.chunks, least);
+        each_chunk(s, r, size, [&](const float(&x)[kPer], int c) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const uint32_t k = key_of(x[i]);
                 if (k >= least) f(k, chunk_at<D>(c, lane, i));
             }
-        }
+        });
     }
 };
 
@@ -278,51 +382,47 @@ struct InList {
     }
 };
 
+__device__ __forceinline__ void to_list(Shared &s, uint32_t key, int at) {
+    const uint32_t i = atomicAdd(&s.list_size, 1u);
+    if (i < kList) {
+        s.list_key[i] = key;
+        s.list_at[i] = static_cast<uint32_t>(at);
+    }
+}
+
 // Candidates from key `least` to `most` into the list, in no order. False if they
 // do not fit.
-template <class From>
-__device__ __forceinline__ bool collect(Shared &s, const From &from, uint32_t least, uint32_t most) {
-    __syncthreads();
-    if (threadIdx.x == 0) s.list_size = 0;
-    __syncthreads();
+template <int D>
+__device__ __forceinline__ bool collect(Shared &s, const InRow<D> &from, uint32_t least,
+                                        uint32_t most) {
+    if (threadIdx.x == 0) s.list_size = 0;  // each() waits before it reads or adds
     from.each(least, [&](uint32_t k, int at) {
-        if (k > most) return;
-        const uint32_t i = atomicAdd(&s.list_size, 1u);
-        if (i < kList) {
-            s.list_key[i] = k;
-            s.list_at[i] = static_cast<uint32_t>(at);
-        }
+        if (k <= most) to_list(s, k, at);
     });
     __syncthreads();
     return s.list_size <= kList;
 }
 
-// The bin in which the running sum over bins reaches target (>= 1, at most the
-// whole sum), and the sum before it.
-__device__ __forceinline__ void find_bin(Shared &s, int bins, uint64_t target, uint32_t &bin,
+// The bin in which the running sum over bins reaches target (>= 1), and the sum
+// before it; false if the whole sum does not reach it.
+__device__ __forceinline__ bool find_bin(Shared &s, int bins, uint64_t target, uint32_t &bin,
                                          uint64_t &before) {
-    constexpr int each = (kBins + kThreads - 1) / kThreads;
+    static_assert(kBins <= 2 * kThreads, "two bins a thread");
     __syncthreads();
-    uint64_t v[each], sum = 0;
-#pragma unroll
-    for (int i = 0; i < each; ++i) {
-        const int b = threadIdx.x * each + i;
-        v[i] = b < bins ? s.hist[b] : 0;
-        sum += v[i];
-    }
+    const int b = 2 * threadIdx.x;
+    const uint64_t v0 = b < bins ? s.hist[b] : 0, v1 = b + 1 < bins ? s.hist[b + 1] : 0;
     uint64_t total;
-    uint64_t run = block_scan(s, sum, total);
-#pragma unroll
-    for (int i = 0; i < each; ++i) {
-        if (run < target && target <= run + v[i]) {
-            s.found_bin = threadIdx.x * each + i;
-            s.found_before = run;
-        }
-        run += v[i];
+    const uint64_t run = block_scan(s, v0 + v1, total);
+    if (total < target) return false;  // the same in every thread
+    if (run < target && target <= run + v0 + v1) {
+        const bool second = target > run + v0;
+        s.found_bin = second ? b + 1 : b;
+        s.found_before = second ? run + v0 : run;
     }
     __syncthreads();
     bin = s.found_bin;
     before = s.found_before;
+    return true;
 }
 
 __device__ __forceinline__ void clear_bins(Shared &s) {
@@ -332,22 +432,20 @@ __device__ __forceinline__ void clear_bins(Shared &s) {
 }
 
 struct Border {
+    bool found;
     uint32_t key;     // of the element in which the running sum reaches the target
     uint64_t before;  // the sum over larger keys
 };
 
-// In descending order of keys from `top` down to, not including, `floor`: where
-// does the running sum of weights reach target? The whole sum has to reach it.
-// Histograms over the distance d = top - key: first log-linear bins, 64 to an
-// octave, over all 32 bits, then 1024 at a time inside the bin that was found.
+// seek() inside the bin [lo, lo + 2^bits) of distances from `top`.
 template <class From, class W>
 __device__ __forceinline__ Border narrow(Shared &s, const From &from, uint32_t top, uint32_t floor,
                                          uint32_t lo, int bits, uint64_t before, uint64_t target,
                                          W weight) {
     while (bits > 0) {
         const int shift = bits > 10 ? bits - 10 : 0;
-        const uint32_t last = lo + ((1u << bits) - 1);  // d of the bin's end
-        uint32_t least = last >= lo && top >= last ? top - last : 0;
+        const uint32_t last = lo + ((1u << bits) - 1);  // no more than 2^32 - 1: see seek()
+        uint32_t least = top >= last ? top - last : 0;
         if (least <= floor) least = floor + 1;
         clear_bins(s);
         from.each(least, [&](uint32_t k, int) {
@@ -356,17 +454,21 @@ __device__ __forceinline__ Border narrow(Shared &s, const From &from, uint32_t t
         });
         uint32_t bin;
         uint64_t in;
-        find_bin(s, 1024, target - before, bin, in);
+        if (!find_bin(s, 1024, target - before, bin, in)) return Border{false, 0, 0};
         before += in;
         lo += bin << shift;
         bits = shift;
     }
-    return Border{top - lo, before};
+    return Border{true, top - lo, before};
 }
 
+// In descending order of keys from `top` down to, not including, `floor`: where
+// does the running sum of weights reach target? Histograms over the distance
+// d = top - key: first log-linear bins, 64 to an octave, over all 32 bits, then
+// 1024 at a time inside the bin that was found.
 template <class From, class W>
-__device__ __forceinline__ Border seek(Shared &s, const From &from, bool in_list, uint32_t top,
-                                       uint32_t floor, uint64_t target, W weight) {
+__device__ __forceinline__ Border seek(Shared &s, const From &from, uint32_t top, uint32_t floor,
+                                       uint64_t target, W weight) {
     clear_bins(s);
     from.each(floor + 1, [&](uint32_t k, int) {
         const uint32_t d = top - k;
@@ -376,16 +478,19 @@ __device__ __forceinline__ Border seek(Shared &s, const From &from, bool in_list
     });
     uint32_t bin;
     uint64_t before;
-    find_bin(s, kBins, target, bin, before);
+    if (!find_bin(s, kBins, target, bin, before)) return Border{false, 0, 0};
+    // the last bin of 64 << 25 distances ends at 2^32 - 1
     const int bits = bin < 64 ? 0 : (bin - 64) / 64;
     const uint32_t lo = bin < 64 ? bin : (64 + (bin & 63)) << bits;
-    if (bits == 0) return Border{top - lo, before};
-    if (!in_list) {
-        const uint32_t last = lo + ((1u << bits) - 1);
-        uint32_t least = last >= lo && top >= last ? top - last : 0;
-        if (least <= floor) least = floor + 1;
-        if (collect(s, from, least, top - lo))
-            return narrow(s, InList{s, s.list_size}, top, floor, lo, bits, before, target, weight);
+    if constexpr (!std::is_same_v<From, InList>) {
+        if (bits > 0) {
+            const uint32_t last = lo + ((1u << bits) - 1);
+            uint32_t least = top >= last ? top - last : 0;
+            if (least <= floor) least = floor + 1;
+            if (collect(s, from, least, top - lo))
+                return narrow(s, InList{s, s.list_size}, top, floor, lo, bits, before, target,
+                              weight);
+        }
     }
     return narrow(s, from, top, floor, lo, bits, before, target, weight);
 }
@@ -408,49 +513,178 @@ __device__ __forceinline__ uint64_t kept_units(Shared &s, const From &from, cons
         if (k > keep.key) sum += r.units(k);
         else ++ties;
     });
-    uint64_t all, tied;
-    block_scan(s, sum, all);
-    block_scan(s, ties, tied);
+    const uint64_t all = block_sum(s, sum);
+    uint64_t tied = block_sum(s, ties);
     if (tied > keep.ties) tied = keep.ties;
     return tied ? all + tied * r.units(keep.key) : all;
 }
 
-// top-k, then top-p over what `from` holds: everything that may be kept. units:
-// the weights' sum, if known (else 0).
+// The least whole number that is at least part * all, and 1.
+__device__ __forceinline__ uint64_t share(float part, uint64_t all) {
+    const double p = static_cast<double>(part) * static_cast<double>(all);
+    const uint64_t t = p > 1.0 ? static_cast<uint64_t>(p) : 1;
+    return static_cast<double>(t) < p ? t + 1 : t;
+}
+
+// The fewest in order from `top` whose sum reaches target, of what `keep` leaves
+// and `from` holds; `before` is the sum of what lies above that.
 template <int D, class From>
-__device__ __forceinline__ void filter(Shared &s, const From &from, bool in_list, const Row<D> &r,
-                                       const Draw &d, uint32_t top, uint64_t units, Keep &keep) {
+__device__ __forceinline__ Keep reach(Shared &s, const From &from, const Row<D> &r, uint32_t top,
+                                      uint64_t before, uint64_t target, Keep keep) {
+    const bool open = keep.ties == kAllTies;
+    const Border b = seek(s, from, top, open ? keep.key - 1 : keep.key, target - before,
+                          [&](uint32_t k) { return r.units(k); });
+    if (b.found) {
+        keep = Keep{b.key, kAllTies};
+        before += b.before;
+    } else if (open) {  // all of it: the target was rounded up
+        return keep;
+    } else {  // among the first ties of the least key
+        uint64_t mine = 0;
+        from.each(keep.key + 1, [&](uint32_t k, int) { mine += r.units(k); });
+        before += block_sum(s, mine);
+    }
+    const uint64_t w = r.units(keep.key);
+    const uint64_t ties = (target - before + w - 1) / w;
+    return Keep{keep.key, ties < keep.ties ? static_cast<uint32_t>(ties) : keep.ties};
+}
+
+// top-k, then top-p over what `from` holds: everything that may be kept. units:
+// the weights' sum, where top-k keeps all of it (else it is added up).
+template <int D, class From>
+__device__ __forceinline__ Keep filter(Shared &s, const From &from, const Row<D> &r, const Draw &d,
+                                       uint32_t top, uint64_t units, Keep keep) {
     if (d.top_k > 0) {
-        uint64_t mine = 0, there;
+        uint64_t mine = 0;
         from.each(keep.key, [&](uint32_t, int) { ++mine; });
-        block_scan(s, mine, there);
         const uint64_t k = static_cast<uint64_t>(d.top_k);
-        if (there > k) {
-            const Border b = seek(s, from, in_list, top, keep.key - 1, k,
+        if (block_sum(s, mine) > k) {
+            const Border b = seek(s, from, top, keep.key - 1, k,
                                   [](uint32_t) { return uint64_t{1}; });
             keep = Keep{b.key, static_cast<uint32_t>(k - b.before)};
         }
-        units = 0;
+        if (d.top_p < 1.0f) units = kept_units(s, from, r, keep);
     }
-    if (!(d.top_p < 1.0f)) return;
-    const uint64_t all = units ? units : kept_units(s, from, r, keep);
-    const double part = static_cast<double>(d.top_p) * static_cast<double>(all);
-    uint64_t target = part > 1.0 ? static_cast<uint64_t>(part) : 1;
-    if (static_cast<double>(target) < part) ++target;
-    const auto weight = [&](uint32_t k) { return r.units(k); };
-    // the weight above the least kept key decides whether the border lies there
-    uint64_t mine = 0, above;
-    from.each(keep.key + 1, [&](uint32_t k, int) { mine += r.units(k); });
-    block_scan(s, mine, above);
-    if (target > above) {
-        const uint64_t w = r.units(keep.key);
-        const uint64_t ties = (target - above + w - 1) / w;
-        if (ties < keep.ties) keep.ties = static_cast<uint32_t>(ties);
-        return;
+    return d.top_p < 1.0f ? reach(s, from, r, top, 0, share(d.top_p, units), keep) : keep;
+}
+
+// A nucleus of more tokens than the list holds. Sums in 32 bits give a window of
+// logits that holds its border; one pass over the row then adds up, exactly, what
+// lies above the window, chunk by chunk, and lists what lies inside. False where
+// the window misses or does not fit: then nothing is decided.
+template <int D>
+__device__ __forceinline__ bool window(Shared &s, const Row<D> &r, float part, uint32_t top,
+                                       uint64_t units, Keep &keep) {
+    if (!r.finite || !(r.scale > 1e-30 && r.scale < 1e30)) return false;
+    const float cut = value_of(keep.key), scale = static_cast<float>(r.scale);
+    // the whole row comes to 2^31
+    const float unit = static_cast<float>(0x1p73 / static_cast<double>(units));
+    clear_bins(s);
+    const uint32_t size = queue_chunks(s, r.chunks, keep.key);
+    each_chunk(s, r, size, [&](const float(&x)[kPer], int) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const float z = (x[i] - r.max) * scale;
+            const uint32_t w = static_cast<uint32_t>(__builtin_amdgcn_exp2f(z) * unit + 0.5f);
+            const uint32_t bin = static_cast<uint32_t>(z * -static_cast<float>(kPerBit));
+            if (x[i] >= cut && w)
+                atomicAdd(reinterpret_cast<uint32_t *>(&s.hist[bin < kBins ? bin : kBins - 1]), w);
+        }
+    });
+    // A window of 2^-10 of the row's weight to either side: rounded weights are off by
+    // half a unit each, 2^-12 of it for the largest vocabulary.
+    const double aim = static_cast<double>(part) * 0x1p31;
+    uint32_t first, end;
+    uint64_t unused;
+    if (!find_bin(s, kBins, aim > 0x1p21 + 1.0 ? static_cast<uint64_t>(aim - 0x1p21) : 1, first,
+                  unused))
+        return false;
+    if (!find_bin(s, kBins, static_cast<uint64_t>(aim + 0x1p21), end, unused) ||
+        end >= kBins - 1)
+        return false;
+    const double max = static_cast<double>(r.max);
+    const uint32_t above = first ? key_from(max - first / (kPerBit * r.scale)) : top;
+    uint32_t least = key_from(max - (end + 1) / (kPerBit * r.scale));
+    if (least < keep.key) least = keep.key;
+    if (least > above) return false;
+    const float high = value_of(above), low = value_of(least);
+    if (threadIdx.x == 0) s.list_size = 0;
+    const uint32_t again = queue_chunks(s, r.chunks, least);
+    const int lane = threadIdx.x & 63;
+    each_chunk(s, r, again, [&](const float(&x)[kPer], int c) {
+        double sum = 0.0;  // whole numbers below 2^53: exact
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            sum = __builtin_fma(r.units_of(x[i]), x[i] > high ? 1.0 : 0.0, sum);
+            if (x[i] >= low && x[i] <= high) to_list(s, key_of(x[i]), chunk_at<D>(c, lane, i));
+        }
+        sum = wave_reduce(sum, Add{});
+        if (lane == 0) s.chunk_units[c] = static_cast<uint64_t>(sum);
+    });
+    __syncthreads();
+    const uint32_t listed = s.list_size;
+    const int tid = threadIdx.x;
+    const uint64_t before = block_sum(s, tid < r.chunks ? s.chunk_units[tid] : 0);
+    const uint64_t target = share(part, units);
+    if (listed > kList || before >= target) return false;
+    const InList list{s, listed};
+    const uint64_t in = kept_units(s, list, r, Keep{least, kAllTies});
+    if (before + in < target) return false;
+    keep = reach(s, list, r, above, before, target, Keep{least, kAllTies});
+    return true;
+}
+
+// Few candidates, and nothing outside them kept: ranked by counting, then every
+// filter is a prefix of the order and every sum a scan.
+template <int D>
+__device__ __forceinline__ void draw_small(Shared &s, const Row<D> &r, const Draw &d, int n,
+                                           uint32_t least, uint64_t units, float u, int32_t *out,
+                                           float *prob) {
+    const int tid = threadIdx.x;
+    uint64_t *order = s.hist;           // as collected, then sorted
+    uint64_t *sorted = s.hist + kSmall;
+    uint64_t *kept = s.hist + 2 * kSmall;
+    if (tid < n) order[tid] = order_of(s.list_key[tid], s.list_at[tid]);
+    rank_all(s, order, n);
+    if (tid < n) sorted[s.rank[tid]] = order[tid];
+    if (tid < kSmall) s.sums[tid] = 0;
+    __syncthreads();
+    const uint64_t mine = tid < n ? sorted[tid] : 0;
+    const uint32_t key = static_cast<uint32_t>(mine >> 32);
+    const uint64_t w = tid < n ? r.units(key) : 0;
+    bool in = tid < n && (d.top_k <= 0 || tid < d.top_k);
+    uint64_t top_units;
+    const uint64_t before = block_scan(s, in ? w : 0, top_units);
+    if (d.top_p < 1.0f) in = in && before < share(d.top_p, d.top_k > 0 ? top_units : units);
+    in = in && (key >= least || tid == 0);
+    uint64_t all;
+    block_scan(s, in ? w : 0, all);
+    if (tid < kSmall) kept[tid] = in ? w : 0;
+    __syncthreads();
+    // in index order: the kept weight before each candidate, four threads to one
+    const int e = tid & (kSmall - 1), part = tid / kSmall;
+    const uint32_t at_e = e < n ? ~static_cast<uint32_t>(sorted[e]) : 0;
+    if (e < n) {
+        const int each = (n + 3) / 4;
+        const int end = each * (part + 1) < n ? each * (part + 1) : n;
+        uint64_t sum = 0;
+#pragma unroll 4
+        for (int j = each * part; j < end; ++j)
+            sum += ~static_cast<uint32_t>(sorted[j]) < at_e ? kept[j] : 0;
+        add(s.sums[e], sum);
     }
-    const Border b = seek(s, from, in_list, top, keep.key, target, weight);
-    const uint64_t w = r.units(b.key);
-    keep = Keep{b.key, static_cast<uint32_t>((target - b.before + w - 1) / w)};
+    __syncthreads();
+    uint64_t at = u > 0.0f ? static_cast<uint64_t>(static_cast<double>(u < 1.0f ? u : 1.0f) *
+                                                   static_cast<double>(all))
+                           : 0;
+    if (at >= all) at = all - 1;
+    if (in && s.sums[tid] <= at && at < s.sums[tid] + w) {
+        *out = static_cast<int32_t>(at_e);
+        if (prob) {
+            const double sum = __builtin_ldexp(static_cast<double>(all), -kUnitBits);
+            *prob = static_cast<float>(exp2_64(log2_weight(value_of(key), r.max, r.scale)) / sum);
+        }
+    }
 }
 
 template <int D>
@@ -460,6 +694,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     const int64_t t = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Draw d = draw_of(a, t);
+    const float u = a.uniform[t];
     const ChunkStat *stats = static_cast<const ChunkStat *>(a.workspace) + t * n.chunks;
 
     Row<D> r;
@@ -489,19 +724,18 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
         return;
     }
     r.max = value_of(top);
+    r.finite = r.max < __builtin_inff();
     r.scale = d.greedy ? 0.0 : kLog2e / static_cast<double>(d.temperature);
 
-    uint64_t units = 0;  // of this thread's chunk
+    uint64_t units = 0;   // of this thread's chunk
     Keep keep{top, 1};
-    bool by_row = false;  // what is kept is not in the list
     bool plain = false;   // every weight above the cut is kept: the scan's sums serve
     if (!d.greedy) {
         const double max = static_cast<double>(r.max), tau = static_cast<double>(d.temperature);
-        const bool finite = r.max < __builtin_inff();
-        keep = Keep{finite ? key_from(max - kCut * kLn2 * tau) : top, kAllTies};
+        keep = Keep{r.finite ? key_from(max - kCut * kLn2 * tau) : top, kAllTies};
         uint32_t least = keep.key;  // of min-p
         // at an infinite temperature every weight is 1
-        if (d.min_p > 0.0f && finite && d.temperature < __builtin_inff()) {
+        if (d.min_p > 0.0f && r.finite && d.temperature < __builtin_inff()) {
             const double p = d.min_p < 1.0f ? static_cast<double>(d.min_p) : 1.0;
             const uint32_t k = key_from(p < 1.0 ? max + log(p) * tau : max);
             least = k > least ? k : least;
@@ -512,68 +746,75 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
                                 kUnitBits)));
             units = units > 0 ? units : 1;
         }
-        const bool filtered = d.top_k > 0 || d.top_p < 1.0f;
-        plain = !filtered && !(d.min_p > 0.0f);
-        if (filtered) {
-            uint64_t all;
-            block_scan(s, units, all);  // top-p's sum; 0 where top-k comes first
-            // Candidates above the rank-th largest chunk maximum: at least `rank` of them, so
-            // enough for top-k, and likely for a nucleus.
-            const int rank = d.top_k > 0 ? d.top_k : kNucleus;
-            uint32_t from = keep.key;
-            if (rank < n.chunks) {
-                int larger = 0;
-                for (int c = 0; c < n.chunks; ++c)
-                    larger += s.chunk_key[c] > my_key || (s.chunk_key[c] == my_key && c < tid);
-                if (tid < n.chunks && larger == rank - 1) s.bound = my_key;
+        const bool by_k = d.top_k > 0, by_p = d.top_p < 1.0f;
+        plain = !by_k && !by_p && !(d.min_p > 0.0f);
+        if (!plain) {
+            const uint64_t row_units = by_p && !by_k ? block_sum(s, units) : 0;
+            // First the candidates above a bound that is known: min-p's, or the rank-th
+            // largest of the chunks' maxima, above which there are at least `rank`. That is
+            // enough for top-k, and likely for a nucleus, unless its weight says that it
+            // holds more tokens.
+            uint32_t from = by_p ? keep.key : least;
+            const int rank = by_k ? d.top_k : kNucleus;
+            const bool wide =
+                by_p && !by_k &&
+                static_cast<double>(d.top_p) * static_cast<double>(row_units) >
+                    static_cast<double>(kNucleusMass) * __builtin_ldexp(1.0, kUnitBits);
+            if ((by_k || (by_p && !wide)) && rank < n.chunks) {
+                if (tid < n.chunks) s.hist[tid] = order_of(my_key, tid);
+                rank_all(s, s.hist, n.chunks);
+                if (tid < n.chunks && s.rank[tid] == static_cast<uint32_t>(rank - 1))
+                    s.bound = my_key;
                 __syncthreads();
                 from = s.bound > from ? s.bound : from;
             }
-            bool listed = collect(s, InRow<D>{s, r}, from, top);
-            if (listed && d.top_k <= 0 && from > keep.key)
-                listed = static_cast<double>(kept_units(s, InList{s, s.list_size}, r,
-                                                        Keep{from, kAllTies})) >=
-                         static_cast<double>(d.top_p) * static_cast<double>(all) + 1.0;
-            if (listed) {
-                keep.key = from;
-                filter(s, InList{s, s.list_size}, true, r, d, top, d.top_k > 0 ? 0 : all, keep);
-            } else {
-                filter(s, InRow<D>{s, r}, false, r, d, top, d.top_k > 0 ? 0 : all, keep);
+            bool listed = !wide && collect(s, InRow<D>{s, r}, from, top);
+            const InList list{s, s.list_size};
+            if (listed && by_p && !by_k && from > keep.key)
+                listed = kept_units(s, list, r, Keep{from, kAllTies}) >=
+                         share(d.top_p, row_units);
+            if (listed && list.size <= kSmall) {
+                draw_small(s, r, d, static_cast<int>(list.size), least, row_units, u, a.out + t,
+                           a.probs ? a.probs + t : nullptr);
+                return;
             }
-            if (least > keep.key) keep = Keep{least, kAllTies};
+            if (listed) {
+                keep = filter(s, list, r, d, top, row_units, Keep{from, kAllTies});
+                if (least > keep.key) keep = Keep{least, kAllTies};
+            } else if (by_p && !by_k && window(s, r, d.top_p, top, row_units, keep)) {
+                listed = least <= keep.key;  // else what is above the window counts too much
+                if (!listed) keep = Keep{least, kAllTies};
+            } else {
+                if (by_k || by_p)
+                    keep = filter(s, InRow<D>{s, r}, r, d, top, row_units, keep);
+                if (least > keep.key) keep = Keep{least, kAllTies};
+            }
             if (listed) {
                 InList{s, s.list_size}.each(keep.key, [&](uint32_t k, int at) {
                     if (k > keep.key) add(s.chunk_units[at / kChunkElems], r.units(k));
                     else atomicAdd(&s.chunk_ties[at / kChunkElems], 1u);
                 });
-            }
-            by_row = !listed;
-        } else if (!plain) {
-            keep = Keep{least, kAllTies};
-            by_row = true;
-        }
-        if (by_row) {
-            for (int c = wave; c < n.chunks; c += kPickWaves) {
-                if (s.chunk_key[c] < keep.key) continue;
-                float x[kPer];
-                load_chunk<D>(r.logits, r.vocab, c, lane, x);
-                uint64_t sum = 0;
-                uint32_t ties = 0;
+            } else {
+                __syncthreads();
+                if (tid < n.chunks) s.chunk_units[tid] = 0;
+                const uint32_t size = queue_chunks(s, n.chunks, keep.key);
+                each_chunk(s, r, size, [&](const float(&x)[kPer], int c) {
+                    uint64_t sum = 0;
+                    uint32_t ties = 0;
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const uint32_t k = key_of(x[i]);
-                    if (k > keep.key) sum += r.units(k);
-                    ties += k == keep.key;
-                }
-                sum = wave_reduce(sum, Add{});
-                ties = wave_reduce(ties, Add{});
-                if (lane == 0) {
-                    s.chunk_units[c] = sum;
-                    s.chunk_ties[c] = ties;
-                }
+                    for (int i = 0; i < kPer; ++i) {
+                        const uint32_t k = key_of(x[i]);
+                        if (k > keep.key) sum += r.units(k);
+                        ties += k == keep.key;
+                    }
+                    sum = wave_reduce(sum, Add{});
+                    ties = wave_reduce(ties, Add{});
+                    if (lane == 0) {
+                        s.chunk_units[c] = sum;
+                        s.chunk_ties[c] = ties;
+                    }
+                });
             }
-        }
-        if (!plain) {
             __syncthreads();
             units = tid < n.chunks ? s.chunk_units[tid] : 0;
         }
@@ -592,9 +833,8 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     }
     uint64_t all;
     const uint64_t before = block_scan(s, units, all);
-    const float u = a.uniform[t];
-    uint64_t at = u > 0.0f ? static_cast<uint64_t>(
-                                 static_cast<double>(u < 1.0f ? u : 1.0f) * static_cast<double>(all))
+    uint64_t at = u > 0.0f ? static_cast<uint64_t>(static_cast<double>(u < 1.0f ? u : 1.0f) *
+                                                   static_cast<double>(all))
                            : 0;
     if (at >= all) at = all - 1;
     if (units && before <= at && at < before + units) {
@@ -605,10 +845,11 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     __syncthreads();
     if (wave != 0) return;
 
-    // The token inside the chunk.
-    const int c = s.chosen;
-    const uint64_t want = s.chosen_at;
-    uint64_t ties_run = s.chosen_ties, run = 0;
+    // The token inside the chunk: which vector of the lanes, then which lane, then which
+    // element.
+    const int c = __builtin_amdgcn_readfirstlane(s.chosen);
+    uint64_t want = s.chosen_at;
+    uint64_t ties_run = s.chosen_ties;
     float x[kPer];
     load_chunk<D>(r.logits, r.vocab, c, lane, x);
     constexpr int VE = kVecElems<D>;
@@ -619,8 +860,12 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
         uint32_t ties = 0;
 #pragma unroll
         for (int i = 0; i < VE; ++i) ties += key_of(x[v * VE + i]) == keep.key;
-        const uint64_t tie_scan = wave_scan(ties, lane);
-        uint64_t rank = ties_run + tie_scan - ties;
+        uint64_t rank = ties_run;
+        if (keep.ties != kAllTies) {
+            const uint64_t tie_scan = wave_scan(ties);
+            rank += tie_scan - ties;
+            ties_run += lane_value(tie_scan, 63);
+        }
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
             const uint32_t k = key_of(x[v * VE + i]);
@@ -630,8 +875,8 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
             w[i] = !in ? 0 : d.greedy ? 1 : r.units(k);
             sum += w[i];
         }
-        const uint64_t scan = wave_scan(sum, lane);
-        uint64_t low = run + scan - sum;
+        const uint64_t scan = wave_scan(sum);
+        uint64_t low = scan - sum;
         int here = -1, kept = -1;
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
@@ -639,14 +884,15 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
             if (w[i]) kept = chunk_at<D>(c, lane, v * VE + i);
             low += w[i];
         }
-        const int found = static_cast<int>(wave_reduce(static_cast<uint32_t>(here + 1), Max{})) - 1;
-        const int tail = static_cast<int>(wave_reduce(static_cast<uint32_t>(kept + 1), Max{})) - 1;
-        if (token < 0) token = found;
-        if (tail >= 0) last = tail;
-        run += lane_value(scan, 63);
-        ties_run += lane_value(tie_scan, 63);
+        const uint64_t hit = __ballot(here >= 0), any = __ballot(kept >= 0);
+        if (any) last = lane_value(kept, 63 - __builtin_clzll(any));
+        if (hit) {
+            token = lane_value(here, __builtin_ctzll(hit));
+            break;
+        }
+        want -= lane_value(scan, 63);
     }
-    if (token < 0) token = last;  // the chunk's own sum was rounded up
+    if (token < 0) token = last < 0 ? 0 : last;  // the chunk's own sum was rounded up
     if (lane == 0) {
         a.out[t] = token;
         if (a.probs) {

@@ -9,11 +9,14 @@
 int main() {
     std::mt19937_64 rng(260708973);
     std::uniform_real_distribution<double> frac(-0.5, 0.5), wide(-1020.0, 1020.0);
-    long double worst = 0;
+    long double worst = 0, worst9 = 0;
     const auto see = [&](double t) {
         const long double want = exp2l(static_cast<long double>(t));
         const long double e = fabsl(static_cast<long double>(sifar::exp2_64(t)) / want - 1);
         if (e > worst) worst = e;
+        const double i = std::rint(t);
+        const long double s = ldexpl(sifar::exp2_fraction9(t - i), static_cast<int>(i));
+        if (fabsl(s / want - 1) > worst9) worst9 = fabsl(s / want - 1);
     };
     for (int i = 0; i < 2000000; ++i) {
         see(frac(rng));
@@ -24,6 +27,6 @@ int main() {
         see(i + 0.5);
         see(std::nextafter(i + 0.5, 0.0));
     }
-    std::printf("%.3Le\n", worst);
-    return worst < 3e-16L ? 0 : 1;
+    std::printf("%.3Le %.3Le\n", worst, worst9);
+    return worst < 3e-16L && worst9 < 4e-14L ? 0 : 1;
 }
