@@ -8,6 +8,8 @@
 // unpacked 32-bit one, so 64 bits cost the longer polynomial and nothing else.
 #pragma once
 
+#include <stdint.h>
+
 #if defined(__HIPCC__)
 #define SIFAR_HD __host__ __device__ __forceinline__
 #else
@@ -32,18 +34,31 @@ SIFAR_HD double exp2_fraction(double f) {
     return __builtin_fma(q, f, 1.0);
 }
 
-// The same with a relative error below 4e-14: for sums in units of 2^-42.
-SIFAR_HD double exp2_fraction9(double f) {
-    double q = 0x1.b638808675ca6p-24;
-    q = __builtin_fma(q, f, 0x1.63d136355f669p-20);
-    q = __builtin_fma(q, f, 0x1.ffcb9515c8f1ap-17);
-    q = __builtin_fma(q, f, 0x1.4308ac85abb17p-13);
-    q = __builtin_fma(q, f, 0x1.5d87fe86fe7ccp-10);
-    q = __builtin_fma(q, f, 0x1.3b2ab7181b74ap-7);
-    q = __builtin_fma(q, f, 0x1.c6b08d7047e52p-5);
-    q = __builtin_fma(q, f, 0x1.ebfbdff823cedp-3);
-    q = __builtin_fma(q, f, 0x1.62e42fefa39efp-1);
-    return __builtin_fma(q, f, 1.0);
+// 2^(t + BITS) for t in [-1000, 0], relative error below 4e-14: for sums in units of
+// 2^-42. Rounding to i and scaling by 2^i are additions to the bits: the
+// conversions and ldexp that they replace issue at a quarter of an fma's rate.
+// Elsewhere the result is garbage, but nothing traps.
+template <int BITS>
+SIFAR_HD double exp2_quick(double t) {
+    constexpr double s = static_cast<double>(1ull << BITS);
+    const double m = t + 0x1.8p52;  // i in the low bits
+    const double f = t - (m - 0x1.8p52);
+    double q = 0x1.b638808675ca6p-24 * s;
+    q = __builtin_fma(q, f, 0x1.63d136355f669p-20 * s);
+    q = __builtin_fma(q, f, 0x1.ffcb9515c8f1ap-17 * s);
+    q = __builtin_fma(q, f, 0x1.4308ac85abb17p-13 * s);
+    q = __builtin_fma(q, f, 0x1.5d87fe86fe7ccp-10 * s);
+    q = __builtin_fma(q, f, 0x1.3b2ab7181b74ap-7 * s);
+    q = __builtin_fma(q, f, 0x1.c6b08d7047e52p-5 * s);
+    q = __builtin_fma(q, f, 0x1.ebfbdff823cedp-3 * s);
+    q = __builtin_fma(q, f, 0x1.62e42fefa39efp-1 * s);
+    q = __builtin_fma(q, f, s);
+    uint64_t bits, shift;
+    __builtin_memcpy(&bits, &q, 8);
+    __builtin_memcpy(&shift, &m, 8);
+    bits += static_cast<uint64_t>(static_cast<uint32_t>(shift) << 20) << 32;
+    __builtin_memcpy(&q, &bits, 8);
+    return q;
 }
 
 // 2^t for |t| <= 1020.

@@ -1,11 +1,11 @@
 // A token from its logits and one given random number: sifar_sample. gfx950
 // (MI355X) only.
 //
-// Two launches. scan_kernel reads every logit once: a wave takes a chunk of 1024
-// and leaves its maximum and, where the row needs it, its weights' sum.
-// pick_kernel, a workgroup a row, finds the threshold of top-k, top-p and min-p
-// and walks to the token in index order, reading again only chunks whose maximum
-// says that they hold something to keep.
+// Two launches. scan_kernel reads every logit once and leaves, for each chunk (the
+// 16 bytes of each of a wave's lanes), the maximum and, where the row needs it,
+// the weights' sum. pick_kernel, a workgroup a row, finds the threshold of top-k,
+// top-p and min-p and walks to the token in index order, reading again only
+// chunks whose maximum says that they hold something to keep.
 //
 // Weights w = 2^((x - max) log2(e) / temperature) are 64-bit values rounded to
 // units of 2^-42 and added as integers: sums do not depend on the order of
@@ -13,8 +13,8 @@
 // tokens is off by 2^-43 a token at most. In 32 bits a draw from a flat row of
 // 100000 tokens would land on the neighbour once in a thousand times.
 //
-// Bound: HBM bytes of the logits for many rows, latency of the two launches and
-// of pick_kernel's barriers for a few.
+// Bound: the 64-bit exponentials for many rows, latency of the two launches and
+// of pick_kernel's barriers and loads for a few.
 #include <hip/hip_runtime.h>
 
 #include "exp2.h"
@@ -23,36 +23,32 @@
 namespace sifar {
 namespace {
 
-constexpr int kChunkElems = 1024;              // logits of a wave's chunk
-constexpr int kPer = kChunkElems / kRowWave;   // of a lane
-constexpr int kScanWaves = 4;                  // chunks of a scan workgroup
+constexpr int kBatch = 4;                      // chunks a wave loads at a time
+constexpr int kScanWaves = 4;                  // waves of a scan workgroup
 constexpr int kThreads = 1024;                 // of a pick workgroup
 constexpr int kPickWaves = kThreads / kRowWave;
-constexpr int kMaxChunks = SIFAR_SAMPLE_MAX_VOCAB / kChunkElems;
+constexpr int kLeastChunk = kRowWave * 4;      // logits of a chunk: 256 of 32 bits, 512 of 16
+constexpr int kMaxChunks = SIFAR_SAMPLE_MAX_VOCAB / kLeastChunk;
 constexpr int kBins = 64 + 26 * 64;            // log-linear bins of a 32-bit distance
-constexpr int kList = 8192;                    // candidates kept in LDS
+constexpr int kList = 4096;                    // candidates kept in LDS
 constexpr int kSmall = 256;                    // most candidates that are ranked by counting
-constexpr int kNucleus = 64;                   // chunk maxima a nucleus is first sought above
-constexpr int kNucleusMass = 128;              // most p * sum / largest weight of such a row
+constexpr int kNucleus = 64;                   // maxima a nucleus is first sought above
+constexpr int kNucleusMass = 24;               // most p * sum / largest weight of such a row
 constexpr int kPerBit = 64;                    // bins of a halving of the weight
 constexpr int kUnitBits = 42;                  // a weight of 1 in units
 constexpr double kLog2e = 1.4426950408889634;
 constexpr double kLn2 = 0.6931471805599453;
 constexpr double kCut = 60.0;                  // weights below 2^-60 are 0
-static_assert(kMaxChunks <= kThreads, "a thread per chunk");
-
-struct ChunkStat {
-    double mass;  // sum of weights relative to the chunk's maximum
-    float max;
-    uint32_t unused;
-};
+constexpr float kLowest = -3.402823466e38f;
 
 struct SampleArgs {
     sifar_sample_args a;
     int32_t chunks;  // of a row
+    double *mass;    // [tokens][chunks] sums of weights relative to the chunk's maximum
+    float *max;      // [tokens][chunks]
 };
 
-// Order-preserving 32 bits of a logit; 0 for one that is not there. -0 counts as 0.
+// Order-preserving 32 bits of a number. -0 counts as 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);
     return u >> 31 ? ~u : u | 0x80000000u;
@@ -66,10 +62,17 @@ constexpr uint32_t kLowestKey = 0x00800000u;  // of the lowest finite fp32
 
 // The least key whose logit is at least `limit`, and of a finite logit.
 __device__ __forceinline__ uint32_t key_from(double limit) {
-    float f = static_cast<float>(limit);
+    const float f = static_cast<float>(limit);
     uint32_t k = key_of(f);
     if (static_cast<double>(f) < limit) ++k;
     return k < kLowestKey ? kLowestKey : k;
+}
+
+// The larger of two numbers; of a number and a NaN, the number.
+__device__ __forceinline__ float max32(float a, float b) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
 }
 
 // How a row is drawn.
@@ -95,39 +98,104 @@ struct __attribute__((packed, aligned(sizeof(Stored<D>)))) Loose {
     U4 v;
 };
 
-// A wave's chunk: vectors of 16 bytes a lane, lanes adjacent. Element i of lane l
-// is logit chunk_at<D>(c, l, i); one past the row, a NaN or -inf is -inf.
 template <int D>
-constexpr int kVecElems = 16 / sizeof(Stored<D>);
+constexpr int kVec = 16 / sizeof(Stored<D>);  // logits of a lane in a chunk
+template <int D>
+constexpr int kChunkOf = kRowWave * kVec<D>;
+
+// The lane's logits of a chunk, as they are stored.
+struct Raw {
+    U4 v;
+};
 
 template <int D>
-__device__ __forceinline__ int chunk_at(int c, int lane, int i) {
-    constexpr int VE = kVecElems<D>;
-    return c * kChunkElems + (i / VE) * (kRowWave * VE) + lane * VE + i % VE;
+__device__ __forceinline__ float logit(const Raw &e, int i) {
+    if constexpr (D == SIFAR_FP32) return __uint_as_float(e.v[i]);
+    else if constexpr (D == SIFAR_BF16)
+        return __uint_as_float(i & 1 ? e.v[i >> 1] & 0xFFFF0000u : e.v[i >> 1] << 16);
+    else
+        return widen<D>(i & 1 ? e.v[i >> 1] >> 16 : e.v[i >> 1] & 0xFFFFu);
 }
 
 template <int D>
-__device__ __forceinline__ void load_chunk(const Stored<D> *row, int vocab, int c, int lane,
-                                           float (&x)[kPer]) {
-    constexpr int VE = kVecElems<D>;
-    const float none = -__builtin_inff();
-#pragma unroll
-    for (int v = 0; v < kPer / VE; ++v) {
-        const int at = chunk_at<D>(c, lane, v * VE);
-        if (at + VE <= vocab) {
-            Eight<D> e;
-            e.v[0] = reinterpret_cast<const Loose<D> *>(row + at)->v;
-#pragma unroll
-            for (int i = 0; i < VE; ++i) x[v * VE + i] = element<D>(e, i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < VE; ++i)
-                x[v * VE + i] = at + i < vocab ? widen<D>(row[at + i]) : none;
-        }
+__device__ __forceinline__ Raw nothing() {  // -inf
+    constexpr uint32_t w = D == SIFAR_FP32 ? 0xFF800000u : D == SIFAR_BF16 ? 0xFF80FF80u : 0xFC00FC00u;
+    return Raw{U4{w, w, w, w}};
+}
+
+// -inf past the row. (A NaN stays: comparisons with it are false, and nothing below
+// asks for less.) The lane that the row ends in loads the row's last 16 bytes and
+// shifts them down; only rows shorter than that are read by element.
+template <int D>
+__device__ __forceinline__ Raw load_chunk(const Stored<D> *row, int vocab, int c, int lane) {
+    const int at = c * kChunkOf<D> + lane * kVec<D>;
+    if (at + kVec<D> <= vocab) return Raw{reinterpret_cast<const Loose<D> *>(row + at)->v};
+    Raw e = nothing<D>();
+    if (at >= vocab) return e;
+    constexpr int bits = 8 * sizeof(Stored<D>);
+    if (vocab >= kVec<D>) {
+        const U4 v = reinterpret_cast<const Loose<D> *>(row + vocab - kVec<D>)->v;
+        const int shift = (at + kVec<D> - vocab) * bits;  // 16 .. 112
+        const unsigned __int128 got = __builtin_bit_cast(unsigned __int128, v) >> shift;
+        const unsigned __int128 fill = __builtin_bit_cast(unsigned __int128, e.v) << (128 - shift);
+        e.v = __builtin_bit_cast(U4, got | fill);
+        return e;
     }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) x[i] = x[i] > none ? x[i] : none;
+    unsigned __int128 all = __builtin_bit_cast(unsigned __int128, e.v);
+#pragma unroll 1
+    for (int i = vocab - at - 1; i >= 0; --i)
+        all = (all << bits) | static_cast<uint32_t>(row[at + i]);
+    e.v = __builtin_bit_cast(U4, all);
+    return e;
 }
+
+// Four values reduced over the wave at once: lanes 16 i .. 16 i + 15 get the i-th
+// one's. The lane swaps of the first two steps put two values' halves into one
+// register.
+template <class T, class Op>
+__device__ __forceinline__ T wave_reduce4(const T (&v)[4], Op op) {
+    const auto join32 = [&](T a, T b) {  // lower half of the lanes: a's, upper: b's
+        if constexpr (sizeof(T) == 4) {
+            const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, a),
+                                                            __builtin_bit_cast(uint32_t, b),
+                                                            false, false);
+            const uint32_t x = r[0], y = r[1];  // (a vector's element has no address)
+            return op(__builtin_bit_cast(T, x), __builtin_bit_cast(T, y));
+        } else {
+            const uint64_t x = __builtin_bit_cast(uint64_t, a), y = __builtin_bit_cast(uint64_t, b);
+            const auto lo = __builtin_amdgcn_permlane32_swap(static_cast<uint32_t>(x),
+                                                             static_cast<uint32_t>(y), false, false);
+            const auto hi =
+                __builtin_amdgcn_permlane32_swap(static_cast<uint32_t>(x >> 32),
+                                                 static_cast<uint32_t>(y >> 32), false, false);
+            return op(__builtin_bit_cast(T, (static_cast<uint64_t>(hi[0]) << 32) | lo[0]),
+                      __builtin_bit_cast(T, (static_cast<uint64_t>(hi[1]) << 32) | lo[1]));
+        }
+    };
+    const auto join16 = [&](T a, T b) {  // even rows of 16: a's, odd rows: b's
+        if constexpr (sizeof(T) == 4) {
+            const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, a),
+                                                            __builtin_bit_cast(uint32_t, b),
+                                                            false, false);
+            const uint32_t x = r[0], y = r[1];  // (a vector's element has no address)
+            return op(__builtin_bit_cast(T, x), __builtin_bit_cast(T, y));
+        } else {
+            const uint64_t x = __builtin_bit_cast(uint64_t, a), y = __builtin_bit_cast(uint64_t, b);
+            const auto lo = __builtin_amdgcn_permlane16_swap(static_cast<uint32_t>(x),
+                                                             static_cast<uint32_t>(y), false, false);
+            const auto hi =
+                __builtin_amdgcn_permlane16_swap(static_cast<uint32_t>(x >> 32),
+                                                 static_cast<uint32_t>(y >> 32), false, false);
+            return op(__builtin_bit_cast(T, (static_cast<uint64_t>(hi[0]) << 32) | lo[0]),
+                      __builtin_bit_cast(T, (static_cast<uint64_t>(hi[1]) << 32) | lo[1]));
+        }
+    };
+    return wave_reduce<16>(join16(join32(v[0], v[2]), join32(v[1], v[3])), op);
+}
+
+struct Max32 {
+    __device__ __forceinline__ float operator()(float a, float b) const { return max32(a, b); }
+};
 
 // log2 of a weight. 0 at the maximum, which may be infinite; finite elsewhere.
 __device__ __forceinline__ double log2_weight(float x, float max, double c) {
@@ -135,77 +203,74 @@ __device__ __forceinline__ double log2_weight(float x, float max, double c) {
     return x == max ? 0.0 : z > -1100.0 ? z : -1100.0;
 }
 
-// The weight of a finite logit under a finite maximum, times 2^bits. Garbage, but
-// finite, for logits far below the cut; -inf and NaN come out as the lowest
-// finite logit.
-__device__ __forceinline__ double weight(float x, double max, double scale, int bits) {
-    const float y = fmaxf(x, -3.402823466e38f);
-    const double z = (static_cast<double>(y) - max) * scale;
-    const double i = __builtin_rint(z);
-    return __builtin_ldexp(exp2_fraction9(z - i), static_cast<int>(i) + bits);
-}
-
-__device__ __forceinline__ double max64(double a, double b) {
-    double r;
-    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-    return r;
-}
-
-// A chunk's maximum and, where the row needs it, the sum of its weights. What
+// Every chunk's maximum and, where the row needs it, the sum of its weights. What
 // top-k keeps is summed when it is known, and so is what min-p alone keeps.
 template <int D>
 __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const SampleArgs n) {
     const sifar_sample_args &a = n.a;
     const int64_t t = blockIdx.x;
     const int lane = threadIdx.x;
-    const int c = blockIdx.y * kScanWaves + threadIdx.y;
-    if (c >= n.chunks) return;
+    const int first = (blockIdx.y * kScanWaves + threadIdx.y) * kBatch;
+    if (first >= n.chunks) return;
     const Draw d = draw_of(a, t);
-    float x[kPer];
-    load_chunk<D>(static_cast<const Stored<D> *>(a.logits) + t * a.logits_stride, a.vocab, c, lane,
-                  x);
-    const float none = -__builtin_inff();
-    float m = none;
+    const Stored<D> *row = static_cast<const Stored<D> *>(a.logits) + t * a.logits_stride;
+    Raw x[kBatch];
+    float top[kBatch];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) m = fmaxf(m, x[i]);
-    m = wave_reduce(m, Max{});
-    double mass = 0.0;
-    if (!d.greedy && d.top_k <= 0 && (d.top_p < 1.0f || !(d.min_p > 0.0f)) && m > none) {
-        const double scale = kLog2e / static_cast<double>(d.temperature);
-        if (m < __builtin_inff()) {
+    for (int b = 0; b < kBatch; ++b) x[b] = load_chunk<D>(row, a.vocab, first + b, lane);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const double w = weight(x[i], m, scale, 0);
-                mass += x[i] > none ? w : 0.0;
-            }
-        } else {
+    for (int b = 0; b < kBatch; ++b) {
+        top[b] = -__builtin_inff();
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) mass += x[i] == m ? 1.0 : 0.0;
-        }
-        mass = wave_reduce(mass, Add{});
+        for (int i = 0; i < kVec<D>; ++i) top[b] = max32(top[b], logit<D>(x[b], i));
     }
-    if (lane == 0)
-        static_cast<ChunkStat *>(a.workspace)[t * n.chunks + c] = ChunkStat{mass, m, 0};
+    const float mine = wave_reduce4(top, Max32{});
+    const int c = first + (lane >> 4);
+    const bool writes = (lane & 15) == 0 && c < n.chunks;
+    if (writes) n.max[t * n.chunks + c] = mine;
+    if (d.greedy || d.top_k > 0 || (d.min_p > 0.0f && !(d.top_p < 1.0f))) return;
+    const double tau = static_cast<double>(d.temperature), scale = kLog2e / tau;
+    double sum[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+        const float m = lane_value(mine, 16 * b);
+        sum[b] = 0.0;
+        if (m < __builtin_inff()) {
+            const double max = static_cast<double>(m);
+            const float least = max32(static_cast<float>(max - kCut * kLn2 * tau), kLowest);
+#pragma unroll
+            for (int i = 0; i < kVec<D>; ++i) {
+                const float l = logit<D>(x[b], i);
+                const double w = exp2_quick<0>((static_cast<double>(l) - max) * scale);
+                sum[b] += l >= least ? w : 0.0;
+            }
+        } else {  // they share the weight
+#pragma unroll
+            for (int i = 0; i < kVec<D>; ++i) sum[b] += logit<D>(x[b], i) == m ? 1.0 : 0.0;
+        }
+    }
+    const double all = wave_reduce4(sum, Add{});
+    if (writes) n.mass[t * n.chunks + c] = all;
 }
 
 // ---- pick_kernel -----------------------------------------------------------------
 
 struct Shared {
-    uint64_t hist[kBins];                // also the candidates in order, or the chunks' ranks
+    uint64_t hist[kBins];                // also the candidates in order
     uint64_t chunk_units[kMaxChunks];
     uint32_t chunk_ties[kMaxChunks];
-    uint32_t chunk_key[kMaxChunks];      // of the chunk's maximum
+    uint32_t chunk_key[kMaxChunks];      // of the chunk's maximum; 0: nothing is there
     uint32_t queue[kMaxChunks];          // chunks to be read
     uint32_t list_key[kList];            // candidates
     uint32_t list_at[kList];
-    uint32_t rank[kThreads];
+    uint32_t rank[kSmall];
     uint64_t sums[kSmall];
     uint64_t wave_sum[kPickWaves];
     uint32_t wave_max[kPickWaves];
     uint64_t found_before;
     uint32_t found_bin;
     uint32_t list_size, queue_size;
-    uint32_t bound;        // of the candidates
+    uint32_t first_top;    // the first chunk that holds the maximum
     uint32_t chosen;       // the token's chunk,
     uint64_t chosen_at;    // the units before the token in it
     uint64_t chosen_ties;  // and the ties before the chunk
@@ -273,46 +338,26 @@ __device__ __forceinline__ uint32_t block_max(Shared &s, uint32_t x) {
     return m;
 }
 
-// Key, then lower index: sorts as the order of the draw.
-__device__ __forceinline__ uint64_t order_of(uint32_t key, uint32_t at) {
-    return (static_cast<uint64_t>(key) << 32) | static_cast<uint32_t>(~at);
-}
-
-// Into s.rank[e]: how many of the first n values of `order` are above the e-th. Up
-// to 256 values the workgroup splits each one's comparisons four ways.
-__device__ __forceinline__ void rank_all(Shared &s, const uint64_t *order, int n) {
-    const int span = n <= kThreads / 4 ? kThreads / 4 : n <= kThreads / 2 ? kThreads / 2 : kThreads;
-    const int parts = kThreads / span;
-    const int e = threadIdx.x & (span - 1), part = threadIdx.x / span;
-    s.rank[threadIdx.x] = 0;
-    __syncthreads();
-    if (e < n) {
-        const int each = (n + parts - 1) / parts;
-        const int end = each * (part + 1) < n ? each * (part + 1) : n;
-        const uint64_t mine = order[e];
-        uint32_t above = 0;
-#pragma unroll 4
-        for (int j = each * part; j < end; ++j) above += order[j] > mine;
-        atomicAdd(&s.rank[e], above);
-    }
-    __syncthreads();
-}
-
 // A row in pick_kernel.
 template <int D>
 struct Row {
     const Stored<D> *logits;
     int vocab, chunks;
     float max;
-    double scale;  // log2(e) / temperature
-    bool finite;   // the maximum is; otherwise the infinite logits share the weight
+    double max64, scale;  // log2(e) / temperature
+    float one;            // logits below it weigh one unit
+    bool finite;          // the maximum is; otherwise the infinite logits share the weight
 
-    // a weight in units; at least one, so that what may be drawn can be
-    __device__ __forceinline__ double units_of(float x) const {
-        return __builtin_rint(max64(weight(x, max, scale, kUnitBits), 1.0));
+    // A weight in units. (Garbage for logits below the cut.)
+    __device__ __forceinline__ uint64_t units_near(float x) const {
+        const double w = exp2_quick<kUnitBits>((static_cast<double>(x) - max64) * scale);
+        return __builtin_bit_cast(uint64_t, w + 0x1p52) & ((uint64_t{1} << 52) - 1);
     }
+    // Of a kept weight at least one, so that what may be drawn can be.
     __device__ __forceinline__ uint64_t units(uint32_t key) const {
-        return finite ? static_cast<uint64_t>(units_of(value_of(key))) : uint64_t{1} << kUnitBits;
+        const float x = value_of(key);
+        const uint64_t u = x >= one ? units_near(x) : 1;
+        return finite ? u : uint64_t{1} << kUnitBits;
     }
 };
 
@@ -321,38 +366,72 @@ __device__ __forceinline__ uint32_t queue_chunks(Shared &s, int chunks, uint32_t
     __syncthreads();
     if (threadIdx.x == 0) s.queue_size = 0;
     __syncthreads();
-    if (static_cast<int>(threadIdx.x) < chunks && s.chunk_key[threadIdx.x] >= least)
-        s.queue[atomicAdd(&s.queue_size, 1u)] = threadIdx.x;
+    for (int c = threadIdx.x; c < chunks; c += kThreads)
+        if (s.chunk_key[c] >= least) s.queue[atomicAdd(&s.queue_size, 1u)] = c;
     __syncthreads();
     return s.queue_size;
 }
 
-// f(logits of a lane, chunk) over the queued chunks, a wave a chunk, the next one
-// loaded while one is worked on.
-template <int D, class F>
-__device__ __forceinline__ void each_chunk(const Shared &s, const Row<D> &r, uint32_t size, F f) {
+// Over the queued chunks: a wave loads four at a time, the next four while it works
+// on these. f(logits of a lane, chunk) is called for each, and its sums, over the
+// wave, go to done(sum, chunk) in one lane. The four take turns in one set of
+// registers: the loop's body is what its instructions cost to fetch.
+template <int D, class F, class Done>
+__device__ __forceinline__ void each_batch(const Shared &s, const Row<D> &r, uint32_t size, F f,
+                                           Done done) {
     const int lane = threadIdx.x & 63;
-    uint32_t q = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // spread over the waves where there are few chunks
+    const uint32_t each = size >= kBatch * kPickWaves ? kBatch : (size + kPickWaves - 1) / kPickWaves;
+    uint32_t q = wave * each;
     if (q >= size) return;
-    float x[kPer], next[kPer];
-    int c = __builtin_amdgcn_readfirstlane(s.queue[q]);
-    load_chunk<D>(r.logits, r.vocab, c, lane, next);
-    while (true) {
+    Raw next[kBatch];
+    int c_next[kBatch];
+    int n_next;
+    const auto load = [&] {
+        n_next = static_cast<int>(size - q < each ? size - q : each);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) x[i] = next[i];
-        const int at = c;
-        q += kPickWaves;
-        const bool more = q < size;
-        if (more) {
-            c = __builtin_amdgcn_readfirstlane(s.queue[q]);
-            load_chunk<D>(r.logits, r.vocab, c, lane, next);
+        for (int b = 0; b < kBatch; ++b) {
+            c_next[b] = b < n_next ? __builtin_amdgcn_readfirstlane(s.queue[q + b]) : 0;
+            next[b] = b < n_next ? load_chunk<D>(r.logits, r.vocab, c_next[b], lane) : nothing<D>();
         }
-        f(x, at);
+    };
+    load();
+    while (true) {
+        Raw x[kBatch];
+        uint64_t sum[kBatch];
+        const int c_mine = lane < 16 ? c_next[0] : lane < 32 ? c_next[1] : lane < 48 ? c_next[2]
+                                                                                     : c_next[3];
+        int c[kBatch];
+        const int n = n_next;
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            x[b] = next[b];
+            c[b] = c_next[b];
+        }
+        q += each * kPickWaves;
+        const bool more = q < size;
+        if (more) load();
+#pragma unroll 1
+        for (int b = 0; b < kBatch; ++b) {
+            const uint64_t mine = f(x[0], c[0]);
+#pragma unroll
+            for (int i = 0; i + 1 < kBatch; ++i) {
+                x[i] = x[i + 1];
+                c[i] = c[i + 1];
+                sum[i] = sum[i + 1];
+            }
+            sum[kBatch - 1] = mine;
+        }
+        const uint64_t all = wave_reduce4(sum, Add{});
+        if ((lane & 15) == 0 && (lane >> 4) < n) done(all, c_mine);
         if (!more) return;
     }
 }
 
-// Where weights are sought: the row's chunks whose maximum reaches `least`...
+// Where weights are sought: the row's chunks whose maximum reaches `least`, a chunk
+// at a time (what goes through here often goes through each_batch instead: its
+// body is four times as long)...
 template <int D>
 struct InRow {
     Shared &s;
@@ -360,14 +439,17 @@ struct InRow {
     template <class F>
     __device__ __forceinline__ void each(uint32_t least, F f) const {
         const int lane = threadIdx.x & 63;
+        const float low = value_of(least);
         const uint32_t size = queue_chunks(s, r.chunks, least);
-        each_chunk(s, r, size, [&](const float(&x)[kPer], int c) {
+        for (uint32_t q = threadIdx.x >> 6; q < size; q += kPickWaves) {
+            const int c = __builtin_amdgcn_readfirstlane(s.queue[q]);
+            const Raw x = load_chunk<D>(r.logits, r.vocab, c, lane);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const uint32_t k = key_of(x[i]);
-                if (k >= least) f(k, chunk_at<D>(c, lane, i));
+            for (int i = 0; i < kVec<D>; ++i) {
+                const float l = logit<D>(x, i);
+                if (l >= low) f(key_of(l), c * kChunkOf<D> + lane * kVec<D> + i);
             }
-        });
+        }
     }
 };
 
@@ -393,24 +475,32 @@ __device__ __forceinline__ void to_list(Shared &s, uint32_t key, int at) {
 // Candidates from key `least` to `most` into the list, in no order. False if they
 // do not fit.
 template <int D>
-__device__ __forceinline__ bool collect(Shared &s, const InRow<D> &from, uint32_t least,
-                                        uint32_t most) {
-    if (threadIdx.x == 0) s.list_size = 0;  // each() waits before it reads or adds
-    from.each(least, [&](uint32_t k, int at) {
-        if (k <= most) to_list(s, k, at);
-    });
+__device__ __forceinline__ bool collect(Shared &s, const Row<D> &r, uint32_t least, uint32_t most) {
+    const int lane = threadIdx.x & 63;
+    const float low = value_of(least), high = value_of(most);
+    if (threadIdx.x == 0) s.list_size = 0;  // queue_chunks() waits
+    const uint32_t size = queue_chunks(s, r.chunks, least);
+    each_batch(s, r, size, [&](const Raw &x, int c) {
+#pragma unroll
+        for (int i = 0; i < kVec<D>; ++i) {
+            const float l = logit<D>(x, i);
+            if (l >= low && l <= high) to_list(s, key_of(l), c * kChunkOf<D> + lane * kVec<D> + i);
+        }
+        return uint64_t{0};
+    }, [](uint64_t, int) {});
     __syncthreads();
     return s.list_size <= kList;
 }
 
 // The bin in which the running sum over bins reaches target (>= 1), and the sum
 // before it; false if the whole sum does not reach it.
-__device__ __forceinline__ bool find_bin(Shared &s, int bins, uint64_t target, uint32_t &bin,
-                                         uint64_t &before) {
+template <class B>
+__device__ __forceinline__ bool find_bin(Shared &s, const B *hist, int bins, uint64_t target,
+                                         uint32_t &bin, uint64_t &before) {
     static_assert(kBins <= 2 * kThreads, "two bins a thread");
     __syncthreads();
     const int b = 2 * threadIdx.x;
-    const uint64_t v0 = b < bins ? s.hist[b] : 0, v1 = b + 1 < bins ? s.hist[b + 1] : 0;
+    const uint64_t v0 = b < bins ? hist[b] : 0, v1 = b + 1 < bins ? hist[b + 1] : 0;
     uint64_t total;
     const uint64_t run = block_scan(s, v0 + v1, total);
     if (total < target) return false;  // the same in every thread
@@ -431,6 +521,17 @@ __device__ __forceinline__ void clear_bins(Shared &s) {
     __syncthreads();
 }
 
+// Log-linear bins of a 32-bit distance: its first 64 values, then 64 to an octave.
+// The last one ends at 2^32 - 1.
+__device__ __forceinline__ uint32_t far_bin(uint32_t d) {
+    const int e = d < 64 ? 6 : 31 - __builtin_clz(d);
+    return d < 64 ? d : 64 + (e - 6) * 64 + ((d >> (e - 6)) & 63);
+}
+__device__ __forceinline__ int bin_bits(uint32_t bin) { return bin < 64 ? 0 : (bin - 64) / 64; }
+__device__ __forceinline__ uint32_t bin_start(uint32_t bin) {
+    return bin < 64 ? bin : (64 + (bin & 63)) << bin_bits(bin);
+}
+
 struct Border {
     bool found;
     uint32_t key;     // of the element in which the running sum reaches the target
@@ -444,7 +545,7 @@ __device__ __forceinline__ Border narrow(Shared &s, const From &from, uint32_t t
                                          W weight) {
     while (bits > 0) {
         const int shift = bits > 10 ? bits - 10 : 0;
-        const uint32_t last = lo + ((1u << bits) - 1);  // no more than 2^32 - 1: see seek()
+        const uint32_t last = lo + ((1u << bits) - 1);  // no more than 2^32 - 1
         uint32_t least = top >= last ? top - last : 0;
         if (least <= floor) least = floor + 1;
         clear_bins(s);
@@ -454,7 +555,7 @@ __device__ __forceinline__ Border narrow(Shared &s, const From &from, uint32_t t
         });
         uint32_t bin;
         uint64_t in;
-        if (!find_bin(s, 1024, target - before, bin, in)) return Border{false, 0, 0};
+        if (!find_bin(s, s.hist, 1024, target - before, bin, in)) return Border{false, 0, 0};
         before += in;
         lo += bin << shift;
         bits = shift;
@@ -464,30 +565,26 @@ __device__ __forceinline__ Border narrow(Shared &s, const From &from, uint32_t t
 
 // In descending order of keys from `top` down to, not including, `floor`: where
 // does the running sum of weights reach target? Histograms over the distance
-// d = top - key: first log-linear bins, 64 to an octave, over all 32 bits, then
-// 1024 at a time inside the bin that was found.
+// d = top - key: first log-linear bins, then 1024 at a time inside the bin that
+// was found.
 template <class From, class W>
 __device__ __forceinline__ Border seek(Shared &s, const From &from, uint32_t top, uint32_t floor,
                                        uint64_t target, W weight) {
     clear_bins(s);
     from.each(floor + 1, [&](uint32_t k, int) {
-        const uint32_t d = top - k;
-        const int e = d < 64 ? 6 : 31 - __builtin_clz(d);
-        const uint32_t bin = d < 64 ? d : 64 + (e - 6) * 64 + ((d >> (e - 6)) & 63);
-        add(s.hist[bin], weight(k));
+        add(s.hist[far_bin(top - k)], weight(k));
     });
     uint32_t bin;
     uint64_t before;
-    if (!find_bin(s, kBins, target, bin, before)) return Border{false, 0, 0};
-    // the last bin of 64 << 25 distances ends at 2^32 - 1
-    const int bits = bin < 64 ? 0 : (bin - 64) / 64;
-    const uint32_t lo = bin < 64 ? bin : (64 + (bin & 63)) << bits;
+    if (!find_bin(s, s.hist, kBins, target, bin, before)) return Border{false, 0, 0};
+    const int bits = bin_bits(bin);
+    const uint32_t lo = bin_start(bin);
     if constexpr (!std::is_same_v<From, InList>) {
         if (bits > 0) {
             const uint32_t last = lo + ((1u << bits) - 1);
             uint32_t least = top >= last ? top - last : 0;
             if (least <= floor) least = floor + 1;
-            if (collect(s, from, least, top - lo))
+            if (collect(s, from.r, least, top - lo))
                 return narrow(s, InList{s, s.list_size}, top, floor, lo, bits, before, target,
                               weight);
         }
@@ -510,8 +607,9 @@ __device__ __forceinline__ uint64_t kept_units(Shared &s, const From &from, cons
     uint64_t sum = 0;
     uint64_t ties = 0;
     from.each(keep.key, [&](uint32_t k, int) {
-        if (k > keep.key) sum += r.units(k);
-        else ++ties;
+        const bool above = k > keep.key;  // (two branches put the sums into memory)
+        sum += above ? r.units(k) : 0;
+        ties += !above;
     });
     const uint64_t all = block_sum(s, sum);
     uint64_t tied = block_sum(s, ties);
@@ -524,6 +622,14 @@ __device__ __forceinline__ uint64_t share(float part, uint64_t all) {
     const double p = static_cast<double>(part) * static_cast<double>(all);
     const uint64_t t = p > 1.0 ? static_cast<uint64_t>(p) : 1;
     return static_cast<double>(t) < p ? t + 1 : t;
+}
+
+// The place of a random number in [0, all).
+__device__ __forceinline__ uint64_t place(float u, uint64_t all) {
+    const uint64_t at = u > 0.0f ? static_cast<uint64_t>(static_cast<double>(u < 1.0f ? u : 1.0f) *
+                                                         static_cast<double>(all))
+                                 : 0;
+    return at < all ? at : all - 1;
 }
 
 // The fewest in order from `top` whose sum reaches target, of what `keep` leaves
@@ -579,52 +685,55 @@ __device__ __forceinline__ bool window(Shared &s, const Row<D> &r, float part, u
     const float cut = value_of(keep.key), scale = static_cast<float>(r.scale);
     // the whole row comes to 2^31
     const float unit = static_cast<float>(0x1p73 / static_cast<double>(units));
+    uint32_t *hist = reinterpret_cast<uint32_t *>(s.hist);
     clear_bins(s);
     const uint32_t size = queue_chunks(s, r.chunks, keep.key);
-    each_chunk(s, r, size, [&](const float(&x)[kPer], int) {
+    each_batch(s, r, size, [&](const Raw &x, int) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const float z = (x[i] - r.max) * scale;
+        for (int i = 0; i < kVec<D>; ++i) {
+            const float l = logit<D>(x, i);
+            const float z = (l - r.max) * scale;
             const uint32_t w = static_cast<uint32_t>(__builtin_amdgcn_exp2f(z) * unit + 0.5f);
             const uint32_t bin = static_cast<uint32_t>(z * -static_cast<float>(kPerBit));
-            if (x[i] >= cut && w)
-                atomicAdd(reinterpret_cast<uint32_t *>(&s.hist[bin < kBins ? bin : kBins - 1]), w);
+            if (l >= cut && w) atomicAdd(&hist[bin < kBins ? bin : kBins - 1], w);
         }
-    });
-    // A window of 2^-10 of the row's weight to either side: rounded weights are off by
-    // half a unit each, 2^-12 of it for the largest vocabulary.
+        return uint64_t{0};
+    }, [](uint64_t, int) {});
+    // A window of 2^-16 of the row's weight to either side: what rounding and 32-bit
+    // exponentials leave is an order less, unless most of the row weighs next to nothing.
     const double aim = static_cast<double>(part) * 0x1p31;
     uint32_t first, end;
     uint64_t unused;
-    if (!find_bin(s, kBins, aim > 0x1p21 + 1.0 ? static_cast<uint64_t>(aim - 0x1p21) : 1, first,
-                  unused))
+    if (!find_bin(s, hist, kBins, aim > 0x1p15 + 1.0 ? static_cast<uint64_t>(aim - 0x1p15) : 1,
+                  first, unused))
         return false;
-    if (!find_bin(s, kBins, static_cast<uint64_t>(aim + 0x1p21), end, unused) ||
+    if (!find_bin(s, hist, kBins, static_cast<uint64_t>(aim + 0x1p15), end, unused) ||
         end >= kBins - 1)
         return false;
-    const double max = static_cast<double>(r.max);
-    const uint32_t above = first ? key_from(max - first / (kPerBit * r.scale)) : top;
-    uint32_t least = key_from(max - (end + 1) / (kPerBit * r.scale));
+    const uint32_t above = first ? key_from(r.max64 - first / (kPerBit * r.scale)) : top;
+    uint32_t least = key_from(r.max64 - (end + 1) / (kPerBit * r.scale));
     if (least < keep.key) least = keep.key;
-    if (least > above) return false;
+    if (least > above || value_of(above) < r.one) return false;
     const float high = value_of(above), low = value_of(least);
     if (threadIdx.x == 0) s.list_size = 0;
     const uint32_t again = queue_chunks(s, r.chunks, least);
     const int lane = threadIdx.x & 63;
-    each_chunk(s, r, again, [&](const float(&x)[kPer], int c) {
-        double sum = 0.0;  // whole numbers below 2^53: exact
+    each_batch(s, r, again, [&](const Raw &x, int c) {
+        uint64_t sum = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            sum = __builtin_fma(r.units_of(x[i]), x[i] > high ? 1.0 : 0.0, sum);
-            if (x[i] >= low && x[i] <= high) to_list(s, key_of(x[i]), chunk_at<D>(c, lane, i));
+        for (int i = 0; i < kVec<D>; ++i) {
+            const float l = logit<D>(x, i);
+            const uint64_t u = r.units_near(l);
+            sum += l > high ? u : 0;
+            if (l >= low && l <= high) to_list(s, key_of(l), c * kChunkOf<D> + lane * kVec<D> + i);
         }
-        sum = wave_reduce(sum, Add{});
-        if (lane == 0) s.chunk_units[c] = static_cast<uint64_t>(sum);
-    });
+        return sum;
+    }, [&](uint64_t sum, int c) { s.chunk_units[c] = sum; });
     __syncthreads();
     const uint32_t listed = s.list_size;
-    const int tid = threadIdx.x;
-    const uint64_t before = block_sum(s, tid < r.chunks ? s.chunk_units[tid] : 0);
+    uint64_t mine = 0;
+    for (int c = threadIdx.x; c < r.chunks; c += kThreads) mine += s.chunk_units[c];
+    const uint64_t before = block_sum(s, mine);
     const uint64_t target = share(part, units);
     if (listed > kList || before >= target) return false;
     const InList list{s, listed};
@@ -634,8 +743,14 @@ __device__ __forceinline__ bool window(Shared &s, const Row<D> &r, float part, u
     return true;
 }
 
-// Few candidates, and nothing outside them kept: ranked by counting, then every
-// filter is a prefix of the order and every sum a scan.
+// Key, then lower index: sorts as the order of the draw.
+__device__ __forceinline__ uint64_t order_of(uint32_t key, uint32_t at) {
+    return (static_cast<uint64_t>(key) << 32) | static_cast<uint32_t>(~at);
+}
+
+// Few candidates, and nothing outside them kept: each is ranked by counting those
+// above it, then every filter is a prefix of the order and every sum a scan. Four
+// threads, or eight for up to 128 candidates, share one's comparisons.
 template <int D>
 __device__ __forceinline__ void draw_small(Shared &s, const Row<D> &r, const Draw &d, int n,
                                            uint32_t least, uint64_t units, float u, int32_t *out,
@@ -644,42 +759,53 @@ __device__ __forceinline__ void draw_small(Shared &s, const Row<D> &r, const Dra
     uint64_t *order = s.hist;           // as collected, then sorted
     uint64_t *sorted = s.hist + kSmall;
     uint64_t *kept = s.hist + 2 * kSmall;
+    const int parts = n <= kSmall / 2 ? 2 * kThreads / kSmall : kThreads / kSmall;
+    const int span = kThreads / parts;
+    const int e = tid & (span - 1), part = n <= kSmall / 2 ? tid / (kSmall / 2) : tid / kSmall;
+    const int share_of = (n + parts - 1) / parts;
+    const int j0 = share_of * part, j1 = j0 + share_of < n ? j0 + share_of : n;
     if (tid < n) order[tid] = order_of(s.list_key[tid], s.list_at[tid]);
-    rank_all(s, order, n);
+    if (tid < kSmall) {
+        s.rank[tid] = 0;
+        s.sums[tid] = 0;
+    }
+    __syncthreads();
+    if (e < n) {
+        const uint64_t mine = order[e];
+        uint32_t above = 0;
+#pragma unroll 4
+        for (int j = j0; j < j1; ++j) above += order[j] > mine;
+        if (above) atomicAdd(&s.rank[e], above);
+    }
+    __syncthreads();
     if (tid < n) sorted[s.rank[tid]] = order[tid];
-    if (tid < kSmall) s.sums[tid] = 0;
     __syncthreads();
     const uint64_t mine = tid < n ? sorted[tid] : 0;
     const uint32_t key = static_cast<uint32_t>(mine >> 32);
     const uint64_t w = tid < n ? r.units(key) : 0;
     bool in = tid < n && (d.top_k <= 0 || tid < d.top_k);
-    uint64_t top_units;
-    const uint64_t before = block_scan(s, in ? w : 0, top_units);
-    if (d.top_p < 1.0f) in = in && before < share(d.top_p, d.top_k > 0 ? top_units : units);
+    if (d.top_p < 1.0f) {
+        uint64_t top_units;
+        const uint64_t before = block_scan(s, in ? w : 0, top_units);
+        in = in && before < share(d.top_p, d.top_k > 0 ? top_units : units);
+    }
     in = in && (key >= least || tid == 0);
-    uint64_t all;
-    block_scan(s, in ? w : 0, all);
-    if (tid < kSmall) kept[tid] = in ? w : 0;
+    const uint64_t all = block_sum(s, in ? w : 0);
+    if (tid < n) kept[tid] = in ? w : 0;
     __syncthreads();
-    // in index order: the kept weight before each candidate, four threads to one
-    const int e = tid & (kSmall - 1), part = tid / kSmall;
+    // in index order: the kept weight before each candidate
     const uint32_t at_e = e < n ? ~static_cast<uint32_t>(sorted[e]) : 0;
     if (e < n) {
-        const int each = (n + 3) / 4;
-        const int end = each * (part + 1) < n ? each * (part + 1) : n;
         uint64_t sum = 0;
 #pragma unroll 4
-        for (int j = each * part; j < end; ++j)
+        for (int j = j0; j < j1; ++j)
             sum += ~static_cast<uint32_t>(sorted[j]) < at_e ? kept[j] : 0;
-        add(s.sums[e], sum);
+        if (sum) add(s.sums[e], sum);
     }
     __syncthreads();
-    uint64_t at = u > 0.0f ? static_cast<uint64_t>(static_cast<double>(u < 1.0f ? u : 1.0f) *
-                                                   static_cast<double>(all))
-                           : 0;
-    if (at >= all) at = all - 1;
+    const uint64_t at = place(u, all);
     if (in && s.sums[tid] <= at && at < s.sums[tid] + w) {
-        *out = static_cast<int32_t>(at_e);
+        *out = static_cast<int32_t>(~static_cast<uint32_t>(mine));
         if (prob) {
             const double sum = __builtin_ldexp(static_cast<double>(all), -kUnitBits);
             *prob = static_cast<float>(exp2_64(log2_weight(value_of(key), r.max, r.scale)) / sum);
@@ -695,22 +821,26 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Draw d = draw_of(a, t);
     const float u = a.uniform[t];
-    const ChunkStat *stats = static_cast<const ChunkStat *>(a.workspace) + t * n.chunks;
 
     Row<D> r;
     r.logits = static_cast<const Stored<D> *>(a.logits) + t * a.logits_stride;
     r.vocab = a.vocab;
     r.chunks = n.chunks;
-    const float none = -__builtin_inff();
-    ChunkStat mine{0.0, none, 0};
-    if (tid < n.chunks) mine = stats[tid];
-    const uint32_t my_key = mine.max > none ? key_of(mine.max) : 0;
-    if (tid < n.chunks) {
-        s.chunk_key[tid] = my_key;
-        s.chunk_units[tid] = 0;
-        s.chunk_ties[tid] = 0;
+    // a thread's chunks: c0 .. c1 - 1, in index order over the threads
+    const int per = (n.chunks + kThreads - 1) / kThreads;
+    const int c0 = tid * per < n.chunks ? tid * per : n.chunks;
+    const int c1 = c0 + per < n.chunks ? c0 + per : n.chunks;
+    uint32_t my_key = 0;
+    for (int c = c0; c < c1; ++c) {
+        const float m = n.max[t * n.chunks + c];
+        const uint32_t k = m > -__builtin_inff() ? key_of(m) : 0;
+        s.chunk_key[c] = k;
+        s.chunk_units[c] = 0;
+        s.chunk_ties[c] = 0;
+        my_key = k > my_key ? k : my_key;
     }
     if (tid == 0) {
+        s.first_top = kMaxChunks;
         s.chosen = 0;
         s.chosen_at = 0;
         s.chosen_ties = 0;
@@ -724,196 +854,229 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
         return;
     }
     r.max = value_of(top);
-    r.finite = r.max < __builtin_inff();
-    r.scale = d.greedy ? 0.0 : kLog2e / static_cast<double>(d.temperature);
-
-    uint64_t units = 0;   // of this thread's chunk
-    Keep keep{top, 1};
-    bool plain = false;   // every weight above the cut is kept: the scan's sums serve
-    if (!d.greedy) {
-        const double max = static_cast<double>(r.max), tau = static_cast<double>(d.temperature);
-        keep = Keep{r.finite ? key_from(max - kCut * kLn2 * tau) : top, kAllTies};
-        uint32_t least = keep.key;  // of min-p
-        // at an infinite temperature every weight is 1
-        if (d.min_p > 0.0f && r.finite && d.temperature < __builtin_inff()) {
-            const double p = d.min_p < 1.0f ? static_cast<double>(d.min_p) : 1.0;
-            const uint32_t k = key_from(p < 1.0 ? max + log(p) * tau : max);
-            least = k > least ? k : least;
-        }
-        if (tid < n.chunks && my_key >= keep.key && mine.mass > 0.0) {
-            units = static_cast<uint64_t>(__builtin_rint(
-                __builtin_ldexp(mine.mass * exp2_64(log2_weight(mine.max, r.max, r.scale)),
-                                kUnitBits)));
-            units = units > 0 ? units : 1;
-        }
-        const bool by_k = d.top_k > 0, by_p = d.top_p < 1.0f;
-        plain = !by_k && !by_p && !(d.min_p > 0.0f);
-        if (!plain) {
-            const uint64_t row_units = by_p && !by_k ? block_sum(s, units) : 0;
-            // First the candidates above a bound that is known: min-p's, or the rank-th
-            // largest of the chunks' maxima, above which there are at least `rank`. That is
-            // enough for top-k, and likely for a nucleus, unless its weight says that it
-            // holds more tokens.
-            uint32_t from = by_p ? keep.key : least;
-            const int rank = by_k ? d.top_k : kNucleus;
-            const bool wide =
-                by_p && !by_k &&
-                static_cast<double>(d.top_p) * static_cast<double>(row_units) >
-                    static_cast<double>(kNucleusMass) * __builtin_ldexp(1.0, kUnitBits);
-            if ((by_k || (by_p && !wide)) && rank < n.chunks) {
-                if (tid < n.chunks) s.hist[tid] = order_of(my_key, tid);
-                rank_all(s, s.hist, n.chunks);
-                if (tid < n.chunks && s.rank[tid] == static_cast<uint32_t>(rank - 1))
-                    s.bound = my_key;
-                __syncthreads();
-                from = s.bound > from ? s.bound : from;
-            }
-            bool listed = !wide && collect(s, InRow<D>{s, r}, from, top);
-            const InList list{s, s.list_size};
-            if (listed && by_p && !by_k && from > keep.key)
-                listed = kept_units(s, list, r, Keep{from, kAllTies}) >=
-                         share(d.top_p, row_units);
-            if (listed && list.size <= kSmall) {
-                draw_small(s, r, d, static_cast<int>(list.size), least, row_units, u, a.out + t,
-                           a.probs ? a.probs + t : nullptr);
-                return;
-            }
-            if (listed) {
-                keep = filter(s, list, r, d, top, row_units, Keep{from, kAllTies});
-                if (least > keep.key) keep = Keep{least, kAllTies};
-            } else if (by_p && !by_k && window(s, r, d.top_p, top, row_units, keep)) {
-                listed = least <= keep.key;  // else what is above the window counts too much
-                if (!listed) keep = Keep{least, kAllTies};
-            } else {
-                if (by_k || by_p)
-                    keep = filter(s, InRow<D>{s, r}, r, d, top, row_units, keep);
-                if (least > keep.key) keep = Keep{least, kAllTies};
-            }
-            if (listed) {
-                InList{s, s.list_size}.each(keep.key, [&](uint32_t k, int at) {
-                    if (k > keep.key) add(s.chunk_units[at / kChunkElems], r.units(k));
-                    else atomicAdd(&s.chunk_ties[at / kChunkElems], 1u);
-                });
-            } else {
-                __syncthreads();
-                if (tid < n.chunks) s.chunk_units[tid] = 0;
-                const uint32_t size = queue_chunks(s, n.chunks, keep.key);
-                each_chunk(s, r, size, [&](const float(&x)[kPer], int c) {
-                    uint64_t sum = 0;
-                    uint32_t ties = 0;
+    if (d.greedy) {
+        if (my_key == top)
+            for (int c = c0; c < c1; ++c)
+                if (s.chunk_key[c] == top) {
+                    atomicMin(&s.first_top, static_cast<uint32_t>(c));
+                    break;
+                }
+        __syncthreads();
+        if (wave != 0) return;
+        const int c = __builtin_amdgcn_readfirstlane(s.first_top);
+        const Raw x = load_chunk<D>(r.logits, r.vocab, c, lane);
+        int here = kVec<D>;
 #pragma unroll
-                    for (int i = 0; i < kPer; ++i) {
-                        const uint32_t k = key_of(x[i]);
-                        if (k > keep.key) sum += r.units(k);
-                        ties += k == keep.key;
-                    }
-                    sum = wave_reduce(sum, Add{});
-                    ties = wave_reduce(ties, Add{});
-                    if (lane == 0) {
-                        s.chunk_units[c] = sum;
-                        s.chunk_ties[c] = ties;
-                    }
-                });
-            }
-            __syncthreads();
-            units = tid < n.chunks ? s.chunk_units[tid] : 0;
+        for (int i = kVec<D> - 1; i >= 0; --i)
+            if (logit<D>(x, i) == r.max) here = i;
+        const uint64_t hit = __ballot(here < kVec<D>);
+        if (hit && lane == __builtin_ctzll(hit)) {
+            a.out[t] = c * kChunkOf<D> + lane * kVec<D> + here;
+            if (a.probs) a.probs[t] = 1.0f;
         }
+        return;
+    }
+    r.max64 = static_cast<double>(r.max);
+    r.finite = r.max < __builtin_inff();
+    const double tau = static_cast<double>(d.temperature);
+    r.scale = kLog2e / tau;
+    r.one = value_of(key_from(r.max64 - kUnitBits * kLn2 * tau));
+
+    Keep keep{r.finite ? key_from(r.max64 - kCut * kLn2 * tau) : top, kAllTies};
+    uint32_t least = keep.key;  // of min-p
+    // at an infinite temperature every weight is 1
+    if (d.min_p > 0.0f && r.finite && d.temperature < __builtin_inff()) {
+        const double p = d.min_p < 1.0f ? static_cast<double>(d.min_p) : 1.0;
+        const uint32_t k = key_from(p < 1.0 ? r.max64 + log(p) * tau : r.max64);
+        least = k > least ? k : least;
+    }
+    const bool by_k = d.top_k > 0, by_p = d.top_p < 1.0f;
+    // every weight above the cut is kept: the scan's sums serve
+    const bool plain = !by_k && !by_p && !(d.min_p > 0.0f);
+    uint64_t row_units = 0;
+    if (plain || (by_p && !by_k)) {
+        uint64_t mine = 0;
+        for (int c = c0; c < c1; ++c) {
+            if (s.chunk_key[c] < keep.key) continue;
+            const double w = exp2_64(log2_weight(value_of(s.chunk_key[c]), r.max, r.scale)) *
+                             n.mass[t * n.chunks + c];
+            uint64_t units = static_cast<uint64_t>(
+                __builtin_rint(__builtin_ldexp(w, kUnitBits)));
+            units = units > 0 ? units : 1;
+            if (plain) s.chunk_units[c] = units;
+            mine += units;
+        }
+        if (!plain) row_units = block_sum(s, mine);
+    }
+    if (!plain) {
+        // First the candidates above a bound that is known: min-p's, or (to a bin) the
+        // rank-th largest of the maxima, above which there are at least `rank`. That is
+        // enough for top-k, and likely for a nucleus, unless its weight says that it
+        // holds more tokens.
+        uint32_t from = by_p ? keep.key : least;
+        const int rank = by_k ? d.top_k : kNucleus;
+        const int groups = (n.chunks + per - 1) / per;
+        const bool wide =
+            by_p && !by_k &&
+            static_cast<double>(d.top_p) * static_cast<double>(row_units) >
+                static_cast<double>(kNucleusMass) * __builtin_ldexp(1.0, kUnitBits);
+        if ((by_k || (by_p && !wide)) && rank < groups) {
+            clear_bins(s);
+            if (tid < groups) add(s.hist[far_bin(top - my_key)], 1);
+            uint32_t bin;
+            uint64_t unused;
+            find_bin(s, s.hist, kBins, static_cast<uint64_t>(rank), bin, unused);
+            const uint32_t last = bin_start(bin) + ((1u << bin_bits(bin)) - 1);
+            const uint32_t bound = top > last ? top - last : 0;
+            from = bound > from ? bound : from;
+        }
+        bool listed = !wide && collect(s, r, from, top);
+        const InList list{s, s.list_size};
+        if (listed && by_p && !by_k && from > keep.key)
+            listed = kept_units(s, list, r, Keep{from, kAllTies}) >=
+                     share(d.top_p, row_units);
+        if (listed && list.size <= kSmall) {
+            draw_small(s, r, d, static_cast<int>(list.size), least, row_units, u, a.out + t,
+                       a.probs ? a.probs + t : nullptr);
+            return;
+        }
+        if (listed) {
+            keep = filter(s, list, r, d, top, row_units, Keep{from, kAllTies});
+            if (least > keep.key) keep = Keep{least, kAllTies};
+        } else if (by_p && !by_k && window(s, r, d.top_p, top, row_units, keep)) {
+            listed = least <= keep.key;  // else what is above the window counts too much
+            if (!listed) keep = Keep{least, kAllTies};
+        } else {
+            if (by_k || by_p) keep = filter(s, InRow<D>{s, r}, r, d, top, row_units, keep);
+            if (least > keep.key) keep = Keep{least, kAllTies};
+        }
+        if (listed) {
+            InList{s, s.list_size}.each(keep.key, [&](uint32_t k, int at) {
+                if (k > keep.key) add(s.chunk_units[at / kChunkOf<D>], r.units(k));
+                else atomicAdd(&s.chunk_ties[at / kChunkOf<D>], 1u);
+            });
+        } else {
+            __syncthreads();
+            for (int c = c0; c < c1; ++c) s.chunk_units[c] = 0;
+            const float low = value_of(keep.key);
+            const uint32_t size = queue_chunks(s, n.chunks, keep.key);
+            // a chunk's ties in the ten top bits of its sum, which weights leave free
+            each_batch(s, r, size, [&](const Raw &x, int) {
+                uint64_t sum = 0;
+#pragma unroll
+                for (int i = 0; i < kVec<D>; ++i) {
+                    const float l = logit<D>(x, i);
+                    if (l > low) sum += r.units(key_of(l));
+                    sum += l == low ? uint64_t{1} << 54 : 0;
+                }
+                return sum;
+            }, [&](uint64_t sum, int c) {
+                s.chunk_units[c] = sum & ((uint64_t{1} << 54) - 1);
+                s.chunk_ties[c] = static_cast<uint32_t>(sum >> 54);
+            });
+        }
+        __syncthreads();
     }
 
     // The chunk of the token, in index order over the kept weights.
-    uint64_t ties_before = 0;
+    uint64_t ties_before = 0, ties = 0;
+    const uint64_t tie_units = r.units(keep.key);
+    const auto kept_ties = [&](uint64_t before, int c) {  // of chunk c, `before` ties before it
+        const uint64_t here = s.chunk_ties[c];
+        const uint64_t left = keep.ties > before ? keep.ties - before : 0;
+        return here < left ? here : left;
+    };
     if (!plain) {
-        const uint64_t ties = d.greedy ? (my_key == top ? 1 : 0)
-                                       : tid < n.chunks ? s.chunk_ties[tid] : 0;
+        for (int c = c0; c < c1; ++c) ties += s.chunk_ties[c];
         uint64_t tied;
         ties_before = block_scan(s, ties, tied);
-        const uint64_t left = keep.ties > ties_before ? keep.ties - ties_before : 0;
-        const uint64_t kept = ties < left ? ties : left;
-        if (kept) units += kept * (d.greedy ? 1 : r.units(keep.key));
+    }
+    uint64_t units = 0, run_ties = ties_before;
+    for (int c = c0; c < c1; ++c) {
+        units += s.chunk_units[c];
+        if (plain) continue;
+        units += kept_ties(run_ties, c) * tie_units;
+        run_ties += s.chunk_ties[c];
     }
     uint64_t all;
     const uint64_t before = block_scan(s, units, all);
-    uint64_t at = u > 0.0f ? static_cast<uint64_t>(static_cast<double>(u < 1.0f ? u : 1.0f) *
-                                                   static_cast<double>(all))
-                           : 0;
-    if (at >= all) at = all - 1;
+    const uint64_t at = place(u, all);
     if (units && before <= at && at < before + units) {
-        s.chosen = tid;
-        s.chosen_at = at - before;
-        s.chosen_ties = ties_before;
+        uint64_t run = before;
+        run_ties = ties_before;
+        for (int c = c0; c < c1; ++c) {
+            const uint64_t here =
+                s.chunk_units[c] + (plain ? 0 : kept_ties(run_ties, c) * tie_units);
+            if (at < run + here) {
+                s.chosen = c;
+                s.chosen_at = at - run;
+                s.chosen_ties = run_ties;
+                break;
+            }
+            run += here;
+            if (!plain) run_ties += s.chunk_ties[c];
+        }
     }
     __syncthreads();
     if (wave != 0) return;
 
-    // The token inside the chunk: which vector of the lanes, then which lane, then which
-    // element.
+    // The token inside the chunk: which lane, then which of its logits.
     const int c = __builtin_amdgcn_readfirstlane(s.chosen);
-    uint64_t want = s.chosen_at;
-    uint64_t ties_run = s.chosen_ties;
-    float x[kPer];
-    load_chunk<D>(r.logits, r.vocab, c, lane, x);
-    constexpr int VE = kVecElems<D>;
-    int token = -1, last = -1;
+    const uint64_t want = s.chosen_at;
+    const Raw x = load_chunk<D>(r.logits, r.vocab, c, lane);
+    const float low_kept = value_of(keep.key);
+    uint64_t w[kVec<D>], sum = 0, rank = s.chosen_ties;
+    if (keep.ties != kAllTies) {
+        uint64_t mine = 0;
 #pragma unroll
-    for (int v = 0; v < kPer / VE; ++v) {
-        uint64_t w[VE], sum = 0;
-        uint32_t ties = 0;
-#pragma unroll
-        for (int i = 0; i < VE; ++i) ties += key_of(x[v * VE + i]) == keep.key;
-        uint64_t rank = ties_run;
-        if (keep.ties != kAllTies) {
-            const uint64_t tie_scan = wave_scan(ties);
-            rank += tie_scan - ties;
-            ties_run += lane_value(tie_scan, 63);
-        }
-#pragma unroll
-        for (int i = 0; i < VE; ++i) {
-            const uint32_t k = key_of(x[v * VE + i]);
-            const bool tie = k == keep.key;
-            const bool in = k > keep.key || (tie && rank < keep.ties);
-            rank += tie;
-            w[i] = !in ? 0 : d.greedy ? 1 : r.units(k);
-            sum += w[i];
-        }
-        const uint64_t scan = wave_scan(sum);
-        uint64_t low = scan - sum;
-        int here = -1, kept = -1;
-#pragma unroll
-        for (int i = 0; i < VE; ++i) {
-            if (w[i] && low <= want && want < low + w[i]) here = chunk_at<D>(c, lane, v * VE + i);
-            if (w[i]) kept = chunk_at<D>(c, lane, v * VE + i);
-            low += w[i];
-        }
-        const uint64_t hit = __ballot(here >= 0), any = __ballot(kept >= 0);
-        if (any) last = lane_value(kept, 63 - __builtin_clzll(any));
-        if (hit) {
-            token = lane_value(here, __builtin_ctzll(hit));
-            break;
-        }
-        want -= lane_value(scan, 63);
+        for (int i = 0; i < kVec<D>; ++i) mine += logit<D>(x, i) == low_kept;
+        rank += wave_scan(mine) - mine;
     }
-    if (token < 0) token = last < 0 ? 0 : last;  // the chunk's own sum was rounded up
+#pragma unroll
+    for (int i = 0; i < kVec<D>; ++i) {
+        const float l = logit<D>(x, i);
+        const bool tie = l == low_kept;
+        const bool in = l > low_kept || (tie && rank < keep.ties);
+        rank += tie;
+        w[i] = in ? r.units(key_of(l)) : 0;
+        sum += w[i];
+    }
+    uint64_t low = wave_scan(sum) - sum;
+    int here = -1, last = -1;
+#pragma unroll
+    for (int i = 0; i < kVec<D>; ++i) {
+        if (w[i] && low <= want && want < low + w[i]) here = i;
+        if (w[i]) last = i;
+        low += w[i];
+    }
+    // past the last weight, where the chunk's own sum was rounded up
+    const uint64_t hit = __ballot(here >= 0), any = __ballot(last >= 0);
+    const int from_lane = hit ? __builtin_ctzll(hit) : any ? 63 - __builtin_clzll(any) : 0;
+    const int i = lane_value(hit ? here : last, from_lane);
+    const int token = c * kChunkOf<D> + from_lane * kVec<D> + (i < 0 ? 0 : i);
     if (lane == 0) {
         a.out[t] = token;
         if (a.probs) {
-            const double w = exp2_64(log2_weight(widen<D>(r.logits[token]), r.max, r.scale));
-            const double sum = __builtin_ldexp(static_cast<double>(all), -kUnitBits);
-            a.probs[t] = d.greedy ? 1.0f : static_cast<float>(w / sum);
+            const double weight = exp2_64(log2_weight(widen<D>(r.logits[token]), r.max, r.scale));
+            const double whole = __builtin_ldexp(static_cast<double>(all), -kUnitBits);
+            a.probs[t] = static_cast<float>(weight / whole);
         }
     }
 }
 
 template <int D>
-hipError_t launch_sample(const SampleArgs &n, hipStream_t s) {
-    const dim3 scan(n.a.tokens, (n.chunks + kScanWaves - 1) / kScanWaves);
+hipError_t launch_sample(SampleArgs &n, hipStream_t s) {
+    n.chunks = (n.a.vocab + kChunkOf<D> - 1) / kChunkOf<D>;
+    n.mass = static_cast<double *>(n.a.workspace);
+    n.max = reinterpret_cast<float *>(n.mass + static_cast<int64_t>(n.a.tokens) * n.chunks);
+    const int per_group = kScanWaves * kBatch;
+    const dim3 scan(n.a.tokens, (n.chunks + per_group - 1) / per_group);
     scan_kernel<D><<<scan, dim3(kRowWave, kScanWaves), 0, s>>>(n);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     pick_kernel<D><<<n.a.tokens, kThreads, 0, s>>>(n);
     return hipGetLastError();
 }
-
-int32_t chunks_of(int32_t vocab) { return (vocab + kChunkElems - 1) / kChunkElems; }
 
 bool good_sizes(int32_t tokens, int32_t vocab) {
     return tokens >= 0 && tokens <= SIFAR_ROWS_MAX_TOKENS && vocab >= 1 &&
@@ -957,7 +1120,8 @@ bool good(const sifar_sample_args &a) {
 extern "C" int64_t sifar_sample_workspace(int32_t tokens, int32_t vocab) {
     using namespace sifar;
     if (!good_sizes(tokens, vocab)) return SIFAR_EINVAL;
-    return static_cast<int64_t>(tokens) * chunks_of(vocab) * static_cast<int64_t>(sizeof(ChunkStat));
+    const int64_t chunks = (vocab + kLeastChunk - 1) / kLeastChunk;
+    return tokens * chunks * static_cast<int64_t>(sizeof(double) + sizeof(float));
 }
 
 extern "C" int sifar_sample(const sifar_sample_args *args, void *stream) {
@@ -966,7 +1130,6 @@ extern "C" int sifar_sample(const sifar_sample_args *args, void *stream) {
     if (args->tokens == 0) return SIFAR_OK;
     SampleArgs n{};
     n.a = *args;
-    n.chunks = chunks_of(args->vocab);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = args->dtype == SIFAR_BF16   ? launch_sample<SIFAR_BF16>(n, s)
                          : args->dtype == SIFAR_FP16 ? launch_sample<SIFAR_FP16>(n, s)

@@ -14,9 +14,10 @@ int main() {
         const long double want = exp2l(static_cast<long double>(t));
         const long double e = fabsl(static_cast<long double>(sifar::exp2_64(t)) / want - 1);
         if (e > worst) worst = e;
-        const double i = std::rint(t);
-        const long double s = ldexpl(sifar::exp2_fraction9(t - i), static_cast<int>(i));
-        if (fabsl(s / want - 1) > worst9) worst9 = fabsl(s / want - 1);
+        if (t < -1000 || t > 0) return;
+        const long double q = sifar::exp2_quick<0>(t) / want;
+        const long double s = ldexpl(sifar::exp2_quick<42>(t), -42) / want;
+        worst9 = fmaxl(worst9, fmaxl(fabsl(q - 1), fabsl(s - 1)));
     };
     for (int i = 0; i < 2000000; ++i) {
         see(frac(rng));
@@ -26,6 +27,8 @@ int main() {
         if (sifar::exp2_64(i) != std::ldexp(1.0, i)) return std::printf("2^%d\n", i), 1;
         see(i + 0.5);
         see(std::nextafter(i + 0.5, 0.0));
+        if (i <= 0 && i >= -1000 && sifar::exp2_quick<42>(i) != std::ldexp(1.0, i + 42))
+            return std::printf("2^%d quick\n", i), 1;
     }
     std::printf("%.3Le %.3Le\n", worst, worst9);
     return worst < 3e-16L && worst9 < 4e-14L ? 0 : 1;
