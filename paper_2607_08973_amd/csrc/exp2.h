@@ -5,7 +5,9 @@
 // interpolates (2^f - 1) / f at Chebyshev nodes; its degree sets the error
 // (tests/test_exp2.py measures both against 80-bit arithmetic). f = 0 gives 1
 // exactly. One fma per degree: on gfx950 a 64-bit fma issues at the rate of an
-// unpacked 32-bit one, so 64 bits cost the longer polynomial and nothing else.
+// unpacked 32-bit one. Rounding to i and scaling by 2^i are additions to the bits:
+// the conversions and ldexp that they replace issue at a fraction of that rate.
+// Outside the stated ranges the result is garbage, but nothing traps.
 #pragma once
 
 #include <stdint.h>
@@ -18,8 +20,23 @@
 
 namespace sifar {
 
-// 1 + f q(f), relative error below 3e-16.
-SIFAR_HD double exp2_fraction(double f) {
+// i in the low bits, for |t| below 2^31.
+SIFAR_HD double exp2_magic(double t) { return t + 0x1.8p52; }
+
+// q * 2^i, where exponents stay in range.
+SIFAR_HD double exp2_scale(double q, double magic) {
+    uint64_t bits, shift;
+    __builtin_memcpy(&bits, &q, 8);
+    __builtin_memcpy(&shift, &magic, 8);
+    bits += static_cast<uint64_t>(static_cast<uint32_t>(shift) << 20) << 32;
+    __builtin_memcpy(&q, &bits, 8);
+    return q;
+}
+
+// 2^t for |t| <= 1020, relative error below 3e-16.
+SIFAR_HD double exp2_64(double t) {
+    const double m = exp2_magic(t);
+    const double f = t - (m - 0x1.8p52);
     double q = 0x1.e9d4d5f786506p-32;
     q = __builtin_fma(q, f, 0x1.e606425df1ca8p-28);
     q = __builtin_fma(q, f, 0x1.b524fa5b1918cp-24);
@@ -31,17 +48,15 @@ SIFAR_HD double exp2_fraction(double f) {
     q = __builtin_fma(q, f, 0x1.c6b08d704a0c2p-5);
     q = __builtin_fma(q, f, 0x1.ebfbdff82c598p-3);
     q = __builtin_fma(q, f, 0x1.62e42fefa39efp-1);
-    return __builtin_fma(q, f, 1.0);
+    return exp2_scale(__builtin_fma(q, f, 1.0), m);
 }
 
 // 2^(t + BITS) for t in [-1000, 0], relative error below 4e-14: for sums in units of
-// 2^-42. Rounding to i and scaling by 2^i are additions to the bits: the
-// conversions and ldexp that they replace issue at a quarter of an fma's rate.
-// Elsewhere the result is garbage, but nothing traps.
+// 2^-42.
 template <int BITS>
 SIFAR_HD double exp2_quick(double t) {
     constexpr double s = static_cast<double>(1ull << BITS);
-    const double m = t + 0x1.8p52;  // i in the low bits
+    const double m = exp2_magic(t);
     const double f = t - (m - 0x1.8p52);
     double q = 0x1.b638808675ca6p-24 * s;
     q = __builtin_fma(q, f, 0x1.63d136355f669p-20 * s);
@@ -52,19 +67,7 @@ SIFAR_HD double exp2_quick(double t) {
     q = __builtin_fma(q, f, 0x1.c6b08d7047e52p-5 * s);
     q = __builtin_fma(q, f, 0x1.ebfbdff823cedp-3 * s);
     q = __builtin_fma(q, f, 0x1.62e42fefa39efp-1 * s);
-    q = __builtin_fma(q, f, s);
-    uint64_t bits, shift;
-    __builtin_memcpy(&bits, &q, 8);
-    __builtin_memcpy(&shift, &m, 8);
-    bits += static_cast<uint64_t>(static_cast<uint32_t>(shift) << 20) << 32;
-    __builtin_memcpy(&q, &bits, 8);
-    return q;
-}
-
-// 2^t for |t| <= 1020.
-SIFAR_HD double exp2_64(double t) {
-    const double i = __builtin_rint(t);
-    return __builtin_ldexp(exp2_fraction(t - i), static_cast<int>(i));
+    return exp2_scale(__builtin_fma(q, f, s), m);
 }
 
 }  // namespace sifar

@@ -1,13 +1,18 @@
 // Routing to experts: sifar_route. gfx950 (MI355X) only.
 //
 // One wave a token. Lane l holds EPL adjacent experts, groups of experts lie in
-// segments of lanes, so an expert's index grows with its place in the wave. The
-// order of the experts is exact: a token's logits become 64-bit keys that sort
-// as (score + bias, lowest index first), each lane sorts its own, and top-k takes
-// k times the largest of the 64 heads. A key is a double whose ten lowest bits
-// hold the index, so keys differ, one v_max_f64 compares value and index, and the
-// largest names its expert. Bound: for many tokens the instructions of the sort
-// and of the k steps; for one token their latency.
+// segments of lanes, so an expert's index grows with its place in the wave. A
+// token's logits become keys that sort as (score + bias, lowest index first) and
+// differ; each lane sorts its own, and top-k takes k times the largest of the 64
+// heads, whose key names its expert.
+//
+// Where a bias or groups decide, keys are 64-bit scores whose ten lowest bits hold
+// the index, so that scores next to each other rank as they should: in 32 bits six
+// of 16384 tokens chose another expert. Without them the logits' own order is the
+// answer, and 16-bit logits fit a 32-bit key together with the index.
+//
+// Bound: for many tokens the instructions of the sort and of the k steps; for one
+// token their latency.
 #include <hip/hip_runtime.h>
 
 #include "exp2.h"
@@ -17,10 +22,11 @@ namespace sifar {
 namespace {
 
 constexpr int kIndexBits = 10;  // experts of a token: at most 1024
-constexpr uint64_t kIndexMask = (1u << kIndexBits) - 1;
+constexpr uint32_t kIndexMask = (1u << kIndexBits) - 1;
 constexpr int kWaves = 4;       // tokens of a workgroup
 constexpr double kLog2e = 1.4426950408889634;
 constexpr double kLargest = 1.7976931348623157e308;
+static_assert(SIFAR_ROUTE_MAX_EXPERTS <= 1 << kIndexBits, "an index fits a key");
 
 struct RouteArgs {
     sifar_route_args a;
@@ -38,25 +44,88 @@ __device__ __forceinline__ double min64(double a, double b) {
     asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
     return r;
 }
-struct Max64 {
-    __device__ __forceinline__ double operator()(double a, double b) const { return max64(a, b); }
-};
+
+// Over the wave, in a scalar register: DPP moves up within rows of 16, then from row
+// to row; the last lane holds the result. 0 where no lane offers more.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    const auto step = [&](auto ctrl, auto rows) {
+        const uint32_t y = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(
+            0, static_cast<int>(x), decltype(ctrl)::value, decltype(rows)::value, 0xF, false));
+        x = x > y ? x : y;
+    };
+    using std::integral_constant;
+    step(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});  // row_shr:1
+    step(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
+    step(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
+    step(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
+    step(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // row_bcast:15
+    step(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // row_bcast:31
+    return lane_value(x, 63);
+}
+
+// ---- keys ------------------------------------------------------------------------
 
 // A finite value and an expert as one double that sorts by value (to 2^-42 of it),
 // then by the lower index.
-__device__ __forceinline__ double key_of(double value, int expert) {
+__device__ __forceinline__ double wide_key(double value, int expert) {
     value = min64(max64(value + 0.0, -kLargest), kLargest);  // -0 counts as 0
     const uint64_t bits = __builtin_bit_cast(uint64_t, value);
     // more mantissa is a larger positive and a smaller negative number
     const uint64_t code = bits >> 63 ? expert : kIndexMask - expert;
-    return __builtin_bit_cast(double, (bits & ~kIndexMask) | code);
+    return __builtin_bit_cast(double, (bits & ~uint64_t{kIndexMask}) | code);
 }
 
-__device__ __forceinline__ int expert_of(double key) {
+// The same as an integer that sorts alike, and never 0.
+__device__ __forceinline__ uint64_t ordered(double key) {
     const uint64_t bits = __builtin_bit_cast(uint64_t, key);
-    const uint32_t code = static_cast<uint32_t>(bits & kIndexMask);
-    return static_cast<int>(bits >> 63 ? code : kIndexMask - code);
+    return bits >> 63 ? ~bits : bits | uint64_t{1} << 63;
 }
+
+__device__ __forceinline__ int wide_expert(uint32_t low) {  // of ordered()'s low word
+    return static_cast<int>(kIndexMask - (low & kIndexMask));
+}
+
+// A finite 16-bit logit and an expert as 32 bits that sort alike. Never 0.
+template <int D>
+__device__ __forceinline__ uint32_t short_key(uint32_t bits, int expert) {
+    bits = bits == 0x8000u ? 0u : bits;  // -0 counts as 0
+    const uint32_t order = bits & 0x8000u ? ~bits & 0xFFFFu : bits | 0x8000u;
+    return order << 16 | (kIndexMask - static_cast<uint32_t>(expert));
+}
+
+template <int D>
+__device__ __forceinline__ float short_logit(uint32_t key) {
+    const uint32_t order = key >> 16;
+    return widen<D>(order & 0x8000u ? order & 0x7FFFu : ~order & 0xFFFFu);
+}
+
+__device__ __forceinline__ void exchange(double &hi, double &lo) {
+    const double m = max64(hi, lo);
+    lo = min64(hi, lo);
+    hi = m;
+}
+__device__ __forceinline__ void exchange(uint32_t &hi, uint32_t &lo) {
+    const uint32_t m = hi > lo ? hi : lo;
+    lo = hi > lo ? lo : hi;
+    hi = m;
+}
+
+// Descending odd-even merge sort (Batcher) of a lane's keys.
+template <int N, class K>
+__device__ __forceinline__ void sort_descending(K (&k)[N]) {
+#pragma unroll
+    for (int p = 1; p < N; p *= 2)
+#pragma unroll
+        for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+            for (int j = q % p; j + q < N; j += 2 * q)
+#pragma unroll
+                for (int i = 0; i < q; ++i)
+                    if (i + j + q < N && (i + j) / (2 * p) == (i + j + q) / (2 * p))
+                        exchange(k[i + j], k[i + j + q]);
+}
+
+// ---- scores ----------------------------------------------------------------------
 
 // 1 / d for d in [1, 2^1000]: the hardware's estimate and two Newton steps.
 __device__ __forceinline__ double inverse(double d) {
@@ -68,32 +137,15 @@ __device__ __forceinline__ double inverse(double d) {
 // Scores below 2^-1000 are 0, which keeps every exponent in range.
 __device__ __forceinline__ double sigmoid(float x) {
     const double t = max64(-kLog2e * static_cast<double>(x), -1000.0);
-    return t > 1000.0 ? 0.0 : inverse(1.0 + exp2_64(t));
+    const double s = inverse(1.0 + exp2_64(t));
+    return t > 1000.0 ? 0.0 : s;
 }
 
 // exp(x - m); 1 at the largest logit, which may be infinite.
 __device__ __forceinline__ double softmax_weight(float x, float m) {
-    if (x == m) return 1.0;
     const double t = (static_cast<double>(x) - static_cast<double>(m)) * kLog2e;
-    return t < -1000.0 ? 0.0 : exp2_64(t);
-}
-
-// Descending odd-even merge sort (Batcher) of a lane's keys.
-template <int N>
-__device__ __forceinline__ void sort_descending(double (&k)[N]) {
-#pragma unroll
-    for (int p = 1; p < N; p *= 2)
-#pragma unroll
-        for (int q = p; q >= 1; q /= 2)
-#pragma unroll
-            for (int j = q % p; j + q < N; j += 2 * q)
-#pragma unroll
-                for (int i = 0; i < q; ++i)
-                    if (i + j + q < N && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
-                        const double hi = max64(k[i + j], k[i + j + q]);
-                        k[i + j + q] = min64(k[i + j], k[i + j + q]);
-                        k[i + j] = hi;
-                    }
+    const double w = exp2_64(t);
+    return x == m ? 1.0 : t > -1000.0 ? w : 0.0;
 }
 
 // The two best of a group, joined with another's.
@@ -103,100 +155,172 @@ __device__ __forceinline__ void join_best(double &b1, double &b2, Pair<double> p
     b2 = max64(min64(p1.a, p1.b), max64(p2.a, p2.b));
 }
 
+// The lane's EPL stored logits: 16 bytes or more at a time where all of them are
+// there (global loads need no alignment beyond an element's).
 template <int D, int EPL>
-__global__ void __launch_bounds__(kRowWave *kWaves) route_kernel(const RouteArgs n) {
-    const sifar_route_args &a = n.a;
-    const int lane = threadIdx.x;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kWaves + threadIdx.y;
-    if (t >= a.tokens) return;
-    const Stored<D> *row = static_cast<const Stored<D> *>(a.logits) + t * a.logits_stride;
-    const int group = lane / n.lanes;
-    const int inside = (lane & (n.lanes - 1)) * EPL;   // of the group
-    const int first = group * n.per + inside;
-    int mine = group < a.groups ? n.per - inside : 0;  // experts of this lane
-    const float none = -__builtin_inff();
+__device__ __forceinline__ void load_logits(const Stored<D> *p, int mine, uint32_t (&x)[EPL],
+                                            uint32_t none) {
+    struct __attribute__((packed, aligned(sizeof(Stored<D>)))) All {
+        Stored<D> v[EPL];
+    };
+    if (mine >= EPL) {
+        const All all = *reinterpret_cast<const All *>(p);
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) x[j] = all.v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) x[j] = j < mine ? p[j] : none;
+    }
+}
 
-    float x[EPL];
-    float m = none;
+// RANKED: a bias or groups decide. Otherwise the order of the logits does.
+template <int D, int EPL, bool RANKED>
+__global__ void __launch_bounds__(kRowWave *kWaves) route_kernel(const RouteArgs n) {
+    // 16-bit logits in 32-bit keys
+    constexpr bool SHORT = !RANKED && D != SIFAR_FP32;
+    __shared__ float logits[RANKED ? kWaves : 1][RANKED ? kRowWave * EPL : 1];
+    const sifar_route_args &a = n.a;
+    const int lane = threadIdx.x, wave = threadIdx.y;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
+    if (t >= a.tokens) return;
+    const int group = lane / n.lanes;
+    const int inside = (lane & (n.lanes - 1)) * EPL;         // of the group
+    const int first = group * n.per + inside;
+    const int mine = group < a.groups ? n.per - inside : 0;  // experts from `first` on
+    const float none = -__builtin_inff();
+    constexpr uint32_t none_bits = D == SIFAR_FP32 ? 0xFF800000u : D == SIFAR_BF16 ? 0xFF80u : 0xFC00u;
+
+    uint32_t raw[EPL];
+    load_logits<D, EPL>(static_cast<const Stored<D> *>(a.logits) + t * a.logits_stride + first,
+                        mine, raw, none_bits);
+    float x[EPL], m = none;
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
-        x[j] = none;
-        if (j < mine) x[j] = widen<D>(row[first + j]);
+        x[j] = widen<D>(raw[j]);
         if (!(x[j] > none)) x[j] = none;  // NaN
-        m = fmaxf(m, x[j]);
+        m = choose(x[j] > m, x[j], m);
     }
     const bool softmax = a.score == SIFAR_ROUTE_SOFTMAX;
-    double total = 1.0;
+    double scale = 1.0;  // 1 / the sum of the weights, where it matters
     if (softmax) {
         m = wave_reduce(m, Max{});
-        if (a.bias || a.groups > 1 || !a.renorm) {
-            total = 0.0;
+        if (RANKED || !a.renorm) {
+            double total = 0.0;
 #pragma unroll
-            for (int j = 0; j < EPL; ++j) total += x[j] > none ? softmax_weight(x[j], m) : 0.0;
+            for (int j = 0; j < EPL; ++j) {
+                const double w = softmax_weight(x[j], m);
+                total += x[j] > none ? w : 0.0;
+            }
             total = wave_reduce(total, Add{});
+            scale = total > 0.0 ? inverse(total) : 0.0;
         }
     }
-    const double scale = total > 0.0 ? inverse(total) : 0.0;
 
-    double key[EPL];
-    if (a.bias || a.groups > 1) {
-        double choice[EPL];
+    int id = -1;         // of lane i: the i-th best expert
+    float chosen = 0.f;  // and its logit
+    if constexpr (SHORT) {
+        uint32_t key[EPL];
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-            choice[j] = none;
-            if (!(x[j] > none)) continue;
-            const double s = softmax ? softmax_weight(x[j], m) * scale : sigmoid(x[j]);
-            const double c = a.bias ? s + static_cast<double>(a.bias[first + j]) : s;
-            if (c > none) choice[j] = c;
+        for (int j = 0; j < EPL; ++j) key[j] = x[j] > none ? short_key<D>(raw[j], first + j) : 0u;
+        sort_descending(key);
+        uint32_t found = 0;
+        for (int i = 0; i < a.topk; ++i) {
+            const uint32_t best = wave_max(key[0]);
+            found = lane == i ? best : found;
+            const bool taken = key[0] == best;
+#pragma unroll
+            for (int j = 0; j + 1 < EPL; ++j) key[j] = choose(taken, key[j + 1], key[j]);
+            key[EPL - 1] = taken ? 0u : key[EPL - 1];
         }
+        if (found) {
+            id = static_cast<int>(kIndexMask - (found & kIndexMask));
+            chosen = short_logit<D>(found);
+        }
+    } else {
+        double value[EPL];
         bool stay = true;
-        if (a.groups > 1) {
+        if constexpr (RANKED) {
             double b1 = none, b2 = none;
 #pragma unroll
             for (int j = 0; j < EPL; ++j) {
-                b2 = max64(b2, min64(b1, choice[j]));
-                b1 = max64(b1, choice[j]);
+                logits[wave][lane * EPL + j] = x[j];
+                const double s = softmax ? softmax_weight(x[j], m) * scale : sigmoid(x[j]);
+                const double c =
+                    a.bias ? s + static_cast<double>(a.bias[j < mine ? first + j : 0]) : s;
+                // c is not there with its logit, nor at -inf or NaN
+                value[j] = x[j] > none && c > none ? c : none;
+                b2 = max64(b2, min64(b1, value[j]));
+                b1 = max64(b1, value[j]);
             }
-            if (n.lanes > 1) join_best(b1, b2, pair<1>(b1), pair<1>(b2));
-            if (n.lanes > 2) join_best(b1, b2, pair<2>(b1), pair<2>(b2));
-            if (n.lanes > 4) join_best(b1, b2, pair<4>(b1), pair<4>(b2));
-            if (n.lanes > 8) join_best(b1, b2, pair<8>(b1), pair<8>(b2));
-            if (n.lanes > 16) join_best(b1, b2, pair<16>(b1), pair<16>(b2));
-            const double worth = a.group_top == 2 && b2 > none ? b1 + b2 : b1;
-            int better = 0;
-            for (int g = 0; g < a.groups; ++g) {
-                const double other = lane_value(worth, g * n.lanes);
-                better += other > worth || (other == worth && g < group);
+            if (a.groups > 1) {
+                if (n.lanes > 1) join_best(b1, b2, pair<1>(b1), pair<1>(b2));
+                if (n.lanes > 2) join_best(b1, b2, pair<2>(b1), pair<2>(b2));
+                if (n.lanes > 4) join_best(b1, b2, pair<4>(b1), pair<4>(b2));
+                if (n.lanes > 8) join_best(b1, b2, pair<8>(b1), pair<8>(b2));
+                if (n.lanes > 16) join_best(b1, b2, pair<16>(b1), pair<16>(b2));
+                const double worth = a.group_top == 2 && b2 > none ? b1 + b2 : b1;
+                int better = 0;
+                for (int g = 0; g < a.groups; ++g) {
+                    const double other = lane_value(worth, g * n.lanes);
+                    better += other > worth || (other == worth && g < group);
+                }
+                stay = better < a.top_groups;
             }
-            stay = better < a.top_groups;
         }
+        double key[EPL];
 #pragma unroll
-        for (int j = 0; j < EPL; ++j)
-            key[j] = stay && choice[j] > none
-                         ? key_of(a.bias ? choice[j] : static_cast<double>(x[j]), first + j)
-                         : none;
-    } else {
+        for (int j = 0; j < EPL; ++j) {
+            const double v = RANKED && a.bias ? value[j] : static_cast<double>(x[j]);
+            const bool there = RANKED ? stay && value[j] > none : x[j] > none;
+            const double k = wide_key(v, first + j);
+            key[j] = there ? k : none;
+        }
+        sort_descending(key);
+        uint32_t hi[EPL], lo[EPL];
 #pragma unroll
-        for (int j = 0; j < EPL; ++j)
-            key[j] = x[j] > none ? key_of(static_cast<double>(x[j]), first + j) : none;
-    }
-    sort_descending(key);
-
-    int id = -1;  // of lane i: the i-th best
-    for (int i = 0; i < a.topk; ++i) {
-        const double best = wave_reduce(key[0], Max64{});
-        if (!(best > none)) break;  // the same in every lane
-        if (lane == i) id = expert_of(best);
-        const bool taken = key[0] == best;
+        for (int j = 0; j < EPL; ++j) {
+            const uint64_t o = key[j] > none ? ordered(key[j]) : 0;
+            hi[j] = static_cast<uint32_t>(o >> 32);
+            lo[j] = static_cast<uint32_t>(o);
+        }
+        uint32_t found_hi = 0, found_lo = 0;
+        for (int i = 0; i < a.topk; ++i) {
+            // the high words decide, or now and then the low words among equal ones
+            const uint32_t best = wave_max(hi[0]);
+            bool taken = hi[0] == best;
+            uint64_t who = __ballot(taken);
+            if (__builtin_popcountll(who) != 1) {
+                const uint32_t low = wave_max(taken ? lo[0] : 0u);
+                taken = taken && lo[0] == low;
+                who = __ballot(taken);
+            }
+            const uint32_t low = lane_value(lo[0], __builtin_ctzll(who));
+            found_hi = lane == i ? best : found_hi;
+            found_lo = lane == i ? low : found_lo;
 #pragma unroll
-        for (int j = 0; j + 1 < EPL; ++j) key[j] = taken ? key[j + 1] : key[j];
-        key[EPL - 1] = taken ? none : key[EPL - 1];
+            for (int j = 0; j + 1 < EPL; ++j) {
+                hi[j] = choose(taken, hi[j + 1], hi[j]);
+                lo[j] = choose(taken, lo[j + 1], lo[j]);
+            }
+            hi[EPL - 1] = taken ? 0u : hi[EPL - 1];
+        }
+        if constexpr (RANKED) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (found_hi) {
+            id = wide_expert(found_lo);
+            if constexpr (RANKED) {
+                const int g = id / n.per, in = id - g * n.per;
+                chosen = logits[wave][g * n.lanes * EPL + in];
+            } else {
+                // the key holds all of an fp32 logit
+                const uint64_t o = (static_cast<uint64_t>(found_hi) << 32) | found_lo;
+                const uint64_t bits = o >> 63 ? o & ~(uint64_t{1} << 63) : ~o;
+                const double v = __builtin_bit_cast(double, bits & ~uint64_t{kIndexMask});
+                chosen = static_cast<float>(v);
+            }
+        }
     }
     double w = 0.0;
-    if (id >= 0) {
-        const float xi = widen<D>(row[id]);
-        w = softmax ? softmax_weight(xi, m) * scale : sigmoid(xi);
-    }
+    if (id >= 0) w = softmax ? softmax_weight(chosen, m) * scale : sigmoid(chosen);
     if (a.renorm) {
         const double sum = wave_reduce(w, Add{});
         w = sum > 0.0 ? w / sum : 0.0;
@@ -207,17 +331,23 @@ __global__ void __launch_bounds__(kRowWave *kWaves) route_kernel(const RouteArgs
     }
 }
 
+template <int D, int EPL>
+hipError_t launch_epl(const RouteArgs &n, hipStream_t s) {
+    const dim3 grid((n.a.tokens + kWaves - 1) / kWaves), block(kRowWave, kWaves);
+    if (n.a.bias || n.a.groups > 1) route_kernel<D, EPL, true><<<grid, block, 0, s>>>(n);
+    else route_kernel<D, EPL, false><<<grid, block, 0, s>>>(n);
+    return hipGetLastError();
+}
+
 template <int D>
 hipError_t launch_route(const RouteArgs &n, hipStream_t s) {
     const int need = (n.per + n.lanes - 1) / n.lanes;
-    const dim3 grid((n.a.tokens + kWaves - 1) / kWaves), block(kRowWave, kWaves);
-    if (need <= 1) route_kernel<D, 1><<<grid, block, 0, s>>>(n);
-    else if (need <= 2) route_kernel<D, 2><<<grid, block, 0, s>>>(n);
-    else if (need <= 4) route_kernel<D, 4><<<grid, block, 0, s>>>(n);
-    else if (need <= 8) route_kernel<D, 8><<<grid, block, 0, s>>>(n);
-    else if (need <= 16) route_kernel<D, 16><<<grid, block, 0, s>>>(n);
-    else route_kernel<D, 32><<<grid, block, 0, s>>>(n);
-    return hipGetLastError();
+    return need <= 1    ? launch_epl<D, 1>(n, s)
+           : need <= 2  ? launch_epl<D, 2>(n, s)
+           : need <= 4  ? launch_epl<D, 4>(n, s)
+           : need <= 8  ? launch_epl<D, 8>(n, s)
+           : need <= 16 ? launch_epl<D, 16>(n, s)
+                        : launch_epl<D, 32>(n, s);
 }
 
 bool good(const sifar_route_args &a) {

@@ -165,13 +165,20 @@ __device__ __forceinline__ T lane_value(T x, int from) {
     }
 }
 
+// c ? a : b of values. (Written with elements of an array in registers, the operator
+// selects between their addresses, and the array is indexed at run time.)
+template <class T>
+__device__ __forceinline__ T choose(bool c, T a, T b) {
+    return c ? static_cast<T>(a) : static_cast<T>(b);
+}
+
 struct Add {
     template <class T>
     __device__ __forceinline__ T operator()(T a, T b) const { return a + b; }
 };
 struct Max {
     template <class T>
-    __device__ __forceinline__ T operator()(T a, T b) const { return a > b ? a : b; }
+    __device__ __forceinline__ T operator()(T a, T b) const { return choose(a > b, a, b); }
 };
 
 }  // namespace sifar

@@ -200,7 +200,7 @@ struct Max32 {
 // log2 of a weight. 0 at the maximum, which may be infinite; finite elsewhere.
 __device__ __forceinline__ double log2_weight(float x, float max, double c) {
     const double z = (static_cast<double>(x) - static_cast<double>(max)) * c;
-    return x == max ? 0.0 : z > -1100.0 ? z : -1100.0;
+    return x == max ? 0.0 : z > -1000.0 ? z : -1000.0;
 }
 
 // Every chunk's maximum and, where the row needs it, the sum of its weights. What
