@@ -458,6 +458,14 @@ _BLOCK_NORM = struct.Struct("@5i4fP2q2PqPqPq2Pq")
 _ROUTE = struct.Struct("@9if1Pq3P")
 _SAMPLE = struct.Struct("@3iPq8Pq")
 _DTYPES = None  # torch dtype -> SIFAR_* element type
+_F32 = _I32 = _U8 = _C = None  # of torch, once a row operator was called
+
+
+def _torch() -> None:
+    global _DTYPES, _F32, _I32, _U8, _C
+    import torch
+    _F32, _I32, _U8, _C = torch.float32, torch.int32, torch.uint8, torch._C
+    _DTYPES = {torch.bfloat16: SIFAR_BF16, torch.float16: SIFAR_FP16, torch.float32: SIFAR_FP32}
 
 
 def _refuse(fn: str, why: str):
@@ -467,11 +475,6 @@ def _refuse(fn: str, why: str):
 
 
 def _dtype(fn: str, dtype) -> int:
-    global _DTYPES
-    if _DTYPES is None:
-        import torch
-        _DTYPES = {torch.bfloat16: SIFAR_BF16, torch.float16: SIFAR_FP16,
-                   torch.float32: SIFAR_FP32}
     code = _DTYPES.get(dtype)
     if code is None:
         _refuse(fn, f"no element type for {dtype}")
@@ -481,25 +484,28 @@ def _dtype(fn: str, dtype) -> int:
 def _gpu(fn: str, name: str, t) -> int:
     """The current device, which has to hold t."""
     dev = t.get_device()
-    if dev < 0 or dev != _current_device():
+    if dev < 0 or dev != _C._cuda_getDevice():  # a GPU tensor: PyTorch has initialised the GPU
         _refuse(fn, f"{name} is on {t.device}, not on the current GPU")
     return dev
 
 
-def _current_device() -> int:
-    import torch
-    return torch._C._cuda_getDevice()  # a GPU tensor exists: PyTorch has initialised the GPU
+def _row_stream(stream, dev: int):
+    if stream is None:
+        return _C._cuda_getCurrentRawStream(dev)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def _operand(fn: str, name: str, t, dtype, shape, dev: int):
     """Address and leading stride of t, which has to be `dtype` of `shape` on
     device `dev` with adjacent elements: the library sees addresses only."""
-    at = t.stride()
-    if (t.dtype is not dtype or t.shape != shape or t.get_device() != dev
-            or (at[-1] != 1 and shape[-1] > 1)):
-        _refuse(fn, f"{name} is {t.dtype} {tuple(t.shape)} on {t.device} at strides {at}, not "
-                    f"{dtype} {tuple(shape)} on the current GPU with adjacent elements")
-    return t.data_ptr(), at[0]
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev:
+        if t.is_contiguous():
+            return t.data_ptr(), shape[-1]
+        at = t.stride()
+        if at[-1] == 1:
+            return t.data_ptr(), at[0]
+    _refuse(fn, f"{name} is {t.dtype} {tuple(t.shape)} on {t.device} at strides {t.stride()}, not "
+                f"{dtype} {tuple(shape)} on the current GPU with adjacent elements")
 
 
 def sifar_block_norm(x, residual, residual_out, post_weight=None, gate=None, norm_weight=None,
@@ -509,6 +515,8 @@ def sifar_block_norm(x, residual, residual_out, post_weight=None, gate=None, nor
     [hidden] or [1][hidden] for all tokens; residual (or None) and residual_out
     [tokens][hidden] in x's type or float32; norm_weight and y together or neither."""
     fn = "sifar_block_norm"
+    if _C is None:
+        _torch()
     shape, at = x.shape, x.stride()
     if len(shape) == 2:
         parts, part_stride = 1, 0
@@ -545,11 +553,11 @@ def sifar_block_norm(x, residual, residual_out, post_weight=None, gate=None, nor
     if (norm_weight is None) != (y is None):
         _refuse(fn, "norm_weight and y go together")
     code = _dtype(fn, dt)
-    rc = load().sifar_block_norm(
+    rc = (_lib or load()).sifar_block_norm(
         _BLOCK_NORM.pack(code, code if rdt is dt else _dtype(fn, rdt), T, H, parts, branch_scale,
                          residual_scale, weight_offset, eps, x.data_ptr(), at[0], part_stride,
                          post, g, g_stride, res, res_stride, out, out_stride, norm, yp, y_stride),
-        _stream(stream))
+        _row_stream(stream, dev))
     if rc:
         _check(fn, rc)
 
@@ -558,29 +566,31 @@ def sifar_route(logits, ids, weights, score="softmax", bias=None, groups=1, top_
                 group_top=1, renorm=True, scale=1.0, stream=None) -> None:
     """logits [tokens][experts]; ids (int32) and weights (float32) [tokens][topk], contiguous;
     bias [experts] float32; score "softmax" or "sigmoid"."""
-    import torch
     fn = "sifar_route"
+    if _C is None:
+        _torch()
     if logits.dim() != 2 or ids.dim() != 2:
         _refuse(fn, "logits or ids do not have 2 dimensions")
-    T, E = logits.shape
-    out, k = ids.shape, ids.shape[1]
+    shape, out = logits.shape, ids.shape
+    T, E = shape
+    k = out[1]
     if T > SIFAR_ROWS_MAX_TOKENS or E > SIFAR_ROUTE_MAX_EXPERTS or k > SIFAR_ROUTE_MAX_TOPK:
         _refuse(fn, f"{T} x {E}, top {k}, is too large")
     if out[0] != T:
         _refuse(fn, f"ids has {out[0]} rows, logits {T}")
     dev = _gpu(fn, "logits", logits)
-    x, x_stride = _operand(fn, "logits", logits, logits.dtype, logits.shape, dev)
-    i, i_stride = _operand(fn, "ids", ids, torch.int32, out, dev)
-    w, w_stride = _operand(fn, "weights", weights, torch.float32, out, dev)
+    x, x_stride = _operand(fn, "logits", logits, logits.dtype, shape, dev)
+    i, i_stride = _operand(fn, "ids", ids, _I32, out, dev)
+    w, w_stride = _operand(fn, "weights", weights, _F32, out, dev)
     if T > 1 and (i_stride != k or w_stride != k):
         _refuse(fn, "the rows of ids or weights are not adjacent")
-    b = 0 if bias is None else _operand(fn, "bias", bias, torch.float32, logits.shape[1:], dev)[0]
+    b = 0 if bias is None else _operand(fn, "bias", bias, _F32, shape[1:], dev)[0]
     mode = ROUTE_SCORE.get(score, score)
     if mode not in (SIFAR_ROUTE_SOFTMAX, SIFAR_ROUTE_SIGMOID):
         _refuse(fn, f"no score {score!r}")
-    rc = load().sifar_route(
+    rc = (_lib or load()).sifar_route(
         _ROUTE.pack(_dtype(fn, logits.dtype), T, E, k, mode, groups, top_groups, group_top,
-                    1 if renorm else 0, scale, x, x_stride, b, i, w), _stream(stream))
+                    1 if renorm else 0, scale, x, x_stride, b, i, w), _row_stream(stream, dev))
     if rc:
         _check(fn, rc)
 
@@ -601,27 +611,29 @@ def sifar_sample(logits, uniform, out, workspace, probs=None, temperature=None, 
     """logits [tokens][vocab]; uniform, temperature, top_p, min_p float32 [tokens], top_k and out
     int32 [tokens], probs float32 [tokens]; workspace: a contiguous uint8 tensor of
     sifar_sample_workspace(tokens, vocab) bytes, not shared by calls that may overlap."""
-    import torch
     fn = "sifar_sample"
-    if logits.dim() != 2:
-        _refuse(fn, f"logits has {logits.dim()} dimensions, not 2")
-    T, V = logits.shape
+    if _C is None:
+        _torch()
+    shape = logits.shape
+    if len(shape) != 2:
+        _refuse(fn, f"logits has {len(shape)} dimensions, not 2")
+    T, V = shape
     if T > SIFAR_ROWS_MAX_TOKENS or V > SIFAR_SAMPLE_MAX_VOCAB:
         _refuse(fn, f"{T} x {V} is too large")
     dev = _gpu(fn, "logits", logits)
-    rows, f32, i32 = logits.shape[:1], torch.float32, torch.int32
-    x, x_stride = _operand(fn, "logits", logits, logits.dtype, logits.shape, dev)
-    u, _ = _operand(fn, "uniform", uniform, f32, rows, dev)
-    o, _ = _operand(fn, "out", out, i32, rows, dev)
-    ws, _ = _operand(fn, "workspace", workspace, torch.uint8, workspace.shape[:1], dev)
-    p = 0 if probs is None else _operand(fn, "probs", probs, f32, rows, dev)[0]
-    t = 0 if temperature is None else _operand(fn, "temperature", temperature, f32, rows, dev)[0]
-    k = 0 if top_k is None else _operand(fn, "top_k", top_k, i32, rows, dev)[0]
-    tp = 0 if top_p is None else _operand(fn, "top_p", top_p, f32, rows, dev)[0]
-    mp = 0 if min_p is None else _operand(fn, "min_p", min_p, f32, rows, dev)[0]
-    rc = load().sifar_sample(
+    rows = shape[:1]
+    x, x_stride = _operand(fn, "logits", logits, logits.dtype, shape, dev)
+    u, _ = _operand(fn, "uniform", uniform, _F32, rows, dev)
+    o, _ = _operand(fn, "out", out, _I32, rows, dev)
+    ws, _ = _operand(fn, "workspace", workspace, _U8, workspace.shape[:1], dev)
+    p = 0 if probs is None else _operand(fn, "probs", probs, _F32, rows, dev)[0]
+    t = 0 if temperature is None else _operand(fn, "temperature", temperature, _F32, rows, dev)[0]
+    k = 0 if top_k is None else _operand(fn, "top_k", top_k, _I32, rows, dev)[0]
+    tp = 0 if top_p is None else _operand(fn, "top_p", top_p, _F32, rows, dev)[0]
+    mp = 0 if min_p is None else _operand(fn, "min_p", min_p, _F32, rows, dev)[0]
+    rc = (_lib or load()).sifar_sample(
         _SAMPLE.pack(_dtype(fn, logits.dtype), T, V, x, x_stride, u, t, k, tp, mp, o, p, ws,
-                     workspace.shape[0]), _stream(stream))
+                     workspace.shape[0]), _row_stream(stream, dev))
     if rc:
         _check(fn, rc)
 

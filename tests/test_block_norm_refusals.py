@@ -109,7 +109,7 @@ def recorder(monkeypatch):
     r = Recorder()
     monkeypatch.setattr(S, "_lib", r)
     monkeypatch.setattr(S, "_gpu", lambda fn, name, t: -1)   # a host tensor's device
-    monkeypatch.setattr(S, "_current_stream", lambda: 0)
+    monkeypatch.setattr(S, "_row_stream", lambda stream, dev: 0)
     return r
 
 
