@@ -5,8 +5,7 @@
 // interpolates (2^f - 1) / f at Chebyshev nodes; its degree sets the error
 // (tests/test_exp2.py measures both against 80-bit arithmetic). f = 0 gives 1
 // exactly. One fma per degree: on gfx950 a 64-bit fma issues at the rate of an
-// unpacked 32-bit one. Rounding to i and scaling by 2^i are additions to the bits:
-// the conversions and ldexp that they replace issue at a fraction of that rate.
+// unpacked 32-bit one. Rounding to i and scaling by 2^i are additions to the bits.
 // Outside the stated ranges the result is garbage, but nothing traps.
 #pragma once
 
@@ -23,12 +22,18 @@ namespace sifar {
 // i in the low bits, for |t| below 2^31.
 SIFAR_HD double exp2_magic(double t) { return t + 0x1.8p52; }
 
+SIFAR_HD uint32_t exp2_whole(double magic) {
+    uint64_t bits;
+    __builtin_memcpy(&bits, &magic, 8);
+    return static_cast<uint32_t>(bits);
+}
+
 // q * 2^i, where exponents stay in range.
-SIFAR_HD double exp2_scale(double q, double magic) {
-    uint64_t bits, shift;
+SIFAR_HD double exp2_scale(double q, uint32_t i) {
+    uint64_t bits;
     __builtin_memcpy(&bits, &q, 8);
-    __builtin_memcpy(&shift, &magic, 8);
-    bits += static_cast<uint64_t>(static_cast<uint32_t>(shift) << 20) << 32;
+    const uint32_t high = static_cast<uint32_t>(bits >> 32) + (i << 20);
+    bits = (static_cast<uint64_t>(high) << 32) | static_cast<uint32_t>(bits);
     __builtin_memcpy(&q, &bits, 8);
     return q;
 }
@@ -48,16 +53,18 @@ SIFAR_HD double exp2_64(double t) {
     q = __builtin_fma(q, f, 0x1.c6b08d704a0c2p-5);
     q = __builtin_fma(q, f, 0x1.ebfbdff82c598p-3);
     q = __builtin_fma(q, f, 0x1.62e42fefa39efp-1);
-    return exp2_scale(__builtin_fma(q, f, 1.0), m);
+    return exp2_scale(__builtin_fma(q, f, 1.0), exp2_whole(m));
 }
 
-// 2^(t + BITS) for t in [-1000, 0], relative error below 4e-14: for sums in units of
-// 2^-42.
+// 2^(y c + BITS) for y c in [-1000, 0], relative error below 4e-14: for sums in
+// units of 2^-42. Below 2^-900 where it is not kept: one select, of the exponent, does
+// for both words (each further one from a comparison costs gfx950 four times the
+// first).
 template <int BITS>
-SIFAR_HD double exp2_quick(double t) {
+SIFAR_HD double exp2_quick(double y, double c, bool keep = true) {
     constexpr double s = static_cast<double>(1ull << BITS);
-    const double m = exp2_magic(t);
-    const double f = t - (m - 0x1.8p52);
+    const double m = __builtin_fma(y, c, 0x1.8p52);
+    const double f = __builtin_fma(y, c, 0x1.8p52 - m);
     double q = 0x1.b638808675ca6p-24 * s;
     q = __builtin_fma(q, f, 0x1.63d136355f669p-20 * s);
     q = __builtin_fma(q, f, 0x1.ffcb9515c8f1ap-17 * s);
@@ -67,7 +74,7 @@ SIFAR_HD double exp2_quick(double t) {
     q = __builtin_fma(q, f, 0x1.c6b08d7047e52p-5 * s);
     q = __builtin_fma(q, f, 0x1.ebfbdff823cedp-3 * s);
     q = __builtin_fma(q, f, 0x1.62e42fefa39efp-1 * s);
-    return exp2_scale(__builtin_fma(q, f, s), m);
+    return exp2_scale(__builtin_fma(q, f, s), keep ? exp2_whole(m) : 0u - 1000u);
 }
 
 }  // namespace sifar

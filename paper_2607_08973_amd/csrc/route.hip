@@ -227,10 +227,12 @@ __global__ void __launch_bounds__(kRowWave *kWaves) route_kernel(const RouteArgs
         for (int i = 0; i < a.topk; ++i) {
             const uint32_t best = wave_max(key[0]);
             found = lane == i ? best : found;
-            const bool taken = key[0] == best;
+            if (key[0] == best) {
+                stay_branch();
 #pragma unroll
-            for (int j = 0; j + 1 < EPL; ++j) key[j] = choose(taken, key[j + 1], key[j]);
-            key[EPL - 1] = taken ? 0u : key[EPL - 1];
+                for (int j = 0; j + 1 < EPL; ++j) key[j] = key[j + 1];
+                key[EPL - 1] = 0;
+            }
         }
         if (found) {
             id = static_cast<int>(kIndexMask - (found & kIndexMask));
@@ -297,12 +299,15 @@ __global__ void __launch_bounds__(kRowWave *kWaves) route_kernel(const RouteArgs
             const uint32_t low = lane_value(lo[0], __builtin_ctzll(who));
             found_hi = lane == i ? best : found_hi;
             found_lo = lane == i ? low : found_lo;
+            if (taken) {
+                stay_branch();
 #pragma unroll
-            for (int j = 0; j + 1 < EPL; ++j) {
-                hi[j] = choose(taken, hi[j + 1], hi[j]);
-                lo[j] = choose(taken, lo[j + 1], lo[j]);
+                for (int j = 0; j + 1 < EPL; ++j) {
+                    hi[j] = hi[j + 1];
+                    lo[j] = lo[j + 1];
+                }
+                hi[EPL - 1] = 0;
             }
-            hi[EPL - 1] = taken ? 0u : hi[EPL - 1];
         }
         if constexpr (RANKED) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (found_hi) {

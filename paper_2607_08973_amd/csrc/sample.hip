@@ -36,6 +36,7 @@ constexpr int kNucleus = 64;                   // maxima a nucleus is first soug
 constexpr int kNucleusMass = 24;               // most p * sum / largest weight of such a row
 constexpr int kPerBit = 64;                    // bins of a halving of the weight
 constexpr int kUnitBits = 42;                  // a weight of 1 in units
+constexpr uint64_t kUnitBase = 0x433ull << 52;  // the bits of 2^52: units are its last place
 constexpr double kLog2e = 1.4426950408889634;
 constexpr double kLn2 = 0.6931471805599453;
 constexpr double kCut = 60.0;                  // weights below 2^-60 are 0
@@ -238,11 +239,20 @@ __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const Sample
         if (m < __builtin_inff()) {
             const double max = static_cast<double>(m);
             const float least = max32(static_cast<float>(max - kCut * kLn2 * tau), kLowest);
+            if ((static_cast<double>(least) - max) * scale < 1.0 - kCut) {
+                // what is below the cut, or not there, counts 2^-60: no more than 2^-51 of
+                // the chunk's weight together, and cheaper than leaving it out
 #pragma unroll
-            for (int i = 0; i < kVec<D>; ++i) {
-                const float l = logit<D>(x[b], i);
-                const double w = exp2_quick<0>((static_cast<double>(l) - max) * scale);
-                sum[b] += l >= least ? w : 0.0;
+                for (int i = 0; i < kVec<D>; ++i)
+                    sum[b] += exp2_quick<0>(
+                        static_cast<double>(max32(logit<D>(x[b], i), least)) - max, scale);
+            } else {  // a temperature or a maximum for which no logit lies at the cut
+#pragma unroll
+                for (int i = 0; i < kVec<D>; ++i) {
+                    const float l = logit<D>(x[b], i);
+                    sum[b] += exp2_quick<0>(static_cast<double>(max32(l, least)) - max, scale,
+                                            l >= least);
+                }
             }
         } else {  // they share the weight
 #pragma unroll
@@ -250,7 +260,7 @@ __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const Sample
         }
     }
     const double all = wave_reduce4(sum, Add{});
-    if (writes) n.mass[t * n.chunks + c] = all;
+    if (writes) n.mass[t * n.chunks + c] = mine > -__builtin_inff() ? all : 0.0;
 }
 
 // ---- pick_kernel -----------------------------------------------------------------
@@ -348,15 +358,15 @@ struct Row {
     float one;            // logits below it weigh one unit
     bool finite;          // the maximum is; otherwise the infinite logits share the weight
 
-    // A weight in units. (Garbage for logits below the cut.)
-    __device__ __forceinline__ uint64_t units_near(float x) const {
-        const double w = exp2_quick<kUnitBits>((static_cast<double>(x) - max64) * scale);
-        return __builtin_bit_cast(uint64_t, w + 0x1p52) & ((uint64_t{1} << 52) - 1);
+    // A weight in units above kUnitBase. (Garbage for logits below the cut.)
+    __device__ __forceinline__ uint64_t units_near(float x, bool keep = true) const {
+        const double w = exp2_quick<kUnitBits>(static_cast<double>(x) - max64, scale, keep);
+        return __builtin_bit_cast(uint64_t, w + 0x1p52);
     }
     // Of a kept weight at least one, so that what may be drawn can be.
     __device__ __forceinline__ uint64_t units(uint32_t key) const {
         const float x = value_of(key);
-        const uint64_t u = x >= one ? units_near(x) : 1;
+        const uint64_t u = x >= one ? units_near(x) - kUnitBase : 1;
         return finite ? u : uint64_t{1} << kUnitBits;
     }
 };
@@ -464,11 +474,37 @@ struct InList {
     }
 };
 
-__device__ __forceinline__ void to_list(Shared &s, uint32_t key, int at) {
-    const uint32_t i = atomicAdd(&s.list_size, 1u);
-    if (i < kList) {
-        s.list_key[i] = key;
-        s.list_at[i] = static_cast<uint32_t>(at);
+// The logits of a lane in chunk c that lie in [low, high], into the list, in no order:
+// one counter's addition and wait for the whole chunk.
+template <int D>
+__device__ __forceinline__ void to_list(Shared &s, const Raw &x, int c, float low, float high) {
+    const int lane = threadIdx.x & 63;
+    uint64_t in[kVec<D>], any = 0;
+    uint32_t count = 0;
+#pragma unroll
+    for (int i = 0; i < kVec<D>; ++i) {
+        in[i] = __ballot(logit<D>(x, i) >= low && logit<D>(x, i) <= high);
+        any |= in[i];
+    }
+    if (!any) return;
+#pragma unroll
+    for (int i = 0; i < kVec<D>; ++i) count += static_cast<uint32_t>(__builtin_popcountll(in[i]));
+    uint32_t at = 0;
+    if (lane == 0) at = atomicAdd(&s.list_size, count);
+    at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+    for (int i = 0; i < kVec<D>; ++i) {
+        if (in[i] >> lane & 1) {
+            const uint32_t place =
+                at + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(in[i] >> 32),
+                                               __builtin_amdgcn_mbcnt_lo(
+                                                   static_cast<uint32_t>(in[i]), 0));
+            if (place < kList) {
+                s.list_key[place] = key_of(logit<D>(x, i));
+                s.list_at[place] = static_cast<uint32_t>(c * kChunkOf<D> + lane * kVec<D> + i);
+            }
+        }
+        at += static_cast<uint32_t>(__builtin_popcountll(in[i]));
     }
 }
 
@@ -476,16 +512,11 @@ __device__ __forceinline__ void to_list(Shared &s, uint32_t key, int at) {
 // do not fit.
 template <int D>
 __device__ __forceinline__ bool collect(Shared &s, const Row<D> &r, uint32_t least, uint32_t most) {
-    const int lane = threadIdx.x & 63;
     const float low = value_of(least), high = value_of(most);
     if (threadIdx.x == 0) s.list_size = 0;  // queue_chunks() waits
     const uint32_t size = queue_chunks(s, r.chunks, least);
     each_batch(s, r, size, [&](const Raw &x, int c) {
-#pragma unroll
-        for (int i = 0; i < kVec<D>; ++i) {
-            const float l = logit<D>(x, i);
-            if (l >= low && l <= high) to_list(s, key_of(l), c * kChunkOf<D> + lane * kVec<D> + i);
-        }
+        to_list<D>(s, x, c, low, high);
         return uint64_t{0};
     }, [](uint64_t, int) {});
     __syncthreads();
@@ -717,16 +748,15 @@ __device__ __forceinline__ bool window(Shared &s, const Row<D> &r, float part, u
     const float high = value_of(above), low = value_of(least);
     if (threadIdx.x == 0) s.list_size = 0;
     const uint32_t again = queue_chunks(s, r.chunks, least);
-    const int lane = threadIdx.x & 63;
     each_batch(s, r, again, [&](const Raw &x, int c) {
+        to_list<D>(s, x, c, low, high);
         uint64_t sum = 0;
 #pragma unroll
         for (int i = 0; i < kVec<D>; ++i) {
             const float l = logit<D>(x, i);
-            const uint64_t u = r.units_near(l);
-            sum += l > high ? u : 0;
-            if (l >= low && l <= high) to_list(s, key_of(l), c * kChunkOf<D> + lane * kVec<D> + i);
+            sum += r.units_near(max32(l, high), l > high);
         }
+        sum -= kVec<D> * kUnitBase;  // modulo 2^64
         return sum;
     }, [&](uint64_t sum, int c) { s.chunk_units[c] = sum; });
     __syncthreads();
