@@ -313,11 +313,13 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t x) {
     return x;
 }
 
-// Exclusive sum over the workgroup's threads, and the whole sum.
+// Exclusive sum over the workgroup's threads, and the whole sum. FRESH: a barrier lies
+// between this call and the one before, whose sums may otherwise still be read.
+template <bool FRESH = false>
 __device__ __forceinline__ uint64_t block_scan(Shared &s, uint64_t x, uint64_t &total) {
     const int wave = threadIdx.x >> 6;
     const uint64_t inc = wave_scan(x);
-    __syncthreads();  // wave_sum may still be read from the call before
+    if constexpr (!FRESH) __syncthreads();
     if ((threadIdx.x & 63) == 63) s.wave_sum[wave] = inc;
     __syncthreads();
     uint64_t before = 0;
@@ -331,20 +333,20 @@ __device__ __forceinline__ uint64_t block_scan(Shared &s, uint64_t x, uint64_t &
     return before + inc - x;
 }
 
+template <bool FRESH = false>
 __device__ __forceinline__ uint64_t block_sum(Shared &s, uint64_t x) {
     uint64_t total;
-    block_scan(s, x, total);
+    block_scan<FRESH>(s, x, total);
     return total;
 }
 
-__device__ __forceinline__ uint32_t block_max(Shared &s, uint32_t x) {
+__device__ __forceinline__ uint32_t block_max(Shared &s, uint32_t x) {  // called once
     x = wave_reduce(x, Max{});
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) s.wave_max[threadIdx.x >> 6] = x;
     __syncthreads();
     uint32_t m = 0;
 #pragma unroll
-    for (int w = 0; w < kPickWaves; ++w) m = s.wave_max[w] > m ? s.wave_max[w] : m;
+    for (int w = 0; w < kPickWaves; ++w) m = choose(s.wave_max[w] > m, s.wave_max[w], m);
     return m;
 }
 
@@ -373,7 +375,7 @@ struct Row {
 
 // The chunks whose maximum reaches `least`, in no order.
 __device__ __forceinline__ uint32_t queue_chunks(Shared &s, int chunks, uint32_t least) {
-    __syncthreads();
+    // every thread has read the size of the queue before, and a barrier has passed since
     if (threadIdx.x == 0) s.queue_size = 0;
     __syncthreads();
     for (int c = threadIdx.x; c < chunks; c += kThreads)
@@ -494,7 +496,8 @@ __device__ __forceinline__ void to_list(Shared &s, const Raw &x, int c, float lo
     at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
     for (int i = 0; i < kVec<D>; ++i) {
-        if (in[i] >> lane & 1) {
+        if (!in[i]) continue;  // the same in every lane
+        if (logit<D>(x, i) >= low && logit<D>(x, i) <= high) {
             const uint32_t place =
                 at + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(in[i] >> 32),
                                                __builtin_amdgcn_mbcnt_lo(
@@ -533,7 +536,7 @@ __device__ __forceinline__ bool find_bin(Shared &s, const B *hist, int bins, uin
     const int b = 2 * threadIdx.x;
     const uint64_t v0 = b < bins ? hist[b] : 0, v1 = b + 1 < bins ? hist[b + 1] : 0;
     uint64_t total;
-    const uint64_t run = block_scan(s, v0 + v1, total);
+    const uint64_t run = block_scan<true>(s, v0 + v1, total);
     if (total < target) return false;  // the same in every thread
     if (run < target && target <= run + v0 + v1) {
         const bool second = target > run + v0;
@@ -816,7 +819,7 @@ __device__ __forceinline__ void draw_small(Shared &s, const Row<D> &r, const Dra
     bool in = tid < n && (d.top_k <= 0 || tid < d.top_k);
     if (d.top_p < 1.0f) {
         uint64_t top_units;
-        const uint64_t before = block_scan(s, in ? w : 0, top_units);
+        const uint64_t before = block_scan<true>(s, in ? w : 0, top_units);
         in = in && before < share(d.top_p, d.top_k > 0 ? top_units : units);
     }
     in = in && (key >= least || tid == 0);
@@ -875,6 +878,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
         s.chosen_at = 0;
         s.chosen_ties = 0;
     }
+    for (int b = tid; b < kBins; b += kThreads) s.hist[b] = 0;
     const uint32_t top = block_max(s, my_key);
     if (top == 0) {  // nothing is there
         if (tid == 0) {
@@ -936,7 +940,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
             if (plain) s.chunk_units[c] = units;
             mine += units;
         }
-        if (!plain) row_units = block_sum(s, mine);
+        if (!plain) row_units = block_sum<true>(s, mine);
     }
     if (!plain) {
         // First the candidates above a bound that is known: min-p's, or (to a bin) the
@@ -951,8 +955,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
             static_cast<double>(d.top_p) * static_cast<double>(row_units) >
                 static_cast<double>(kNucleusMass) * __builtin_ldexp(1.0, kUnitBits);
         if ((by_k || (by_p && !wide)) && rank < groups) {
-            clear_bins(s);
-            if (tid < groups) add(s.hist[far_bin(top - my_key)], 1);
+            if (tid < groups) add(s.hist[far_bin(top - my_key)], 1);  // cleared above
             uint32_t bin;
             uint64_t unused;
             find_bin(s, s.hist, kBins, static_cast<uint64_t>(rank), bin, unused);
@@ -1019,7 +1022,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     if (!plain) {
         for (int c = c0; c < c1; ++c) ties += s.chunk_ties[c];
         uint64_t tied;
-        ties_before = block_scan(s, ties, tied);
+        ties_before = block_scan<true>(s, ties, tied);  // behind the barrier above
     }
     uint64_t units = 0, run_ties = ties_before;
     for (int c = c0; c < c1; ++c) {
