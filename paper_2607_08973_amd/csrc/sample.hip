@@ -322,15 +322,17 @@ __device__ __forceinline__ uint64_t block_scan(Shared &s, uint64_t x, uint64_t &
     if constexpr (!FRESH) __syncthreads();
     if ((threadIdx.x & 63) == 63) s.wave_sum[wave] = inc;
     __syncthreads();
-    uint64_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kPickWaves; ++w) {
-        const uint64_t v = s.wave_sum[w];
-        before += w < wave ? v : 0;
-        total += v;
-    }
-    return before + inc - x;
+    // the waves' sums, scanned by the 16 lanes of a row at once
+    static_assert(kPickWaves == 16, "a row of lanes");
+    uint64_t sums = s.wave_sum[threadIdx.x & 15];
+    sums = add_from<0x111, 0xF>(sums);
+    sums = add_from<0x112, 0xF>(sums);
+    sums = add_from<0x114, 0xF>(sums);
+    sums = add_from<0x118, 0xF>(sums);
+    total = lane_value(sums, 15);
+    const uint64_t through = lane_value(sums, __builtin_amdgcn_readfirstlane(wave));
+    const uint64_t mine = lane_value(inc, 63);
+    return through - mine + inc - x;
 }
 
 template <bool FRESH = false>
@@ -344,10 +346,8 @@ __device__ __forceinline__ uint32_t block_max(Shared &s, uint32_t x) {  // calle
     x = wave_reduce(x, Max{});
     if ((threadIdx.x & 63) == 0) s.wave_max[threadIdx.x >> 6] = x;
     __syncthreads();
-    uint32_t m = 0;
-#pragma unroll
-    for (int w = 0; w < kPickWaves; ++w) m = choose(s.wave_max[w] > m, s.wave_max[w], m);
-    return m;
+    return __builtin_amdgcn_readfirstlane(
+        wave_reduce<kPickWaves>(s.wave_max[threadIdx.x & (kPickWaves - 1)], Max{}));
 }
 
 // A row in pick_kernel.
@@ -367,9 +367,10 @@ struct Row {
     }
     // Of a kept weight at least one, so that what may be drawn can be.
     __device__ __forceinline__ uint64_t units(uint32_t key) const {
+        if (!finite) return uint64_t{1} << kUnitBits;  // the same in every lane
         const float x = value_of(key);
-        const uint64_t u = x >= one ? units_near(x) - kUnitBase : 1;
-        return finite ? u : uint64_t{1} << kUnitBits;
+        const uint64_t u = units_near(max32(x, one), x >= one) - kUnitBase;
+        return u | (x >= one ? 0 : 1);
     }
 };
 
