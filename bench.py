@@ -192,7 +192,8 @@ def parse():
     ap.add_argument("--floor-nodes", type=int, default=64)
     ap.add_argument("--workload", default="llama8b-decode",
                     choices=["llama8b-decode", "smoke-n2", "spec-stress", "sweep", "moe-rmsnorm",
-                             "ablation", "retry-curve", "reduce-cold", "litmus", "misspec-vs-tp"],
+                             "ablation", "retry-curve", "reduce-cold", "litmus", "misspec-vs-tp",
+                             "row-ops"],
                     help="llama8b-decode is the headline line; the others print one "
                          "JSON line per configuration")
     ap.add_argument("--wpg", type=int, default=1, choices=[1, 2, 4, 8, 16],
@@ -547,6 +548,68 @@ def torch_sum_reference(w, scrub, reps=30):
     return res
 
 
+def row_ops_points(reps=20):
+    """The row operators of a decode step (sifar_block_norm, sifar_route, sifar_sample) at
+    decode batches and a prefill's, each as a captured graph of `reps` calls: microseconds
+    per call, launches included, and the rate of the bytes a call has to move."""
+    import torch
+
+    import paper_2607_08973_amd as S
+
+    def timed(call):
+        call()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(reps):
+                call()
+        g.replay()
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(10):
+            g.replay()
+        b.record()
+        torch.cuda.synchronize()
+        return a.elapsed_time(b) * 1e3 / (10 * reps)
+
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(260708973)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda:0")
+    bf16 = lambda *s: rand(*s).to(torch.bfloat16)
+    N, H, E, K, V = 8, 8192, 256, 8, 128256
+    for T in (1, 8, 64, 512, 4096):
+        res, out, y = bf16(T, H), bf16(T, H), bf16(T, H)
+        post, norm, gate = bf16(H), bf16(H), bf16(H)
+        for parts in (1, N) if T <= 512 else (1,):
+            x = bf16(parts, T, H)
+            us = timed(lambda: S.sifar_block_norm(x, res, out, post, gate, norm, y))
+            yield {"op": "block_norm", "tokens": T, "hidden": H, "parts": parts,
+                   "us_per_call": us, "bytes": (parts + 3) * T * H * 2 + 3 * H * 2}
+        logits, bias = rand(T, E), 0.1 * rand(E)
+        ids = torch.empty((T, K), dtype=torch.int32, device="cuda:0")
+        w = torch.empty((T, K), device="cuda:0")
+        for name, kw in (("route-softmax", dict()),
+                         ("route-sigmoid-bias-groups", dict(score="sigmoid", bias=bias, groups=8,
+                                                            top_groups=4, group_top=2))):
+            us = timed(lambda: S.sifar_route(logits, ids, w, **kw))
+            yield {"op": name, "tokens": T, "experts": E, "topk": K, "us_per_call": us,
+                   "bytes": T * E * 4 + T * K * 8}
+        if T > 512:
+            continue
+        logits = 2.5 * rand(T, V)
+        u = torch.rand((T,), generator=gen, device="cuda:0")
+        tok = torch.empty((T,), dtype=torch.int32, device="cuda:0")
+        ws = torch.empty(S.sifar_sample_workspace(T, V), dtype=torch.uint8, device="cuda:0")
+        k = torch.full((T,), 50, dtype=torch.int32, device="cuda:0")
+        p = torch.full((T,), 0.9, device="cuda:0")
+        zero = torch.zeros((T,), device="cuda:0")
+        for name, kw in (("sample-greedy", dict(temperature=zero)), ("sample", dict()),
+                         ("sample-top-k", dict(top_k=k)), ("sample-top-p", dict(top_p=p)),
+                         ("sample-top-k-top-p", dict(top_k=k, top_p=p))):
+            us = timed(lambda: S.sifar_sample(logits, u, tok, ws, **kw))
+            yield {"op": name, "tokens": T, "vocab": V, "us_per_call": us, "bytes": T * V * 4}
+
+
 def suite(args):
     """Secondary workloads: one JSON line each (not the headline metric)."""
     import synth
@@ -559,6 +622,13 @@ def suite(args):
         for p in pts:
             print(json.dumps({k: (round(v, 4) if isinstance(v, float) else v)
                               for k, v in p.items()}), flush=True)
+        return
+    if args.workload == "row-ops":
+        for p in row_ops_points():
+            p["gbs"] = p["bytes"] / p["us_per_call"] / 1e3
+            print(json.dumps({"workload": "row-ops", **{
+                k: (round(v, 3) if isinstance(v, float) else v) for k, v in p.items()}}),
+                flush=True)
         return
     if args.workload == "litmus":
         # the handoff litmus (sifar_litmus): both reader orders, producer and

@@ -72,24 +72,34 @@ __global__ void __launch_bounds__(kMaxThreads) block_norm_kernel(const NormArgs 
         if (gated) gate[v] = load8<D>(a.gate, t * a.gate_stride + h[v]);
         if (added) res[v] = load8<R>(a.residual, t * a.residual_stride + h[v]);
     }
-    // The other partials, as many in flight as registers allow: one after the other
-    // each would cost a memory round trip.
+    // The other partials, up to seven in flight: one after the other each would cost a
+    // memory round trip. (Long rows have enough vectors of one partial for that.)
     constexpr int FLIGHT = V == 1 ? kMaxParts - 1 : V == 2 ? 2 : 1;
     for (int p = 1; p < a.parts; p += FLIGHT) {
-        Eight<D> e[FLIGHT][V];
+        if constexpr (AHEAD) {
+            Eight<D> e[FLIGHT][V];
 #pragma unroll
-        for (int q = 0; q < FLIGHT; ++q)
+            for (int q = 0; q < FLIGHT; ++q)
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (p + q < a.parts && on[v])
-                    e[q][v] = load8<D>(a.x, (p + q) * a.part_stride + t * a.x_stride + h[v]);
+                for (int v = 0; v < V; ++v)
+                    if (p + q < a.parts && on[v])
+                        e[q][v] = load8<D>(a.x, (p + q) * a.part_stride + t * a.x_stride + h[v]);
 #pragma unroll
-        for (int q = 0; q < FLIGHT; ++q)
+            for (int q = 0; q < FLIGHT; ++q)
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (p + q < a.parts && on[v])
+                for (int v = 0; v < V; ++v)
+                    if (p + q < a.parts && on[v])
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) f[v][i] += element<D>(e[q][v], i);
+                        for (int i = 0; i < 8; ++i) f[v][i] += element<D>(e[q][v], i);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (!on[v]) continue;
+                const Eight<D> e = load8<D>(a.x, p * a.part_stride + t * a.x_stride + h[v]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[v][i] += element<D>(e, i);
+            }
+        }
     }
     float inv = 1.f;
     if (posted) {
