@@ -658,7 +658,8 @@ int sifar_route(const sifar_route_args *a, void *stream);
  *
  * Limits: 1 <= vocab <= SIFAR_SAMPLE_MAX_VOCAB; 0 <= tokens <=
  * SIFAR_ROWS_MAX_TOKENS; pointers aligned to their elements. Outputs and
- * workspace that overlap each other or an input are refused. Two launches. */
+ * workspace that overlap each other or an input are refused. Two launches; with
+ * top_p and no top_k, up to 64 rows of 65536 logits or more take four. */
 #define SIFAR_SAMPLE_MAX_VOCAB 1048576
 typedef struct {
     int32_t dtype;
@@ -678,7 +679,8 @@ typedef struct {
 } sifar_sample_args;
 int sifar_sample(const sifar_sample_args *a, void *stream);
 
-/* Bytes of workspace that sifar_sample needs, or SIFAR_EINVAL. */
+/* Bytes of workspace that sifar_sample needs, or SIFAR_EINVAL. Never less for more
+ * tokens or a larger vocabulary: a workspace for the largest batch serves all. */
 int64_t sifar_sample_workspace(int32_t tokens, int32_t vocab);
 
 #ifdef __cplusplus

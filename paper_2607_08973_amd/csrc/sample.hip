@@ -5,7 +5,10 @@
 // 16 bytes of each of a wave's lanes), the maximum and, where the row needs it,
 // the weights' sum. pick_kernel, a workgroup a row, finds the threshold of top-k,
 // top-p and min-p and walks to the token in index order, reading again only
-// chunks whose maximum says that they hold something to keep.
+// chunks whose maximum says that they hold something to keep. A nucleus of many
+// tokens takes two more passes over its row, which a workgroup makes in 63 us for
+// 128256 logits; where few rows would leave the GPU idle meanwhile, two launches
+// between spread them over several workgroups a row.
 //
 // Weights w = 2^((x - max) log2(e) / temperature) are 64-bit values rounded to
 // units of 2^-42 and added as integers: sums do not depend on the order of
@@ -32,9 +35,15 @@ constexpr int kMaxChunks = SIFAR_SAMPLE_MAX_VOCAB / kLeastChunk;
 constexpr int kBins = 64 + 26 * 64;            // log-linear bins of a 32-bit distance
 constexpr int kList = 4096;                    // candidates kept in LDS
 constexpr int kSmall = 256;                    // most candidates that are ranked by counting
-constexpr int kNucleus = 64;                   // maxima a nucleus is first sought above
-constexpr int kNucleusMass = 24;               // most p * sum / largest weight of such a row
 constexpr int kPerBit = 64;                    // bins of a halving of the weight
+// Passes over rows are spread for up to 64 rows of 65536 logits or more. 1 x 128256: a
+// wide nucleus took 69 us in one workgroup and takes 40, a narrow one, for which the
+// two launches find nothing to do, 16 and 20; 64 x 128256: 82 and 63. At 32768 logits a
+// workgroup needs 33 us for a wide nucleus, the four launches 38; 65 x 128256 would
+// leave a workgroup as much as it has now.
+constexpr int kSpreadRows = 64;
+constexpr int kSpreadVocab = 65536;
+constexpr int kSpreadGroups = 256;             // workgroups of a spread launch: one a CU
 constexpr int kUnitBits = 42;                  // a weight of 1 in units
 constexpr uint64_t kUnitBase = 0x433ull << 52;  // the bits of 2^52: units are its last place
 constexpr double kLog2e = 1.4426950408889634;
@@ -46,7 +55,13 @@ struct SampleArgs {
     sifar_sample_args a;
     int32_t chunks;  // of a row
     double *mass;    // [tokens][chunks] sums of weights relative to the chunk's maximum
+    uint64_t *units; // [tokens][chunks], of what lies above a spread row's window
     float *max;      // [tokens][chunks]
+    // spread rows, or null
+    uint32_t *hist;  // [tokens][kBins]
+    uint32_t *listed;                // [tokens] candidates in the window,
+    uint32_t *list_key, *list_at;    // [tokens][kList]
+    int32_t groups;  // workgroups of a row
 };
 
 // Order-preserving 32 bits of a number. -0 counts as 0.
@@ -212,6 +227,11 @@ __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const Sample
     const int64_t t = blockIdx.x;
     const int lane = threadIdx.x;
     const int first = (blockIdx.y * kScanWaves + threadIdx.y) * kBatch;
+    if (n.hist && blockIdx.y == 0) {  // for the launches behind this one
+        for (int b = threadIdx.y * kRowWave + lane; b < kBins; b += kScanWaves * kRowWave)
+            n.hist[t * kBins + b] = 0;
+        if (threadIdx.y == 0 && lane == 0) n.listed[t] = 0;
+    }
     if (first >= n.chunks) return;
     const Draw d = draw_of(a, t);
     const Stored<D> *row = static_cast<const Stored<D> *>(a.logits) + t * a.logits_stride;
@@ -374,12 +394,17 @@ struct Row {
     }
 };
 
+// A row's chunks, or some of them.
+struct Span {
+    int first, end;
+};
+
 // The chunks whose maximum reaches `least`, in no order.
-__device__ __forceinline__ uint32_t queue_chunks(Shared &s, int chunks, uint32_t least) {
+__device__ __forceinline__ uint32_t queue_chunks(Shared &s, Span span, uint32_t least) {
     // every thread has read the size of the queue before, and a barrier has passed since
     if (threadIdx.x == 0) s.queue_size = 0;
     __syncthreads();
-    for (int c = threadIdx.x; c < chunks; c += kThreads)
+    for (int c = span.first + threadIdx.x; c < span.end; c += kThreads)
         if (s.chunk_key[c] >= least) s.queue[atomicAdd(&s.queue_size, 1u)] = c;
     __syncthreads();
     return s.queue_size;
@@ -453,7 +478,7 @@ struct InRow {
     __device__ __forceinline__ void each(uint32_t least, F f) const {
         const int lane = threadIdx.x & 63;
         const float low = value_of(least);
-        const uint32_t size = queue_chunks(s, r.chunks, least);
+        const uint32_t size = queue_chunks(s, Span{0, r.chunks}, least);
         for (uint32_t q = threadIdx.x >> 6; q < size; q += kPickWaves) {
             const int c = __builtin_amdgcn_readfirstlane(s.queue[q]);
             const Raw x = load_chunk<D>(r.logits, r.vocab, c, lane);
@@ -518,7 +543,7 @@ template <int D>
 __device__ __forceinline__ bool collect(Shared &s, const Row<D> &r, uint32_t least, uint32_t most) {
     const float low = value_of(least), high = value_of(most);
     if (threadIdx.x == 0) s.list_size = 0;  // queue_chunks() waits
-    const uint32_t size = queue_chunks(s, r.chunks, least);
+    const uint32_t size = queue_chunks(s, Span{0, r.chunks}, least);
     each_batch(s, r, size, [&](const Raw &x, int c) {
         to_list<D>(s, x, c, low, high);
         return uint64_t{0};
@@ -711,18 +736,23 @@ __device__ __forceinline__ Keep filter(Shared &s, const From &from, const Row<D>
 
 // A nucleus of more tokens than the list holds. Sums in 32 bits give a window of
 // logits that holds its border; one pass over the row then adds up, exactly, what
-// lies above the window, chunk by chunk, and lists what lies inside. False where
-// the window misses or does not fit: then nothing is decided.
+// lies above the window, chunk by chunk, and lists what lies inside.
+
+// The two passes are bounded where temperature and maximum are ordinary.
 template <int D>
-__device__ __forceinline__ bool window(Shared &s, const Row<D> &r, float part, uint32_t top,
-                                       uint64_t units, Keep &keep) {
-    if (!r.finite || !(r.scale > 1e-30 && r.scale < 1e30)) return false;
-    const float cut = value_of(keep.key), scale = static_cast<float>(r.scale);
-    // the whole row comes to 2^31
+__device__ __forceinline__ bool window_fits(const Row<D> &r) {
+    return r.finite && r.scale > 1e-30 && r.scale < 1e30;
+}
+
+// First pass, over some chunks: the histogram, in LDS, cleared before. The whole row
+// comes to 2^31.
+template <int D>
+__device__ __forceinline__ void window_bins(Shared &s, const Row<D> &r, Span span, uint32_t cut_key,
+                                            uint64_t units) {
+    const float cut = value_of(cut_key), scale = static_cast<float>(r.scale);
     const float unit = static_cast<float>(0x1p73 / static_cast<double>(units));
     uint32_t *hist = reinterpret_cast<uint32_t *>(s.hist);
-    clear_bins(s);
-    const uint32_t size = queue_chunks(s, r.chunks, keep.key);
+    const uint32_t size = queue_chunks(s, span, cut_key);
     each_batch(s, r, size, [&](const Raw &x, int) {
 #pragma unroll
         for (int i = 0; i < kVec<D>; ++i) {
@@ -734,25 +764,45 @@ __device__ __forceinline__ bool window(Shared &s, const Row<D> &r, float part, u
         }
         return uint64_t{0};
     }, [](uint64_t, int) {});
-    // A window of 2^-16 of the row's weight to either side: what rounding and 32-bit
-    // exponentials leave is an order less, unless most of the row weighs next to nothing.
+}
+
+struct Window {
+    bool found;
+    uint32_t above, least;  // keys: what is larger lies above, the border is least or more
+};
+
+// A window of 2^-16 of the row's weight to either side: what rounding and 32-bit
+// exponentials leave is an order less, unless most of the row weighs next to nothing.
+template <int D>
+__device__ __forceinline__ Window window_of(Shared &s, const Row<D> &r, float part, uint32_t top,
+                                            uint32_t cut_key) {
+    const uint32_t *hist = reinterpret_cast<const uint32_t *>(s.hist);
     const double aim = static_cast<double>(part) * 0x1p31;
     uint32_t first, end;
     uint64_t unused;
     if (!find_bin(s, hist, kBins, aim > 0x1p15 + 1.0 ? static_cast<uint64_t>(aim - 0x1p15) : 1,
                   first, unused))
-        return false;
+        return Window{false, 0, 0};
     if (!find_bin(s, hist, kBins, static_cast<uint64_t>(aim + 0x1p15), end, unused) ||
         end >= kBins - 1)
-        return false;
-    const uint32_t above = first ? key_from(r.max64 - first / (kPerBit * r.scale)) : top;
-    uint32_t least = key_from(r.max64 - (end + 1) / (kPerBit * r.scale));
-    if (least < keep.key) least = keep.key;
-    if (least > above || value_of(above) < r.one) return false;
-    const float high = value_of(above), low = value_of(least);
+        return Window{false, 0, 0};
+    Window w;
+    w.above = first ? key_from(r.max64 - first / (kPerBit * r.scale)) : top;
+    w.least = key_from(r.max64 - (end + 1) / (kPerBit * r.scale));
+    if (w.least < cut_key) w.least = cut_key;
+    // weights above the window are more than a unit
+    w.found = w.least <= w.above && value_of(w.above) >= r.one;
+    return w;
+}
+
+// Second pass, over some chunks: s.chunk_units of what lies above, the list of what
+// lies inside.
+template <int D>
+__device__ __forceinline__ void window_sums(Shared &s, const Row<D> &r, Span span, const Window &w) {
+    const float high = value_of(w.above), low = value_of(w.least);
     if (threadIdx.x == 0) s.list_size = 0;
-    const uint32_t again = queue_chunks(s, r.chunks, least);
-    each_batch(s, r, again, [&](const Raw &x, int c) {
+    const uint32_t size = queue_chunks(s, span, w.least);
+    each_batch(s, r, size, [&](const Raw &x, int c) {
         to_list<D>(s, x, c, low, high);
         uint64_t sum = 0;
 #pragma unroll
@@ -764,6 +814,13 @@ __device__ __forceinline__ bool window(Shared &s, const Row<D> &r, float part, u
         return sum;
     }, [&](uint64_t sum, int c) { s.chunk_units[c] = sum; });
     __syncthreads();
+}
+
+// The border, from the sums of every chunk and the list. False where the window misses
+// it or does not fit the list: then nothing is decided.
+template <int D>
+__device__ __forceinline__ bool window_border(Shared &s, const Row<D> &r, float part,
+                                              const Window &w, uint64_t units, Keep &keep) {
     const uint32_t listed = s.list_size;
     uint64_t mine = 0;
     for (int c = threadIdx.x; c < r.chunks; c += kThreads) mine += s.chunk_units[c];
@@ -771,9 +828,9 @@ __device__ __forceinline__ bool window(Shared &s, const Row<D> &r, float part, u
     const uint64_t target = share(part, units);
     if (listed > kList || before >= target) return false;
     const InList list{s, listed};
-    const uint64_t in = kept_units(s, list, r, Keep{least, kAllTies});
+    const uint64_t in = kept_units(s, list, r, Keep{w.least, kAllTies});
     if (before + in < target) return false;
-    keep = reach(s, list, r, above, before, target, Keep{least, kAllTies});
+    keep = reach(s, list, r, w.above, before, target, Keep{w.least, kAllTies});
     return true;
 }
 
@@ -847,40 +904,236 @@ __device__ __forceinline__ void draw_small(Shared &s, const Row<D> &r, const Dra
     }
 }
 
+// What a workgroup knows of its row when it starts.
+template <int D>
+struct Begun {
+    Draw d;
+    Row<D> r;
+    uint32_t top, my_key;  // of the row's maximum (0: nothing is there), of this thread's chunks'
+    int c0, c1;            // a thread's chunks, in index order over the threads
+};
+
+template <int D>
+__device__ __forceinline__ Begun<D> begin_row(Shared &s, const SampleArgs &n, int64_t t) {
+    Begun<D> b;
+    const int tid = threadIdx.x;
+    b.d = draw_of(n.a, t);
+    b.r.logits = static_cast<const Stored<D> *>(n.a.logits) + t * n.a.logits_stride;
+    b.r.vocab = n.a.vocab;
+    b.r.chunks = n.chunks;
+    const int per = (n.chunks + kThreads - 1) / kThreads;
+    b.c0 = tid * per < n.chunks ? tid * per : n.chunks;
+    b.c1 = b.c0 + per < n.chunks ? b.c0 + per : n.chunks;
+    b.my_key = 0;
+    for (int c = b.c0; c < b.c1; ++c) {
+        const float m = n.max[t * n.chunks + c];
+        const uint32_t k = m > -__builtin_inff() ? key_of(m) : 0;
+        s.chunk_key[c] = k;
+        s.chunk_units[c] = 0;
+        s.chunk_ties[c] = 0;
+        b.my_key = k > b.my_key ? k : b.my_key;
+    }
+    for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
+    b.top = block_max(s, b.my_key);
+    b.r.max = value_of(b.top);
+    return b;
+}
+
+// The limits of what a row keeps, and the kinds of rows.
+struct Limits {
+    Keep keep;           // by the cut
+    uint32_t least;      // and min-p
+    bool by_k, by_p;
+    bool plain;          // every weight above the cut is kept: the scan's sums serve
+    uint32_t bound;      // what top-k or top-p keeps is among the keys from here on (0: not known)
+    bool wide;           // a nucleus of many tokens: no such bound
+    bool spread;         // whose passes are launches of their own
+    uint64_t row_units;  // the whole weight, where top-p starts from it
+};
+
+template <int D>
+__device__ __forceinline__ Limits limit_row(Shared &s, const SampleArgs &n, int64_t t, Begun<D> &b) {
+    const Draw &d = b.d;
+    Row<D> &r = b.r;
+    Limits l;
+    r.max64 = static_cast<double>(r.max);
+    r.finite = r.max < __builtin_inff();
+    const double tau = static_cast<double>(d.temperature);
+    r.scale = kLog2e / tau;
+    r.one = value_of(key_from(r.max64 - kUnitBits * kLn2 * tau));
+    l.keep = Keep{r.finite ? key_from(r.max64 - kCut * kLn2 * tau) : b.top, kAllTies};
+    l.least = l.keep.key;
+    // at an infinite temperature every weight is 1
+    if (d.min_p > 0.0f && r.finite && d.temperature < __builtin_inff()) {
+        const double p = d.min_p < 1.0f ? static_cast<double>(d.min_p) : 1.0;
+        const uint32_t k = key_from(p < 1.0 ? r.max64 + log(p) * tau : r.max64);
+        l.least = k > l.least ? k : l.least;
+    }
+    l.by_k = d.top_k > 0;
+    l.by_p = d.top_p < 1.0f;
+    l.plain = !l.by_k && !l.by_p && !(d.min_p > 0.0f);
+    l.row_units = 0;
+    if (l.plain || (l.by_p && !l.by_k)) {
+        uint64_t mine = 0;
+        for (int c = b.c0; c < b.c1; ++c) {
+            if (s.chunk_key[c] < l.keep.key) continue;
+            const double w = exp2_64(log2_weight(value_of(s.chunk_key[c]), r.max, r.scale)) *
+                             n.mass[t * n.chunks + c];
+            uint64_t units = static_cast<uint64_t>(
+                __builtin_rint(__builtin_ldexp(w, kUnitBits)));
+            units = units > 0 ? units : 1;
+            if (l.plain) s.chunk_units[c] = units;
+            mine += units;
+        }
+        if (!l.plain) l.row_units = block_sum<true>(s, mine);
+    }
+    l.bound = 0;
+    l.wide = l.spread = false;
+    // The chunks' maxima bound what is kept: the k-th largest of them (to a bin of the
+    // histogram) has k tokens at or above it, and the one at which their own weights
+    // reach top-p's share has that much at or above it. A row whose maxima do not reach it
+    // has a wide nucleus.
+    if ((l.by_k && d.top_k < n.chunks) || (l.by_p && !l.by_k)) {
+        for (int c = b.c0; c < b.c1; ++c)
+            if (s.chunk_key[c] >= l.keep.key)
+                add(s.hist[far_bin(b.top - s.chunk_key[c])],
+                    l.by_k ? 1 : r.units(s.chunk_key[c]));
+        uint32_t bin;
+        uint64_t unused;
+        if (find_bin(s, s.hist, kBins,
+                     l.by_k ? static_cast<uint64_t>(d.top_k) : share(d.top_p, l.row_units), bin,
+                     unused)) {
+            const uint32_t last = bin_start(bin) + ((1u << bin_bits(bin)) - 1);
+            l.bound = b.top > last ? b.top - last : 0;
+        } else {
+            l.wide = !l.by_k;
+            l.spread = l.wide && n.hist && window_fits(r);
+        }
+    }
+    return l;
+}
+
+// The chunks of a row that a workgroup of a spread launch takes.
+__device__ __forceinline__ Span span_of(const SampleArgs &n, int group) {
+    const int each = (n.chunks + n.groups - 1) / n.groups;
+    const int first = each * group < n.chunks ? each * group : n.chunks;
+    return Span{first, first + each < n.chunks ? first + each : n.chunks};
+}
+
+// A spread launch's row and its limits; false where the row has no use for it.
+template <int D>
+__device__ __forceinline__ bool spread_row(Shared &s, const SampleArgs &n, int64_t t, Begun<D> &b,
+                                           Limits &l) {
+    b = begin_row<D>(s, n, t);
+    if (b.top == 0 || b.d.greedy) return false;
+    l = limit_row(s, n, t, b);
+    return l.spread;
+}
+
+// The first pass over such rows, spread: LDS histograms added up in memory.
+template <int D>
+__global__ void __launch_bounds__(kThreads) spread_bins_kernel(const SampleArgs n) {
+    __shared__ Shared s;
+    const int64_t t = blockIdx.y;
+    Begun<D> b;
+    Limits l;
+    if (!spread_row(s, n, t, b, l)) return;
+    clear_bins(s);
+    window_bins(s, b.r, span_of(n, blockIdx.x), l.keep.key, l.row_units);
+    __syncthreads();
+    const uint32_t *hist = reinterpret_cast<const uint32_t *>(s.hist);
+    for (int i = threadIdx.x; i < kBins; i += kThreads)
+        if (hist[i]) atomicAdd(&n.hist[t * kBins + i], hist[i]);
+}
+
+// The added-up histogram into LDS, where the row's own is cleared.
+__device__ __forceinline__ void load_bins(Shared &s, const SampleArgs &n, int64_t t) {
+    __syncthreads();
+    uint32_t *hist = reinterpret_cast<uint32_t *>(s.hist);
+    for (int i = threadIdx.x; i < kBins; i += kThreads) hist[i] = n.hist[t * kBins + i];
+}
+
+// The second pass, spread: chunks' sums and the candidates inside the window.
+template <int D>
+__global__ void __launch_bounds__(kThreads) spread_sums_kernel(const SampleArgs n) {
+    __shared__ Shared s;
+    const int64_t t = blockIdx.y;
+    const int tid = threadIdx.x;
+    Begun<D> b;
+    Limits l;
+    if (!spread_row(s, n, t, b, l)) return;
+    load_bins(s, n, t);
+    const Window w = window_of(s, b.r, b.d.top_p, b.top, l.keep.key);
+    if (!w.found) return;
+    const Span span = span_of(n, blockIdx.x);
+    window_sums(s, b.r, span, w);
+    for (int c = span.first + tid; c < span.end; c += kThreads)
+        n.units[t * n.chunks + c] = s.chunk_units[c];
+    // a list that does not fit is counted, and noticed by its size
+    const uint32_t size = s.list_size < kList ? s.list_size : kList;
+    if (tid == 0) s.found_bin = atomicAdd(&n.listed[t], s.list_size);
+    __syncthreads();
+    const uint32_t at = s.found_bin;
+    for (uint32_t i = tid; i < size; i += kThreads)
+        if (at + i < kList) {
+            n.list_key[t * kList + at + i] = s.list_key[i];
+            n.list_at[t * kList + at + i] = s.list_at[i];
+        }
+}
+
+// What the spread launches left, into LDS.
+template <int D>
+__device__ __forceinline__ void load_spread(Shared &s, const SampleArgs &n, int64_t t) {
+    const uint32_t listed = n.listed[t];
+    for (int c = threadIdx.x; c < n.chunks; c += kThreads)
+        s.chunk_units[c] = n.units[t * n.chunks + c];
+    for (uint32_t i = threadIdx.x; i < (listed < kList ? listed : kList); i += kThreads) {
+        s.list_key[i] = n.list_key[t * kList + i];
+        s.list_at[i] = n.list_at[t * kList + i];
+    }
+    if (threadIdx.x == 0) s.list_size = listed;
+    __syncthreads();
+}
+
+// The border of a nucleus that the list does not hold, by its window. `spread`: the two
+// passes were made already. False where nothing is decided.
+template <int D>
+__device__ __forceinline__ bool nucleus(Shared &s, const SampleArgs &n, int64_t t, const Row<D> &r,
+                                        float part, uint32_t top, uint64_t units, bool spread,
+                                        Keep &keep) {
+    if (!window_fits(r)) return false;
+    const Span all{0, r.chunks};
+    if (spread) {
+        load_bins(s, n, t);
+    } else {
+        clear_bins(s);
+        window_bins(s, r, all, keep.key, units);
+    }
+    const Window w = window_of(s, r, part, top, keep.key);
+    if (!w.found) return false;
+    if (spread) load_spread<D>(s, n, t);
+    else window_sums(s, r, all, w);
+    return window_border(s, r, part, w, units, keep);
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     __shared__ Shared s;
     const sifar_sample_args &a = n.a;
     const int64_t t = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const Draw d = draw_of(a, t);
     const float u = a.uniform[t];
-
-    Row<D> r;
-    r.logits = static_cast<const Stored<D> *>(a.logits) + t * a.logits_stride;
-    r.vocab = a.vocab;
-    r.chunks = n.chunks;
-    // a thread's chunks: c0 .. c1 - 1, in index order over the threads
-    const int per = (n.chunks + kThreads - 1) / kThreads;
-    const int c0 = tid * per < n.chunks ? tid * per : n.chunks;
-    const int c1 = c0 + per < n.chunks ? c0 + per : n.chunks;
-    uint32_t my_key = 0;
-    for (int c = c0; c < c1; ++c) {
-        const float m = n.max[t * n.chunks + c];
-        const uint32_t k = m > -__builtin_inff() ? key_of(m) : 0;
-        s.chunk_key[c] = k;
-        s.chunk_units[c] = 0;
-        s.chunk_ties[c] = 0;
-        my_key = k > my_key ? k : my_key;
-    }
     if (tid == 0) {
         s.first_top = kMaxChunks;
         s.chosen = 0;
         s.chosen_at = 0;
         s.chosen_ties = 0;
     }
-    for (int b = tid; b < kBins; b += kThreads) s.hist[b] = 0;
-    const uint32_t top = block_max(s, my_key);
+    Begun<D> b = begin_row<D>(s, n, t);
+    const Draw &d = b.d;
+    Row<D> &r = b.r;
+    const uint32_t top = b.top, my_key = b.my_key;
+    const int c0 = b.c0, c1 = b.c1;
     if (top == 0) {  // nothing is there
         if (tid == 0) {
             a.out[t] = -1;
@@ -888,7 +1141,6 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
         }
         return;
     }
-    r.max = value_of(top);
     if (d.greedy) {
         if (my_key == top)
             for (int c = c0; c < c1; ++c)
@@ -911,64 +1163,17 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
         }
         return;
     }
-    r.max64 = static_cast<double>(r.max);
-    r.finite = r.max < __builtin_inff();
-    const double tau = static_cast<double>(d.temperature);
-    r.scale = kLog2e / tau;
-    r.one = value_of(key_from(r.max64 - kUnitBits * kLn2 * tau));
-
-    Keep keep{r.finite ? key_from(r.max64 - kCut * kLn2 * tau) : top, kAllTies};
-    uint32_t least = keep.key;  // of min-p
-    // at an infinite temperature every weight is 1
-    if (d.min_p > 0.0f && r.finite && d.temperature < __builtin_inff()) {
-        const double p = d.min_p < 1.0f ? static_cast<double>(d.min_p) : 1.0;
-        const uint32_t k = key_from(p < 1.0 ? r.max64 + log(p) * tau : r.max64);
-        least = k > least ? k : least;
-    }
-    const bool by_k = d.top_k > 0, by_p = d.top_p < 1.0f;
-    // every weight above the cut is kept: the scan's sums serve
-    const bool plain = !by_k && !by_p && !(d.min_p > 0.0f);
-    uint64_t row_units = 0;
-    if (plain || (by_p && !by_k)) {
-        uint64_t mine = 0;
-        for (int c = c0; c < c1; ++c) {
-            if (s.chunk_key[c] < keep.key) continue;
-            const double w = exp2_64(log2_weight(value_of(s.chunk_key[c]), r.max, r.scale)) *
-                             n.mass[t * n.chunks + c];
-            uint64_t units = static_cast<uint64_t>(
-                __builtin_rint(__builtin_ldexp(w, kUnitBits)));
-            units = units > 0 ? units : 1;
-            if (plain) s.chunk_units[c] = units;
-            mine += units;
-        }
-        if (!plain) row_units = block_sum<true>(s, mine);
-    }
+    const Limits limits = limit_row(s, n, t, b);
+    Keep keep = limits.keep;
+    const uint32_t least = limits.least;
+    const bool by_k = limits.by_k, by_p = limits.by_p, plain = limits.plain;
+    const uint64_t row_units = limits.row_units;
     if (!plain) {
-        // First the candidates above a bound that is known: min-p's, or (to a bin) the
-        // rank-th largest of the maxima, above which there are at least `rank`. That is
-        // enough for top-k, and likely for a nucleus, unless its weight says that it
-        // holds more tokens.
+        // First the candidates above a bound that is known, if they are few.
         uint32_t from = by_p ? keep.key : least;
-        const int rank = by_k ? d.top_k : kNucleus;
-        const int groups = (n.chunks + per - 1) / per;
-        const bool wide =
-            by_p && !by_k &&
-            static_cast<double>(d.top_p) * static_cast<double>(row_units) >
-                static_cast<double>(kNucleusMass) * __builtin_ldexp(1.0, kUnitBits);
-        if ((by_k || (by_p && !wide)) && rank < groups) {
-            if (tid < groups) add(s.hist[far_bin(top - my_key)], 1);  // cleared above
-            uint32_t bin;
-            uint64_t unused;
-            find_bin(s, s.hist, kBins, static_cast<uint64_t>(rank), bin, unused);
-            const uint32_t last = bin_start(bin) + ((1u << bin_bits(bin)) - 1);
-            const uint32_t bound = top > last ? top - last : 0;
-            from = bound > from ? bound : from;
-        }
-        bool listed = !wide && collect(s, r, from, top);
+        from = limits.bound > from ? limits.bound : from;
+        bool listed = !limits.wide && collect(s, r, from, top);
         const InList list{s, s.list_size};
-        if (listed && by_p && !by_k && from > keep.key)
-            listed = kept_units(s, list, r, Keep{from, kAllTies}) >=
-                     share(d.top_p, row_units);
         if (listed && list.size <= kSmall) {
             draw_small(s, r, d, static_cast<int>(list.size), least, row_units, u, a.out + t,
                        a.probs ? a.probs + t : nullptr);
@@ -977,7 +1182,8 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
         if (listed) {
             keep = filter(s, list, r, d, top, row_units, Keep{from, kAllTies});
             if (least > keep.key) keep = Keep{least, kAllTies};
-        } else if (by_p && !by_k && window(s, r, d.top_p, top, row_units, keep)) {
+        } else if (by_p && !by_k && nucleus(s, n, t, r, d.top_p, top, row_units, limits.spread,
+                                           keep)) {
             listed = least <= keep.key;  // else what is above the window counts too much
             if (!listed) keep = Keep{least, kAllTies};
         } else {
@@ -993,7 +1199,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
             __syncthreads();
             for (int c = c0; c < c1; ++c) s.chunk_units[c] = 0;
             const float low = value_of(keep.key);
-            const uint32_t size = queue_chunks(s, n.chunks, keep.key);
+            const uint32_t size = queue_chunks(s, Span{0, n.chunks}, keep.key);
             // a chunk's ties in the ten top bits of its sum, which weights leave free
             each_batch(s, r, size, [&](const Raw &x, int) {
                 uint64_t sum = 0;
@@ -1098,17 +1304,70 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     }
 }
 
+// Byte offsets in the workspace, each a multiple of 16, for the most chunks that any
+// type has.
+struct Workspace {
+    int64_t mass, units, max, hist, listed, list_key, list_at, end;
+};
+
+Workspace workspace_of(int32_t tokens, int32_t vocab) {
+    const int64_t t = tokens, chunks = t * ((vocab + kLeastChunk - 1) / kLeastChunk);
+    // of the batches that may be spread, so that a larger one's workspace serves them
+    const int64_t rows = vocab < kSpreadVocab ? 0 : tokens < kSpreadRows ? tokens : kSpreadRows;
+    int64_t at = 0;
+    const auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += (bytes + 15) / 16 * 16;
+        return here;
+    };
+    Workspace w;
+    w.mass = take(chunks * 8);
+    w.max = take(chunks * 4);
+    w.units = take(t ? chunks / t * rows * 8 : 0);
+    w.hist = take(rows * kBins * 4);
+    w.listed = take(rows * 4);
+    w.list_key = take(rows * kList * 4);
+    w.list_at = take(rows * kList * 4);
+    w.end = at;
+    return w;
+}
+
 template <int D>
 hipError_t launch_sample(SampleArgs &n, hipStream_t s) {
-    n.chunks = (n.a.vocab + kChunkOf<D> - 1) / kChunkOf<D>;
-    n.mass = static_cast<double *>(n.a.workspace);
-    n.max = reinterpret_cast<float *>(n.mass + static_cast<int64_t>(n.a.tokens) * n.chunks);
+    const sifar_sample_args &a = n.a;
+    n.chunks = (a.vocab + kChunkOf<D> - 1) / kChunkOf<D>;
+    const Workspace w = workspace_of(a.tokens, a.vocab);
+    const auto at = [&](int64_t offset) {
+        return static_cast<void *>(static_cast<char *>(a.workspace) + offset);
+    };
+    n.mass = static_cast<double *>(at(w.mass));
+    n.max = static_cast<float *>(at(w.max));
+    const bool spread =
+        a.top_p && !a.top_k && a.tokens <= kSpreadRows && a.vocab >= kSpreadVocab;
+    if (spread) {
+        n.units = static_cast<uint64_t *>(at(w.units));
+        n.hist = static_cast<uint32_t *>(at(w.hist));
+        n.listed = static_cast<uint32_t *>(at(w.listed));
+        n.list_key = static_cast<uint32_t *>(at(w.list_key));
+        n.list_at = static_cast<uint32_t *>(at(w.list_at));
+        // a batch of chunks for each wave at least
+        const int most = (n.chunks + kPickWaves * kBatch - 1) / (kPickWaves * kBatch);
+        n.groups = kSpreadGroups / a.tokens < most ? kSpreadGroups / a.tokens : most;
+    }
     const int per_group = kScanWaves * kBatch;
-    const dim3 scan(n.a.tokens, (n.chunks + per_group - 1) / per_group);
+    const dim3 scan(a.tokens, (n.chunks + per_group - 1) / per_group);
     scan_kernel<D><<<scan, dim3(kRowWave, kScanWaves), 0, s>>>(n);
-    const hipError_t e = hipGetLastError();
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && spread) {
+        const dim3 grid(n.groups, a.tokens);
+        spread_bins_kernel<D><<<grid, kThreads, 0, s>>>(n);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        spread_sums_kernel<D><<<grid, kThreads, 0, s>>>(n);
+        e = hipGetLastError();
+    }
     if (e != hipSuccess) return e;
-    pick_kernel<D><<<n.a.tokens, kThreads, 0, s>>>(n);
+    pick_kernel<D><<<a.tokens, kThreads, 0, s>>>(n);
     return hipGetLastError();
 }
 
@@ -1154,8 +1413,7 @@ bool good(const sifar_sample_args &a) {
 extern "C" int64_t sifar_sample_workspace(int32_t tokens, int32_t vocab) {
     using namespace sifar;
     if (!good_sizes(tokens, vocab)) return SIFAR_EINVAL;
-    const int64_t chunks = (vocab + kLeastChunk - 1) / kLeastChunk;
-    return tokens * chunks * static_cast<int64_t>(sizeof(double) + sizeof(float));
+    return workspace_of(tokens, vocab).end;
 }
 
 extern "C" int sifar_sample(const sifar_sample_args *args, void *stream) {

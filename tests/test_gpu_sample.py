@@ -284,6 +284,56 @@ def test_largest_vocabulary():
         check(x, [0.3, 0.999], **kw)
 
 
+@pytest.mark.parametrize("T,V", [(1, 65536), (3, 70001), (64, 66000), (65, 66000), (2, 262144)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_nucleus_of_large_rows(T, V, dtype):
+    """Few rows of many logits, whose passes are spread over workgroups, and the batch
+    beyond: flat and peaked rows side by side, greedy and masked ones among them; with
+    min-p, which cuts a nucleus short."""
+    x = logits(30, T, V, dtype)
+    x[T // 2] = logits(31, 1, V, dtype, "peaked")[0]
+    x[T - 1, : V // 3] = -INF
+    r = rng(30, T, V)
+    tau = 0.7 + 0.6 * r.random(T)
+    tau[2::7] = 0.0
+    if T > 4:
+        x[4] = -INF
+    u, p = r.random(T), 0.3 + 0.699 * r.random(T)
+    check(x, u, temperature=tau, top_p=p)
+    check(x, u, temperature=tau, top_p=p, min_p=0.02)
+    check(x, u, temperature=tau, top_p=p, top_k=0)
+
+
+def test_nucleus_of_rows_with_few_values():
+    """A window that no list holds: many equal logits at the border."""
+    x = torch.from_numpy(rng(32).integers(0, 3, (4, 70000)).astype(np.float32)).to(DEV)
+    x[1] = 5.0
+    check(x, [0.1, 0.5, 0.9, 0.99], top_p=[0.3, 0.5, 0.9, 0.999])
+
+
+def test_spread_rows_replay():
+    T, V = 3, 70000
+    r = rng(33)
+    x, u = logits(33, T, V), torch.from_numpy(r.random(T)).float().to(DEV)
+    p = torch.full((T,), 0.9, device=DEV)
+    ws = [torch.full((S.sifar_sample_workspace(256, V),), 0x5A, dtype=torch.uint8, device=DEV)
+          for _ in range(2)]
+    out = [torch.empty(T, dtype=torch.int32, device=DEV) for _ in range(2)]
+    S.sifar_sample(x, u, out[0], ws[0], top_p=p)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        S.sifar_sample(x, u, out[0], ws[0], top_p=p)
+    for k in range(4):
+        x.copy_(logits(34 + k, T, V, shape=("flat", "peaked")[k & 1]))
+        u.copy_(torch.from_numpy(r.random(T)))
+        g.replay()
+        S.sifar_sample(x, u, out[1], ws[1], top_p=p)
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], out[1])
+        check(x, u.cpu(), top_p=0.9)
+
+
 def test_streams_and_replays():
     x0, r = logits(14, 9, 5000), rng(14)
     u = torch.from_numpy(r.random(9)).float().to(DEV)

@@ -60,6 +60,10 @@ def test_workspace_sizes():
     assert S.sifar_sample_workspace(0, 1) == 0
     assert 0 < S.sifar_sample_workspace(1, 1) <= S.sifar_sample_workspace(1, 1024)
     assert S.sifar_sample_workspace(1, 1024) < S.sifar_sample_workspace(1, 1025)
+    for v in (1, 65535, 65536, 128256, 1 << 20):     # more tokens or logits never need less
+        need = [S.sifar_sample_workspace(t, v) for t in (0, 1, 2, 63, 64, 65, 256, 4096)]
+        assert need == sorted(need)
+        assert need[3] <= S.sifar_sample_workspace(63, min(v + 1, 1 << 20))
     big = S.sifar_sample_workspace(S.SIFAR_ROWS_MAX_TOKENS, S.SIFAR_SAMPLE_MAX_VOCAB)
     assert big >= 1 << 30    # past 32 bits of bytes, not wrapped
     for t, v in ((-1, 5), (5, 0), (5, -1), (1 << 21, 5), (5, 1 << 21), (1 << 40, 5)):
