@@ -620,6 +620,8 @@ def sifar_sample(logits, uniform, out, workspace, probs=None, temperature=None, 
     T, V = shape
     if T > SIFAR_ROWS_MAX_TOKENS or V > SIFAR_SAMPLE_MAX_VOCAB:
         _refuse(fn, f"{T} x {V} is too large")
+    if workspace.dim() != 1:
+        _refuse(fn, f"workspace has {workspace.dim()} dimensions, not 1")
     dev = _gpu(fn, "logits", logits)
     rows = shape[:1]
     x, x_stride = _operand(fn, "logits", logits, logits.dtype, shape, dev)

@@ -84,7 +84,7 @@ __device__ __forceinline__ uint32_t key_from(double limit) {
     return k < kLowestKey ? kLowestKey : k;
 }
 
-// The larger of two numbers; of a number and a NaN, the number.
+// The larger of two numbers; of a number and a quiet NaN, the number.
 __device__ __forceinline__ float max32(float a, float b) {
     float r;
     asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
@@ -131,6 +131,14 @@ __device__ __forceinline__ float logit(const Raw &e, int i) {
         return __uint_as_float(i & 1 ? e.v[i >> 1] & 0xFFFF0000u : e.v[i >> 1] << 16);
     else
         return widen<D>(i & 1 ? e.v[i >> 1] >> 16 : e.v[i >> 1] & 0xFFFFu);
+}
+
+// The same where v_max_f32 reads it, which would answer a signalling NaN with a NaN:
+// quiet. (Half precision comes quiet from its conversion.)
+template <int D>
+__device__ __forceinline__ float quiet_logit(const Raw &e, int i) {
+    const float x = logit<D>(e, i);
+    return D == SIFAR_FP16 ? x : max32(x, x);
 }
 
 template <int D>
@@ -243,7 +251,7 @@ __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const Sample
     for (int b = 0; b < kBatch; ++b) {
         top[b] = -__builtin_inff();
 #pragma unroll
-        for (int i = 0; i < kVec<D>; ++i) top[b] = max32(top[b], logit<D>(x[b], i));
+        for (int i = 0; i < kVec<D>; ++i) top[b] = max32(top[b], quiet_logit<D>(x[b], i));
     }
     const float mine = wave_reduce4(top, Max32{});
     const int c = first + (lane >> 4);
@@ -265,11 +273,11 @@ __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const Sample
 #pragma unroll
                 for (int i = 0; i < kVec<D>; ++i)
                     sum[b] += exp2_quick<0>(
-                        static_cast<double>(max32(logit<D>(x[b], i), least)) - max, scale);
+                        static_cast<double>(max32(quiet_logit<D>(x[b], i), least)) - max, scale);
             } else {  // a temperature or a maximum for which no logit lies at the cut
 #pragma unroll
                 for (int i = 0; i < kVec<D>; ++i) {
-                    const float l = logit<D>(x[b], i);
+                    const float l = quiet_logit<D>(x[b], i);
                     sum[b] += exp2_quick<0>(static_cast<double>(max32(l, least)) - max, scale,
                                             l >= least);
                 }
@@ -807,7 +815,7 @@ __device__ __forceinline__ void window_sums(Shared &s, const Row<D> &r, Span spa
         uint64_t sum = 0;
 #pragma unroll
         for (int i = 0; i < kVec<D>; ++i) {
-            const float l = logit<D>(x, i);
+            const float l = quiet_logit<D>(x, i);
             sum += r.units_near(max32(l, high), l > high);
         }
         sum -= kVec<D> * kUnitBase;  // modulo 2^64

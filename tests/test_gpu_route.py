@@ -175,6 +175,15 @@ def test_bias_that_is_not_finite():
     check(x, 6, "softmax", b, 4, 2, 1)
 
 
+@pytest.mark.parametrize("dtype,bits", [("fp32", 0x7F800001), ("bf16", 0x7F81), ("fp16", 0x7C01)])
+def test_signalling_nans_are_not_there(dtype, bits):
+    x = logits(15, 5, 130, dtype)
+    x.view(torch.int32 if dtype == "fp32" else torch.int16)[:, 3::5] = bits
+    for kw in (dict(), dict(score="sigmoid"), dict(renorm=False),
+               dict(score="sigmoid", bias=balance(15, 130), groups=10, top_groups=3, group_top=2)):
+        check(x, 7, **kw)
+
+
 def test_saturated_scores_keep_the_order_of_their_logits():
     x = torch.arange(64, device=DEV).float()[None] + 40.0
     ids, _ = run(x, 8, "sigmoid")

@@ -176,6 +176,20 @@ def test_nothing_is_there():
             check(x, rng(4, V).random(6), **kw)
 
 
+@pytest.mark.parametrize("dtype,bits", [("fp32", 0x7F800001), ("fp32", 0xFFA00000 - (1 << 32)),
+                                        ("bf16", 0x7F81), ("bf16", 0xFF81 - (1 << 16)),
+                                        ("fp16", 0x7C01), ("fp16", 0xFD00 - (1 << 16))])
+@pytest.mark.parametrize("V", [900, 70000])
+def test_signalling_nans_are_not_there(dtype, bits, V):
+    x = logits(45, 3, V, dtype)
+    raw = x.view(torch.int32 if dtype == "fp32" else torch.int16)
+    raw[:, 5::7] = bits
+    raw[1, : V // 2] = bits
+    for kw in (dict(), dict(temperature=0.0), dict(top_k=9), dict(top_p=0.95),
+               dict(top_k=V, top_p=0.9), dict(min_p=0.05), dict(temperature=INF)):
+        check(x, [0.1, 0.6, 0.95], **kw)
+
+
 def test_infinite_logits_share_the_weight():
     x = logits(5, 4, 2500)
     x[0, 7] = INF

@@ -148,7 +148,8 @@ def test_marshalling(recorder):
     dict(top_p=torch.zeros(T, 1)), dict(min_p=torch.zeros(1)), dict(probs=torch.zeros(T - 1)),
     dict(temperature=torch.zeros(T, dtype=torch.float16)),
     dict(workspace=torch.zeros(NEED)), dict(workspace=torch.zeros(2, NEED, dtype=torch.uint8)),
-], ids=range(14))
+    dict(workspace=torch.zeros((), dtype=torch.uint8)),
+], ids=range(15))
 def test_refused_by_the_binding(recorder, kw):
     with pytest.raises(S.SifarError) as e:
         S.sifar_sample(**tensors(**kw))
