@@ -659,7 +659,7 @@ int sifar_route(const sifar_route_args *a, void *stream);
  * Limits: 1 <= vocab <= SIFAR_SAMPLE_MAX_VOCAB; 0 <= tokens <=
  * SIFAR_ROWS_MAX_TOKENS; pointers aligned to their elements. Outputs and
  * workspace that overlap each other or an input are refused. Two launches; with
- * top_p and no top_k, up to 64 rows of 65536 logits or more take four. */
+ * top_p and no top_k, up to 128 rows of 65536 logits or more take four. */
 #define SIFAR_SAMPLE_MAX_VOCAB 1048576
 typedef struct {
     int32_t dtype;

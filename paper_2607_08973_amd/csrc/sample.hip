@@ -6,15 +6,16 @@
 // the weights' sum. pick_kernel, a workgroup a row, finds the threshold of top-k,
 // top-p and min-p and walks to the token in index order, reading again only
 // chunks whose maximum says that they hold something to keep. A nucleus of many
-// tokens takes two more passes over its row, which a workgroup makes in 63 us for
+// tokens takes two more passes over its row, which a workgroup makes in 60 us for
 // 128256 logits; where few rows would leave the GPU idle meanwhile, two launches
 // between spread them over several workgroups a row.
 //
 // Weights w = 2^((x - max) log2(e) / temperature) are 64-bit values rounded to
 // units of 2^-42 and added as integers: sums do not depend on the order of
 // addition, so histograms may be filled by atomics, and a border between two
-// tokens is off by 2^-43 a token at most. In 32 bits a draw from a flat row of
-// 100000 tokens would land on the neighbour once in a thousand times.
+// tokens is off by 2^-43 a token at most. In 32 bits, where a running sum is off by
+// some 1e-8, one draw in a thousand from a flat row of 100000 tokens would land on
+// the neighbour.
 //
 // Bound: the 64-bit exponentials for many rows, latency of the two launches and
 // of pick_kernel's barriers and loads for a few.
@@ -36,13 +37,13 @@ constexpr int kBins = 64 + 26 * 64;            // log-linear bins of a 32-bit di
 constexpr int kList = 4096;                    // candidates kept in LDS
 constexpr int kSmall = 256;                    // most candidates that are ranked by counting
 constexpr int kPerBit = 64;                    // bins of a halving of the weight
-// Passes over rows are spread for up to 64 rows of 65536 logits or more. 1 x 128256: a
-// wide nucleus took 69 us in one workgroup and takes 40, a narrow one, for which the
-// two launches find nothing to do, 16 and 20; 64 x 128256: 82 and 63. At 32768 logits a
-// workgroup needs 33 us for a wide nucleus, the four launches 38; 65 x 128256 would
-// leave a workgroup as much as it has now.
-constexpr int kSpreadRows = 64;
+// Passes over rows are spread for up to 128 rows of 65536 logits or more. A wide
+// nucleus, us a call in one workgroup a row and spread: 1 x 65536 47 and 33, 1 x 128256
+// 69 and 34, 128 x 65536 59 and 58, 128 x 128256 94 and 78. A narrow one, for which
+// the two launches find nothing to do: 1 x 65536 12 and 16.
+constexpr int kSpreadRows = 128;
 constexpr int kSpreadVocab = 65536;
+constexpr int kSpreadMaxima = 160;             // most chunks that hold a narrow nucleus
 constexpr int kSpreadGroups = 256;             // workgroups of a spread launch: one a CU
 constexpr int kUnitBits = 42;                  // a weight of 1 in units
 constexpr uint64_t kUnitBase = 0x433ull << 52;  // the bits of 2^52: units are its last place
@@ -51,6 +52,16 @@ constexpr double kLn2 = 0.6931471805599453;
 constexpr double kCut = 60.0;                  // weights below 2^-60 are 0
 constexpr float kLowest = -3.402823466e38f;
 
+// What the first spread launch finds out about a row, for the launches behind it, and
+// the second for the third.
+struct RowState {
+    uint64_t row_units;
+    uint32_t top, bound;
+    uint32_t wide, spread;
+    uint32_t above, least, found;  // the window
+    uint32_t unused;
+};
+
 struct SampleArgs {
     sifar_sample_args a;
     int32_t chunks;  // of a row
@@ -58,6 +69,7 @@ struct SampleArgs {
     uint64_t *units; // [tokens][chunks], of what lies above a spread row's window
     float *max;      // [tokens][chunks]
     // spread rows, or null
+    RowState *state; // [tokens]
     uint32_t *hist;  // [tokens][kBins]
     uint32_t *listed;                // [tokens] candidates in the window,
     uint32_t *list_key, *list_at;    // [tokens][kList]
@@ -319,8 +331,8 @@ __device__ __forceinline__ void add(uint64_t &sum, uint64_t x) {  // in LDS
 }
 
 // Inclusive sum over the lanes below: DPP moves within rows of 16, then the last
-// lane of a row, and of the lower half, to the rows above. (Shuffles through LDS
-// took six times as long, and a row's walk has a dozen of these.)
+// lane of a row, and of the lower half, to the rows above. (By shuffles
+// through LDS a call of 1 x 32000 took 3 us more: a row's walk has a dozen of these.)
 template <int CTRL, int ROWS>
 __device__ __forceinline__ uint64_t add_from(uint64_t x) {
     const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(static_cast<uint32_t>(x)), CTRL,
@@ -943,7 +955,6 @@ __device__ __forceinline__ Begun<D> begin_row(Shared &s, const SampleArgs &n, in
     }
     for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
     b.top = block_max(s, b.my_key);
-    b.r.max = value_of(b.top);
     return b;
 }
 
@@ -959,17 +970,17 @@ struct Limits {
     uint64_t row_units;  // the whole weight, where top-p starts from it
 };
 
+// From the maximum alone.
 template <int D>
-__device__ __forceinline__ Limits limit_row(Shared &s, const SampleArgs &n, int64_t t, Begun<D> &b) {
-    const Draw &d = b.d;
-    Row<D> &r = b.r;
+__device__ __forceinline__ Limits limit_row(const Draw &d, uint32_t top, Row<D> &r) {
     Limits l;
+    r.max = value_of(top);
     r.max64 = static_cast<double>(r.max);
     r.finite = r.max < __builtin_inff();
     const double tau = static_cast<double>(d.temperature);
     r.scale = kLog2e / tau;
     r.one = value_of(key_from(r.max64 - kUnitBits * kLn2 * tau));
-    l.keep = Keep{r.finite ? key_from(r.max64 - kCut * kLn2 * tau) : b.top, kAllTies};
+    l.keep = Keep{r.finite ? key_from(r.max64 - kCut * kLn2 * tau) : top, kAllTies};
     l.least = l.keep.key;
     // at an infinite temperature every weight is 1
     if (d.min_p > 0.0f && r.finite && d.temperature < __builtin_inff()) {
@@ -981,6 +992,17 @@ __device__ __forceinline__ Limits limit_row(Shared &s, const SampleArgs &n, int6
     l.by_p = d.top_p < 1.0f;
     l.plain = !l.by_k && !l.by_p && !(d.min_p > 0.0f);
     l.row_units = 0;
+    l.bound = 0;
+    l.wide = l.spread = false;
+    return l;
+}
+
+// From the chunks' maxima and sums.
+template <int D>
+__device__ __forceinline__ void weigh_row(Shared &s, const SampleArgs &n, int64_t t,
+                                          const Begun<D> &b, Limits &l) {
+    const Draw &d = b.d;
+    const Row<D> &r = b.r;
     if (l.plain || (l.by_p && !l.by_k)) {
         uint64_t mine = 0;
         for (int c = b.c0; c < b.c1; ++c) {
@@ -995,8 +1017,6 @@ __device__ __forceinline__ Limits limit_row(Shared &s, const SampleArgs &n, int6
         }
         if (!l.plain) l.row_units = block_sum<true>(s, mine);
     }
-    l.bound = 0;
-    l.wide = l.spread = false;
     // The chunks' maxima bound what is kept: the k-th largest of them (to a bin of the
     // histogram) has k tokens at or above it, and the one at which their own weights
     // reach top-p's share has that much at or above it. A row whose maxima do not reach it
@@ -1013,12 +1033,18 @@ __device__ __forceinline__ Limits limit_row(Shared &s, const SampleArgs &n, int6
                      unused)) {
             const uint32_t last = bin_start(bin) + ((1u << bin_bits(bin)) - 1);
             l.bound = b.top > last ? b.top - last : 0;
+            if (n.hist && !l.by_k) {
+                // more than a few candidates take longer to list and sort out than spread
+                // passes do: 55 us against 39 for 4 x 128256
+                uint64_t mine = 0;
+                for (int c = b.c0; c < b.c1; ++c) mine += s.chunk_key[c] >= l.bound;
+                l.wide = block_sum(s, mine) > kSpreadMaxima;
+            }
         } else {
             l.wide = !l.by_k;
-            l.spread = l.wide && n.hist && window_fits(r);
         }
+        l.spread = l.wide && n.hist && window_fits(r);
     }
-    return l;
 }
 
 // The chunks of a row that a workgroup of a spread launch takes.
@@ -1028,24 +1054,27 @@ __device__ __forceinline__ Span span_of(const SampleArgs &n, int group) {
     return Span{first, first + each < n.chunks ? first + each : n.chunks};
 }
 
-// A spread launch's row and its limits; false where the row has no use for it.
-template <int D>
-__device__ __forceinline__ bool spread_row(Shared &s, const SampleArgs &n, int64_t t, Begun<D> &b,
-                                           Limits &l) {
-    b = begin_row<D>(s, n, t);
-    if (b.top == 0 || b.d.greedy) return false;
-    l = limit_row(s, n, t, b);
-    return l.spread;
-}
-
 // The first pass over such rows, spread: LDS histograms added up in memory.
 template <int D>
 __global__ void __launch_bounds__(kThreads) spread_bins_kernel(const SampleArgs n) {
     __shared__ Shared s;
     const int64_t t = blockIdx.y;
-    Begun<D> b;
-    Limits l;
-    if (!spread_row(s, n, t, b, l)) return;
+    Begun<D> b = begin_row<D>(s, n, t);
+    if (b.top == 0 || b.d.greedy) {  // the same in every thread
+        if (blockIdx.x == 0 && threadIdx.x == 0) n.state[t].spread = 0;
+        return;
+    }
+    Limits l = limit_row(b.d, b.top, b.r);
+    if (l.by_p) weigh_row(s, n, t, b, l);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        RowState *state = n.state + t;
+        state->row_units = l.row_units;
+        state->top = b.top;
+        state->bound = l.bound;
+        state->wide = l.wide;
+        state->spread = l.spread;
+    }
+    if (!l.spread) return;
     clear_bins(s);
     window_bins(s, b.r, span_of(n, blockIdx.x), l.keep.key, l.row_units);
     __syncthreads();
@@ -1054,27 +1083,36 @@ __global__ void __launch_bounds__(kThreads) spread_bins_kernel(const SampleArgs 
         if (hist[i]) atomicAdd(&n.hist[t * kBins + i], hist[i]);
 }
 
-// The added-up histogram into LDS, where the row's own is cleared.
-__device__ __forceinline__ void load_bins(Shared &s, const SampleArgs &n, int64_t t) {
-    __syncthreads();
-    uint32_t *hist = reinterpret_cast<uint32_t *>(s.hist);
-    for (int i = threadIdx.x; i < kBins; i += kThreads) hist[i] = n.hist[t * kBins + i];
-}
-
 // The second pass, spread: chunks' sums and the candidates inside the window.
 template <int D>
 __global__ void __launch_bounds__(kThreads) spread_sums_kernel(const SampleArgs n) {
     __shared__ Shared s;
     const int64_t t = blockIdx.y;
     const int tid = threadIdx.x;
-    Begun<D> b;
-    Limits l;
-    if (!spread_row(s, n, t, b, l)) return;
-    load_bins(s, n, t);
-    const Window w = window_of(s, b.r, b.d.top_p, b.top, l.keep.key);
-    if (!w.found) return;
+    const RowState state = n.state[t];
+    if (!state.spread) return;
+    const Draw d = draw_of(n.a, t);
+    Row<D> r;
+    r.logits = static_cast<const Stored<D> *>(n.a.logits) + t * n.a.logits_stride;
+    r.vocab = n.a.vocab;
+    r.chunks = n.chunks;
+    const Limits l = limit_row(d, state.top, r);
     const Span span = span_of(n, blockIdx.x);
-    window_sums(s, b.r, span, w);
+    for (int c = span.first + tid; c < span.end; c += kThreads) {
+        const float m = n.max[t * n.chunks + c];
+        s.chunk_key[c] = m > -__builtin_inff() ? key_of(m) : 0;
+        s.chunk_units[c] = 0;
+    }
+    uint32_t *hist = reinterpret_cast<uint32_t *>(s.hist);
+    for (int i = tid; i < kBins; i += kThreads) hist[i] = n.hist[t * kBins + i];
+    const Window w = window_of(s, r, d.top_p, state.top, l.keep.key);
+    if (blockIdx.x == 0 && tid == 0) {
+        n.state[t].above = w.above;
+        n.state[t].least = w.least;
+        n.state[t].found = w.found;
+    }
+    if (!w.found) return;
+    window_sums(s, r, span, w);
     for (int c = span.first + tid; c < span.end; c += kThreads)
         n.units[t * n.chunks + c] = s.chunk_units[c];
     // a list that does not fit is counted, and noticed by its size
@@ -1109,18 +1147,20 @@ template <int D>
 __device__ __forceinline__ bool nucleus(Shared &s, const SampleArgs &n, int64_t t, const Row<D> &r,
                                         float part, uint32_t top, uint64_t units, bool spread,
                                         Keep &keep) {
+    if (spread) {
+        const RowState state = n.state[t];
+        if (!state.found) return false;
+        __syncthreads();
+        load_spread<D>(s, n, t);
+        return window_border(s, r, part, Window{true, state.above, state.least}, units, keep);
+    }
     if (!window_fits(r)) return false;
     const Span all{0, r.chunks};
-    if (spread) {
-        load_bins(s, n, t);
-    } else {
-        clear_bins(s);
-        window_bins(s, r, all, keep.key, units);
-    }
+    clear_bins(s);
+    window_bins(s, r, all, keep.key, units);
     const Window w = window_of(s, r, part, top, keep.key);
     if (!w.found) return false;
-    if (spread) load_spread<D>(s, n, t);
-    else window_sums(s, r, all, w);
+    window_sums(s, r, all, w);
     return window_border(s, r, part, w, units, keep);
 }
 
@@ -1140,6 +1180,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     Begun<D> b = begin_row<D>(s, n, t);
     const Draw &d = b.d;
     Row<D> &r = b.r;
+    r.max = value_of(b.top);
     const uint32_t top = b.top, my_key = b.my_key;
     const int c0 = b.c0, c1 = b.c1;
     if (top == 0) {  // nothing is there
@@ -1171,7 +1212,16 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
         }
         return;
     }
-    const Limits limits = limit_row(s, n, t, b);
+    Limits limits = limit_row(d, top, r);
+    if (n.hist && limits.by_p) {
+        const RowState state = n.state[t];
+        limits.row_units = state.row_units;
+        limits.bound = state.bound;
+        limits.wide = state.wide;
+        limits.spread = state.spread;
+    } else {
+        weigh_row(s, n, t, b, limits);
+    }
     Keep keep = limits.keep;
     const uint32_t least = limits.least;
     const bool by_k = limits.by_k, by_p = limits.by_p, plain = limits.plain;
@@ -1315,7 +1365,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
 // Byte offsets in the workspace, each a multiple of 16, for the most chunks that any
 // type has.
 struct Workspace {
-    int64_t mass, units, max, hist, listed, list_key, list_at, end;
+    int64_t mass, units, max, state, hist, listed, list_key, list_at, end;
 };
 
 Workspace workspace_of(int32_t tokens, int32_t vocab) {
@@ -1332,6 +1382,7 @@ Workspace workspace_of(int32_t tokens, int32_t vocab) {
     w.mass = take(chunks * 8);
     w.max = take(chunks * 4);
     w.units = take(t ? chunks / t * rows * 8 : 0);
+    w.state = take(rows * static_cast<int64_t>(sizeof(RowState)));
     w.hist = take(rows * kBins * 4);
     w.listed = take(rows * 4);
     w.list_key = take(rows * kList * 4);
@@ -1354,6 +1405,7 @@ hipError_t launch_sample(SampleArgs &n, hipStream_t s) {
         a.top_p && !a.top_k && a.tokens <= kSpreadRows && a.vocab >= kSpreadVocab;
     if (spread) {
         n.units = static_cast<uint64_t *>(at(w.units));
+        n.state = static_cast<RowState *>(at(w.state));
         n.hist = static_cast<uint32_t *>(at(w.hist));
         n.listed = static_cast<uint32_t *>(at(w.listed));
         n.list_key = static_cast<uint32_t *>(at(w.list_key));

@@ -298,12 +298,12 @@ def test_largest_vocabulary():
         check(x, [0.3, 0.999], **kw)
 
 
-@pytest.mark.parametrize("T,V", [(1, 65536), (3, 70001), (64, 66000), (65, 66000), (2, 262144)])
+@pytest.mark.parametrize("T,V", [(1, 65536), (3, 70001), (65, 66000), (2, 262144)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_nucleus_of_large_rows(T, V, dtype):
-    """Few rows of many logits, whose passes are spread over workgroups, and the batch
-    beyond: flat and peaked rows side by side, greedy and masked ones among them; with
-    min-p, which cuts a nucleus short."""
+    """Few rows of many logits, whose passes are spread over workgroups: flat and peaked
+    rows side by side, greedy and masked ones among them; with min-p, which cuts a
+    nucleus short, and where a top-k for some rows keeps the passes in one workgroup."""
     x = logits(30, T, V, dtype)
     x[T // 2] = logits(31, 1, V, dtype, "peaked")[0]
     x[T - 1, : V // 3] = -INF
