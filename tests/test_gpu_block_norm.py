@@ -280,3 +280,9 @@ def test_far_rows():
     rows.copy_(i["x"])
     out, y = run(dict(i, x=rows))
     check_run(i, out, y)
+
+
+def test_most_rows():
+    i = inputs(60, S.SIFAR_ROWS_MAX_TOKENS, 8, "bf16", gate="channel")
+    out, y = run(i)
+    check_run(i, out, y)

@@ -249,3 +249,15 @@ def test_streams_and_replays():
         ei, ew = run(x, 4, "sigmoid", bias, 8, 4, 2)
         torch.cuda.synchronize()
         assert torch.equal(gi, ei) and torch.equal(gw, ew)
+
+
+@pytest.mark.parametrize("biased", [False, True])
+def test_most_tokens(biased):
+    x = logits(50, S.SIFAR_ROWS_MAX_TOKENS, 3)
+    bias = torch.tensor([0.1, 0.0, -0.2], device=DEV) if biased else None
+    ids, w = run(x, 1, "sigmoid", bias, renorm=False)
+    s = torch.sigmoid(x.double().cpu())
+    best = (s + bias.double().cpu() if biased else s).argmax(-1, keepdim=True)
+    assert torch.equal(ids.cpu().long(), best)
+    s = s.gather(1, best)
+    assert ((w.double().cpu() - s).abs() <= s * (2.0 ** -24 + 1e-13)).all()

@@ -374,3 +374,43 @@ def test_streams_and_replays():
         S.sifar_sample(x, u, out[1], ws[1], top_p=p)
         torch.cuda.synchronize()
         assert torch.equal(out[0], out[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_spread_rows_at_the_ends_of_their_ranges(dtype):
+    """Rows whose passes may be spread: infinite logits, masks of both kinds, and
+    temperatures at which the passes cannot be bounded."""
+    V = 70000
+    x, u = logits(40, 9, V, dtype), [0.7, 0.5, 0.1, 0.9, 0.3, 0.99, 0.0, 0.6, 0.4]
+    x[0, 7] = INF
+    x[1, [3, 1100, 69999]] = INF
+    x[2] = -INF
+    x[2, 66000] = INF
+    x[3] = torch.finfo(DT[dtype]).min
+    x[4, : V - 3] = torch.finfo(DT[dtype]).min
+    x[5] = NAN
+    x[6, ::2] = NAN
+    x[7] = -3.0
+    for p in (0.6, 0.9999, 0.0, [1.0, 0.5] * 4 + [0.7]):
+        check(x, u, top_p=p)
+        check(x, u, top_p=p, min_p=0.2)
+        check(x, u, top_p=p, temperature=[1e-45, 1e-30, 1e-3, 30.0, 1e30, INF, -1.0, NAN, 200.0])
+        check(x, u, top_p=p, temperature=[INF, 1e30, 1e-45, 2.0, 0.5, 1.0, 50.0, 1e-3, INF])
+
+
+def test_most_rows():
+    T = S.SIFAR_ROWS_MAX_TOKENS
+    x = logits(41, T, 3)
+    u = torch.from_numpy(rng(41).random(T).astype(np.float32))
+    x64, at = x.double().cpu(), u.double()
+    out, _ = run(x, u)
+    mass = torch.softmax(x64, -1).cumsum(-1)
+    assert torch.equal(out.cpu().long(), (mass[:, :2] <= at[:, None]).sum(-1))
+    out, _ = run(x, u, top_k=2)
+    least = 2 - x64.flip(-1).argmin(-1, keepdim=True)   # of equal ones, the last leaves
+    mass = torch.softmax(x64.scatter(1, least, -INF), -1).cumsum(-1)
+    want = (mass[:, :2] <= at[:, None]).sum(-1)
+    want = torch.where((want == 2) & (least[:, 0] == 2), 1, want)
+    assert torch.equal(out.cpu().long(), want)
+    out, probs = run(x, u, temperature=0.0)
+    assert torch.equal(out.cpu().long(), x64.argmax(-1)) and (probs == 1).all()
