@@ -32,7 +32,13 @@ SIFAR_HD uint32_t exp2_whole(double magic) {
 SIFAR_HD double exp2_scale(double q, uint32_t i) {
     uint64_t bits;
     __builtin_memcpy(&bits, &q, 8);
-    const uint32_t high = static_cast<uint32_t>(bits >> 32) + (i << 20);
+    uint32_t high = static_cast<uint32_t>(bits >> 32);
+#if defined(__HIP_DEVICE_COMPILE__)
+    // (left to itself the compiler makes two to five instructions on 64 bits of it)
+    asm("v_lshl_add_u32 %0, %1, 20, %0" : "+v"(high) : "v"(i));
+#else
+    high += i << 20;
+#endif
     bits = (static_cast<uint64_t>(high) << 32) | static_cast<uint32_t>(bits);
     __builtin_memcpy(&q, &bits, 8);
     return q;

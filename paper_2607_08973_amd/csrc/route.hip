@@ -65,38 +65,48 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 
 // ---- keys ------------------------------------------------------------------------
 
-// A finite value and an expert as one double that sorts by value (to 2^-42 of it),
-// then by the lower index.
+// All ones for a negative number, by its high word.
+__device__ __forceinline__ uint32_t sign_mask(uint32_t high) {
+    return static_cast<uint32_t>(static_cast<int32_t>(high) >> 31);
+}
+
+// A value and an expert as one finite double that sorts by value (to 2^-42 of it),
+// then by the lower index. -inf, of what is not there, sorts behind every score.
 __device__ __forceinline__ double wide_key(double value, int expert) {
     value = min64(max64(value + 0.0, -kLargest), kLargest);  // -0 counts as 0
     const uint64_t bits = __builtin_bit_cast(uint64_t, value);
+    const uint32_t high = static_cast<uint32_t>(bits >> 32);
     // more mantissa is a larger positive and a smaller negative number
-    const uint64_t code = bits >> 63 ? expert : kIndexMask - expert;
-    return __builtin_bit_cast(double, (bits & ~uint64_t{kIndexMask}) | code);
+    // (past the last expert, where nothing is, an index may not fit)
+    const uint32_t code = (kIndexMask - static_cast<uint32_t>(expert)) ^ sign_mask(high);
+    const uint32_t low = (static_cast<uint32_t>(bits) & ~kIndexMask) | (code & kIndexMask);
+    return __builtin_bit_cast(double, (static_cast<uint64_t>(high) << 32) | low);
 }
 
-// The same as an integer that sorts alike, and never 0.
-__device__ __forceinline__ uint64_t ordered(double key) {
+// The same as an integer that sorts alike, in two words.
+__device__ __forceinline__ void ordered(double key, uint32_t &hi, uint32_t &lo) {
     const uint64_t bits = __builtin_bit_cast(uint64_t, key);
-    return bits >> 63 ? ~bits : bits | uint64_t{1} << 63;
+    const uint32_t high = static_cast<uint32_t>(bits >> 32), sign = sign_mask(high);
+    hi = high ^ (sign | 0x80000000u);
+    lo = static_cast<uint32_t>(bits) ^ sign;
 }
+constexpr uint32_t kNoneHigh = 0x00100000u;  // ordered()'s high word of what is not there
 
 __device__ __forceinline__ int wide_expert(uint32_t low) {  // of ordered()'s low word
     return static_cast<int>(kIndexMask - (low & kIndexMask));
 }
 
-// A finite 16-bit logit and an expert as 32 bits that sort alike. Never 0.
-template <int D>
-__device__ __forceinline__ uint32_t short_key(uint32_t bits, int expert) {
-    bits = bits == 0x8000u ? 0u : bits;  // -0 counts as 0
-    const uint32_t order = bits & 0x8000u ? ~bits & 0xFFFFu : bits | 0x8000u;
-    return order << 16 | (kIndexMask - static_cast<uint32_t>(expert));
+// A logit that was stored in 16 bits, whose ten lowest bits as fp32 are 0, and an
+// expert as 32 bits that sort alike. -inf gives no more than kNoneKey.
+__device__ __forceinline__ uint32_t short_key(float x, int expert) {
+    const uint32_t bits = __float_as_uint(x + 0.0f);  // -0 counts as 0
+    const uint32_t order = bits ^ (sign_mask(bits) | 0x80000000u);
+    return (order & ~kIndexMask) | (kIndexMask - static_cast<uint32_t>(expert));
 }
+constexpr uint32_t kNoneKey = 0x007FFFFFu;
 
-template <int D>
 __device__ __forceinline__ float short_logit(uint32_t key) {
-    const uint32_t order = key >> 16;
-    return widen<D>(order & 0x8000u ? order & 0x7FFFu : ~order & 0xFFFFu);
+    return __uint_as_float((key ^ (~sign_mask(key) | 0x80000000u)) & ~kIndexMask);
 }
 
 __device__ __forceinline__ void exchange(double &hi, double &lo) {
@@ -221,7 +231,7 @@ __global__ void __launch_bounds__(kRowWave *kWaves) route_kernel(const RouteArgs
     if constexpr (SHORT) {
         uint32_t key[EPL];
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) key[j] = x[j] > none ? short_key<D>(raw[j], first + j) : 0u;
+        for (int j = 0; j < EPL; ++j) key[j] = short_key(x[j], first + j);
         sort_descending(key);
         uint32_t found = 0;
         for (int i = 0; i < a.topk; ++i) {
@@ -234,13 +244,12 @@ __global__ void __launch_bounds__(kRowWave *kWaves) route_kernel(const RouteArgs
                 key[EPL - 1] = 0;
             }
         }
-        if (found) {
+        if (found > kNoneKey) {
             id = static_cast<int>(kIndexMask - (found & kIndexMask));
-            chosen = short_logit<D>(found);
+            chosen = short_logit(found);
         }
     } else {
         double value[EPL];
-        bool stay = true;
         if constexpr (RANKED) {
             double b1 = none, b2 = none;
 #pragma unroll
@@ -266,25 +275,24 @@ __global__ void __launch_bounds__(kRowWave *kWaves) route_kernel(const RouteArgs
                     const double other = lane_value(worth, g * n.lanes);
                     better += other > worth || (other == worth && g < group);
                 }
-                stay = better < a.top_groups;
+                if (better >= a.top_groups) {
+                    stay_branch();
+#pragma unroll
+                    for (int j = 0; j < EPL; ++j) x[j] = value[j] = none;
+                }
             }
+        }
+        if (!RANKED || !a.bias) {  // the same order, also where scores saturate
+#pragma unroll
+            for (int j = 0; j < EPL; ++j) value[j] = static_cast<double>(x[j]);
         }
         double key[EPL];
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-            const double v = RANKED && a.bias ? value[j] : static_cast<double>(x[j]);
-            const bool there = RANKED ? stay && value[j] > none : x[j] > none;
-            const double k = wide_key(v, first + j);
-            key[j] = there ? k : none;
-        }
+        for (int j = 0; j < EPL; ++j) key[j] = wide_key(value[j], first + j);
         sort_descending(key);
         uint32_t hi[EPL], lo[EPL];
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-            const uint64_t o = key[j] > none ? ordered(key[j]) : 0;
-            hi[j] = static_cast<uint32_t>(o >> 32);
-            lo[j] = static_cast<uint32_t>(o);
-        }
+        for (int j = 0; j < EPL; ++j) ordered(key[j], hi[j], lo[j]);
         uint32_t found_hi = 0, found_lo = 0;
         for (int i = 0; i < a.topk; ++i) {
             // the high words decide, or now and then the low words among equal ones
@@ -310,7 +318,7 @@ __global__ void __launch_bounds__(kRowWave *kWaves) route_kernel(const RouteArgs
             }
         }
         if constexpr (RANKED) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (found_hi) {
+        if (found_hi > kNoneHigh) {
             id = wide_expert(found_lo);
             if constexpr (RANKED) {
                 const int g = id / n.per, in = id - g * n.per;
@@ -339,8 +347,13 @@ __global__ void __launch_bounds__(kRowWave *kWaves) route_kernel(const RouteArgs
 template <int D, int EPL>
 hipError_t launch_epl(const RouteArgs &n, hipStream_t s) {
     const dim3 grid((n.a.tokens + kWaves - 1) / kWaves), block(kRowWave, kWaves);
-    if (n.a.bias || n.a.groups > 1) route_kernel<D, EPL, true><<<grid, block, 0, s>>>(n);
-    else route_kernel<D, EPL, false><<<grid, block, 0, s>>>(n);
+    if constexpr (EPL <= SIFAR_ROUTE_MAX_EXPERTS / kRowWave) {  // more only with groups
+        if (!n.a.bias && n.a.groups == 1) {
+            route_kernel<D, EPL, false><<<grid, block, 0, s>>>(n);
+            return hipGetLastError();
+        }
+    }
+    route_kernel<D, EPL, true><<<grid, block, 0, s>>>(n);
     return hipGetLastError();
 }
 

@@ -103,6 +103,13 @@ __device__ __forceinline__ float max32(float a, float b) {
     return r;
 }
 
+// The same of three.
+__device__ __forceinline__ float max32(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // How a row is drawn.
 struct Draw {
     float temperature, top_p, min_p;
@@ -255,15 +262,17 @@ __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const Sample
     if (first >= n.chunks) return;
     const Draw d = draw_of(a, t);
     const Stored<D> *row = static_cast<const Stored<D> *>(a.logits) + t * a.logits_stride;
-    Raw x[kBatch];
-    float top[kBatch];
+    Raw raw[kBatch];
+    float x[kBatch][kVec<D>], top[kBatch];
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b) x[b] = load_chunk<D>(row, a.vocab, first + b, lane);
+    for (int b = 0; b < kBatch; ++b) raw[b] = load_chunk<D>(row, a.vocab, first + b, lane);
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
         top[b] = -__builtin_inff();
 #pragma unroll
-        for (int i = 0; i < kVec<D>; ++i) top[b] = max32(top[b], quiet_logit<D>(x[b], i));
+        for (int i = 0; i < kVec<D>; ++i) x[b][i] = quiet_logit<D>(raw[b], i);
+#pragma unroll
+        for (int i = 0; i < kVec<D>; i += 2) top[b] = max32(top[b], x[b][i], x[b][i + 1]);
     }
     const float mine = wave_reduce4(top, Max32{});
     const int c = first + (lane >> 4);
@@ -285,18 +294,17 @@ __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const Sample
 #pragma unroll
                 for (int i = 0; i < kVec<D>; ++i)
                     sum[b] += exp2_quick<0>(
-                        static_cast<double>(max32(quiet_logit<D>(x[b], i), least)) - max, scale);
+                        static_cast<double>(max32(x[b][i], least)) - max, scale);
             } else {  // a temperature or a maximum for which no logit lies at the cut
 #pragma unroll
                 for (int i = 0; i < kVec<D>; ++i) {
-                    const float l = quiet_logit<D>(x[b], i);
-                    sum[b] += exp2_quick<0>(static_cast<double>(max32(l, least)) - max, scale,
-                                            l >= least);
+                    sum[b] += exp2_quick<0>(static_cast<double>(max32(x[b][i], least)) - max,
+                                            scale, x[b][i] >= least);
                 }
             }
         } else {  // they share the weight
 #pragma unroll
-            for (int i = 0; i < kVec<D>; ++i) sum[b] += logit<D>(x[b], i) == m ? 1.0 : 0.0;
+            for (int i = 0; i < kVec<D>; ++i) sum[b] += x[b][i] == m ? 1.0 : 0.0;
         }
     }
     const double all = wave_reduce4(sum, Add{});

@@ -33,7 +33,7 @@ def resources(source, tmp):
 
 
 @pytest.mark.parametrize("source,kernels,vgprs", [
-    ("block_norm.hip", 20, 128), ("route.hip", 36, 256), ("sample.hip", 12, 128),
+    ("block_norm.hip", 20, 128), ("route.hip", 33, 256), ("sample.hip", 12, 128),
 ])
 def test_registers(source, kernels, vgprs, tmp_path):
     found = resources(source, tmp_path)
