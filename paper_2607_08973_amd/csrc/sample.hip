@@ -76,14 +76,16 @@ struct SampleArgs {
     int32_t groups;  // workgroups of a row
 };
 
-// Order-preserving 32 bits of a number. -0 counts as 0.
+// Order-preserving 32 bits of a number: a negative one's turned over, others' sign bit
+// set. -0 counts as 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);
-    return u >> 31 ? ~u : u | 0x80000000u;
+    return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
 
 __device__ __forceinline__ float value_of(uint32_t key) {
-    return __uint_as_float(key >> 31 ? key & 0x7FFFFFFFu : ~key);
+    return __uint_as_float(
+        key ^ (static_cast<uint32_t>(static_cast<int32_t>(~key) >> 31) | 0x80000000u));
 }
 
 constexpr uint32_t kLowestKey = 0x00800000u;  // of the lowest finite fp32
@@ -415,8 +417,10 @@ struct Row {
     }
     // Of a kept weight at least one, so that what may be drawn can be.
     __device__ __forceinline__ uint64_t units(uint32_t key) const {
+        return units_of(value_of(key));
+    }
+    __device__ __forceinline__ uint64_t units_of(float x) const {
         if (!finite) return uint64_t{1} << kUnitBits;  // the same in every lane
-        const float x = value_of(key);
         const uint64_t u = units_near(max32(x, one), x >= one) - kUnitBase;
         return u | (x >= one ? 0 : 1);
     }
@@ -551,7 +555,7 @@ __device__ __forceinline__ void to_list(Shared &s, const Raw &x, int c, float lo
 #pragma unroll
     for (int i = 0; i < kVec<D>; ++i) {
         if (!in[i]) continue;  // the same in every lane
-        if (logit<D>(x, i) >= low && logit<D>(x, i) <= high) {
+        if (__builtin_amdgcn_inverse_ballot_w64(in[i])) {
             const uint32_t place =
                 at + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(in[i] >> 32),
                                                __builtin_amdgcn_mbcnt_lo(
@@ -1272,7 +1276,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
 #pragma unroll
                 for (int i = 0; i < kVec<D>; ++i) {
                     const float l = logit<D>(x, i);
-                    if (l > low) sum += r.units(key_of(l));
+                    if (l > low) sum += r.units_of(l);
                     sum += l == low ? uint64_t{1} << 54 : 0;
                 }
                 return sum;
@@ -1344,7 +1348,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
         const bool tie = l == low_kept;
         const bool in = l > low_kept || (tie && rank < keep.ties);
         rank += tie;
-        w[i] = in ? r.units(key_of(l)) : 0;
+        w[i] = in ? r.units_of(l) : 0;
         sum += w[i];
     }
     uint64_t low = wave_scan(sum) - sum;
