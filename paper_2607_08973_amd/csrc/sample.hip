@@ -18,7 +18,10 @@
 // the neighbour.
 //
 // Bound: the 64-bit exponentials for many rows, latency of the two launches and
-// of pick_kernel's barriers and loads for a few.
+// of pick_kernel's barriers and loads for a few. Measured: 256 x 151936 bf16 (15 us at
+// a copy's rate) scan 34 us, pick 85 for flat rows under top-p, of which 18 go to the
+// window's histogram and 47 to the exact pass; 8 x 128256 fp32 under every filter 14
+// us a call, 1 x 32000 without one 8 in a graph.
 #include <hip/hip_runtime.h>
 
 #include "exp2.h"

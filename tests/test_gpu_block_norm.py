@@ -286,3 +286,12 @@ def test_most_rows():
     i = inputs(60, S.SIFAR_ROWS_MAX_TOKENS, 8, "bf16", gate="channel")
     out, y = run(i)
     check_run(i, out, y)
+
+
+@pytest.mark.parametrize("H", [6136, 6144, 8192, 12288, 16384])
+@pytest.mark.parametrize("parts", [1, 2])
+def test_rows_of_many_lanes(H, parts):
+    """Around the lengths from which one partial's rows take fewer lanes."""
+    i = inputs(61, 3, H, "bf16", "fp32", parts=parts, gate="token")
+    out, y = run(i)
+    check_run(i, out, y)
