@@ -719,11 +719,12 @@ __device__ __forceinline__ uint64_t share(float part, uint64_t all) {
     return static_cast<double>(t) < p ? t + 1 : t;
 }
 
-// The place of a random number in [0, all).
+// The place of a random number in [0, all); the last one from 1 on. (1.0 times `all`, which
+// a double need not hold to the unit, would be a place before the last tokens.)
 __device__ __forceinline__ uint64_t place(float u, uint64_t all) {
-    const uint64_t at = u > 0.0f ? static_cast<uint64_t>(static_cast<double>(u < 1.0f ? u : 1.0f) *
-                                                         static_cast<double>(all))
-                                 : 0;
+    if (u >= 1.0f) return all - 1;
+    const uint64_t at =
+        u > 0.0f ? static_cast<uint64_t>(static_cast<double>(u) * static_cast<double>(all)) : 0;
     return at < all ? at : all - 1;
 }
 
