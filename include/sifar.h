@@ -644,9 +644,14 @@ int sifar_route(const sifar_route_args *a, void *stream);
  * are +inf, they share the weight. uniform belongs in [0, 1); below 0 or NaN
  * counts as 0, and 1 or above draws the last token kept.
  *
- * Sums are exact integers in units of 2^-42 of the largest weight, so the token
+ * Weights are added as whole numbers of units of 2^-42 of the largest, so the token
  * does not depend on the order of addition: ranks that hold equal logits draw
- * equal tokens from equal random numbers.
+ * equal tokens from equal random numbers. Under a filter each weight is rounded to
+ * units, a kept one to one at least. In a row without filters, and for the whole that
+ * top-p takes its share of where there is no top-k, it is the sum of each 256 adjacent
+ * logits (512 of 16 bits), added in 64 bits in a fixed order, and the tokens
+ * of a run share its units by their weights. So a border between two tokens lies
+ * within a unit for each token before it.
  *
  *   logits    [tokens][vocab] dtype, rows logits_stride elements apart
  *   uniform, temperature, top_k, top_p, min_p   [tokens] fp32 (top_k: int32);

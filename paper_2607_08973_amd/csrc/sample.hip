@@ -12,10 +12,12 @@
 //
 // Weights w = 2^((x - max) log2(e) / temperature) are 64-bit values rounded to
 // units of 2^-42 and added as integers: sums do not depend on the order of
-// addition, so histograms may be filled by atomics, and a border between two
-// tokens is off by 2^-43 a token at most. In 32 bits, where a running sum is off by
-// some 1e-8, one draw in a thousand from a flat row of 100000 tokens would land on
-// the neighbour.
+// addition, so histograms may be filled by atomics. A kept token counts one unit at
+// least, so a border between two tokens is off by up to a unit for each before it (half
+// a unit by rounding, 0.2 by the exponential). Without a filter it is a chunk's sum that
+// is rounded to units, and the chunk's tokens share it. In 32 bits, where a running sum
+// is off by some 1e-8, one draw in a thousand from a flat row of 100000 tokens would
+// land on the neighbour.
 //
 // Bound: the 64-bit exponentials for many rows, latency of the two launches and
 // of pick_kernel's barriers and loads for a few. Measured: 256 x 151936 bf16 (15 us at
@@ -719,13 +721,20 @@ __device__ __forceinline__ uint64_t share(float part, uint64_t all) {
     return static_cast<double>(t) < p ? t + 1 : t;
 }
 
-// The place of a random number in [0, all); the last one from 1 on. (1.0 times `all`, which
-// a double need not hold to the unit, would be a place before the last tokens.)
-__device__ __forceinline__ uint64_t place(float u, uint64_t all) {
-    if (u >= 1.0f) return all - 1;
-    const uint64_t at =
-        u > 0.0f ? static_cast<uint64_t>(static_cast<double>(u) * static_cast<double>(all)) : 0;
-    return at < all ? at : all - 1;
+// The place of a random number in [0, all), and the part of a unit behind it; from 1 on the
+// end of the last one. (1.0 times `all`, which a double need not hold to the unit, would
+// be a place before the last tokens.)
+struct Place {
+    uint64_t at;
+    double part;
+};
+__device__ __forceinline__ Place place(float u, uint64_t all) {
+    if (!(u >= 1.0f)) {
+        const double p = u > 0.0f ? static_cast<double>(u) * static_cast<double>(all) : 0.0;
+        const uint64_t at = static_cast<uint64_t>(p);
+        if (at < all) return Place{at, p - static_cast<double>(at)};
+    }
+    return Place{all - 1, 1.0};
 }
 
 // The fewest in order from `top` whose sum reaches target, of what `keep` leaves
@@ -930,7 +939,7 @@ __device__ __forceinline__ void draw_small(Shared &s, const Row<D> &r, const Dra
         if (sum) add(s.sums[e], sum);
     }
     __syncthreads();
-    const uint64_t at = place(u, all);
+    const uint64_t at = place(u, all).at;
     if (in && s.sums[tid] <= at && at < s.sums[tid] + w) {
         *out = static_cast<int32_t>(~static_cast<uint32_t>(mine));
         if (prob) {
@@ -1314,7 +1323,8 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     }
     uint64_t all;
     const uint64_t before = block_scan(s, units, all);
-    const uint64_t at = place(u, all);
+    const Place target = place(u, all);
+    const uint64_t at = target.at;
     if (units && before <= at && at < before + units) {
         uint64_t run = before;
         run_ties = ties_before;
@@ -1334,9 +1344,18 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     __syncthreads();
     if (wave != 0) return;
 
-    // The token inside the chunk: which lane, then which of its logits.
+    // The token inside the chunk: which lane, then which of its logits. The sum of a chunk
+    // of a row without filters came from the scan, rounded to units once, so its tokens
+    // share it: by weights in units of 2^-42 of the chunk's maximum, the place in
+    // proportion. In the row's units each would count one at least, and a chunk of light
+    // tokens would end before its heavy ones.
     const int c = __builtin_amdgcn_readfirstlane(s.chosen);
-    const uint64_t want = s.chosen_at;
+    Row<D> inside = r;
+    if (plain && r.finite) {  // the same in every lane
+        inside.max64 = static_cast<double>(value_of(s.chunk_key[c]));
+        inside.one = value_of(key_from(inside.max64 - kUnitBits * kLn2 *
+                                                          static_cast<double>(d.temperature)));
+    }
     const Raw x = load_chunk<D>(r.logits, r.vocab, c, lane);
     const float low_kept = value_of(keep.key);
     uint64_t w[kVec<D>], sum = 0, rank = s.chosen_ties;
@@ -1352,21 +1371,27 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
         const bool tie = l == low_kept;
         const bool in = l > low_kept || (tie && rank < keep.ties);
         rank += tie;
-        w[i] = in ? r.units_of(l) : 0;
+        w[i] = in ? inside.units_of(l) : 0;
         sum += w[i];
     }
-    uint64_t low = wave_scan(sum) - sum;
-    int here = -1, last = -1;
+    const uint64_t through = wave_scan(sum);
+    uint64_t want = s.chosen_at;
+    if (plain) {
+        const uint64_t whole = lane_value(through, 63);
+        const double share = static_cast<double>(whole) / static_cast<double>(s.chunk_units[c]);
+        want = static_cast<uint64_t>((static_cast<double>(want) + target.part) * share);
+        want = want < whole ? want : whole - 1;
+    }
+    uint64_t low = through - sum;
+    int here = -1;
 #pragma unroll
     for (int i = 0; i < kVec<D>; ++i) {
         if (w[i] && low <= want && want < low + w[i]) here = i;
-        if (w[i]) last = i;
         low += w[i];
     }
-    // past the last weight, where the chunk's own sum was rounded up
-    const uint64_t hit = __ballot(here >= 0), any = __ballot(last >= 0);
-    const int from_lane = hit ? __builtin_ctzll(hit) : any ? 63 - __builtin_clzll(any) : 0;
-    const int i = lane_value(hit ? here : last, from_lane);
+    const uint64_t hit = __ballot(here >= 0);  // one lane: want is below the chunk's sum
+    const int from_lane = hit ? __builtin_ctzll(hit) : 0;
+    const int i = lane_value(here, from_lane);
     const int token = c * kChunkOf<D> + from_lane * kVec<D> + (i < 0 ? 0 : i);
     if (lane == 0) {
         a.out[t] = token;
