@@ -464,8 +464,9 @@ _F32 = _I32 = _U8 = _C = None  # of torch, once a row operator was called
 def _torch() -> None:
     global _DTYPES, _F32, _I32, _U8, _C
     import torch
-    _F32, _I32, _U8, _C = torch.float32, torch.int32, torch.uint8, torch._C
     _DTYPES = {torch.bfloat16: SIFAR_BF16, torch.float16: SIFAR_FP16, torch.float32: SIFAR_FP32}
+    _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
+    _C = torch._C  # last: callers on other threads look at it alone
 
 
 def _refuse(fn: str, why: str):
