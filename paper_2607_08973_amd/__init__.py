@@ -457,6 +457,7 @@ def sifar_allreduce_noalloc(src, src_rank_stride: int, nranks: int, tokens: int,
 _BLOCK_NORM = struct.Struct("@5i4fP2q2PqPqPq2Pq")
 _ROUTE = struct.Struct("@9if1Pq3P")
 _SAMPLE = struct.Struct("@3iPq8Pq")
+_UNPACKABLE = (struct.error, OverflowError)  # no such number in the struct's field
 _DTYPES = None  # torch dtype -> SIFAR_* element type
 _F32 = _I32 = _U8 = _C = None  # of torch, once a row operator was called
 
@@ -554,11 +555,14 @@ def sifar_block_norm(x, residual, residual_out, post_weight=None, gate=None, nor
     if (norm_weight is None) != (y is None):
         _refuse(fn, "norm_weight and y go together")
     code = _dtype(fn, dt)
-    rc = (_lib or load()).sifar_block_norm(
-        _BLOCK_NORM.pack(code, code if rdt is dt else _dtype(fn, rdt), T, H, parts, branch_scale,
-                         residual_scale, weight_offset, eps, x.data_ptr(), at[0], part_stride,
-                         post, g, g_stride, res, res_stride, out, out_stride, norm, yp, y_stride),
-        _row_stream(stream, dev))
+    try:
+        args = _BLOCK_NORM.pack(
+            code, code if rdt is dt else _dtype(fn, rdt), T, H, parts, branch_scale,
+            residual_scale, weight_offset, eps, x.data_ptr(), at[0], part_stride, post, g,
+            g_stride, res, res_stride, out, out_stride, norm, yp, y_stride)
+    except _UNPACKABLE as e:
+        _refuse(fn, f"a scale, the offset or eps: {e}")
+    rc = (_lib or load()).sifar_block_norm(args, _row_stream(stream, dev))
     if rc:
         _check(fn, rc)
 
@@ -589,9 +593,13 @@ def sifar_route(logits, ids, weights, score="softmax", bias=None, groups=1, top_
     mode = ROUTE_SCORE.get(score, score)
     if mode not in (SIFAR_ROUTE_SOFTMAX, SIFAR_ROUTE_SIGMOID):
         _refuse(fn, f"no score {score!r}")
-    rc = (_lib or load()).sifar_route(
-        _ROUTE.pack(_dtype(fn, logits.dtype), T, E, k, mode, groups, top_groups, group_top,
-                    1 if renorm else 0, scale, x, x_stride, b, i, w), _row_stream(stream, dev))
+    code = _dtype(fn, logits.dtype)
+    try:
+        args = _ROUTE.pack(code, T, E, k, mode, groups, top_groups, group_top,
+                           1 if renorm else 0, scale, x, x_stride, b, i, w)
+    except _UNPACKABLE as e:
+        _refuse(fn, f"the groups or the scale: {e}")
+    rc = (_lib or load()).sifar_route(args, _row_stream(stream, dev))
     if rc:
         _check(fn, rc)
 

@@ -1,5 +1,5 @@
-"""The row operators' binding, beside what test_*_refusals.py cover: its first calls from
-several threads. No GPU is used."""
+"""The row operators' binding, beside what test_*_refusals.py cover: values that
+no struct of the library holds and first calls from several threads. No GPU is used."""
 from __future__ import annotations
 
 import threading
@@ -58,6 +58,27 @@ def test_plain_calls(library):
     route()
     sample()
     assert library.calls == 3
+
+
+@pytest.mark.parametrize("call,kw", [
+    (norm, dict(eps=1e39)), (norm, dict(branch_scale=-1e39)), (norm, dict(residual_scale=1e300)),
+    (norm, dict(weight_offset=1e39)), (norm, dict(eps=None)), (norm, dict(branch_scale="1")),
+    (route, dict(scale=1e39)), (route, dict(scale=None)), (route, dict(groups=1 << 31)),
+    (route, dict(groups=-(1 << 40))), (route, dict(top_groups=1 << 64)),
+    (route, dict(group_top=1.5)), (route, dict(groups=None)),
+])
+def test_values_that_no_struct_holds(library, call, kw):
+    with pytest.raises(S.SifarError) as e:
+        call(**kw)
+    assert e.value.code == S.SIFAR_EINVAL and not library.calls
+    assert str(e.value).startswith("sifar_" + ("block_norm" if call is norm else "route"))
+
+
+@pytest.mark.parametrize("eps", [0.0, 3.4e38, 1e-45])
+def test_values_at_the_ends_of_their_range(library, eps):
+    norm(eps=eps)
+    route(scale=-eps)
+    assert library.calls == 2
 
 
 class Torch:
