@@ -451,11 +451,13 @@ def sifar_allreduce_noalloc(src, src_rank_stride: int, nranks: int, tokens: int,
 
 
 # ---- row operators: tensors in, shapes and strides taken from them ----------
-# Their arguments are packed in one call each (the structs above, in native
-# layout): filling a ctypes structure of 22 fields takes longer than the launch.
+# Their arguments are packed in one call each (the structs above): filling a
+# ctypes structure of 22 fields takes longer than the launch. Those with floats are
+# spelled out in standard layout, which refuses a number that is finite and not an
+# fp32's; native layout makes an infinity of it.
 
-_BLOCK_NORM = struct.Struct("@5i4fP2q2PqPqPq2Pq")
-_ROUTE = struct.Struct("@9if1Pq3P")
+_BLOCK_NORM = struct.Struct("<5i4f4xQ2q2QqQqQq2Qq")
+_ROUTE = struct.Struct("<9ifQq3Q")
 _SAMPLE = struct.Struct("@3iPq8Pq")
 _UNPACKABLE = (struct.error, OverflowError)  # no such number in the struct's field
 _DTYPES = None  # torch dtype -> SIFAR_* element type
