@@ -609,8 +609,8 @@ def sifar_route(logits, ids, weights, score="softmax", bias=None, groups=1, top_
 def sifar_sample_workspace(tokens: int, vocab: int) -> int:
     """Bytes of workspace that sifar_sample needs."""
     fn = "sifar_sample_workspace"
-    if tokens > SIFAR_ROWS_MAX_TOKENS or vocab > SIFAR_SAMPLE_MAX_VOCAB:
-        _refuse(fn, f"{tokens} x {vocab} is too large")
+    if not (0 <= tokens <= SIFAR_ROWS_MAX_TOKENS and 0 < vocab <= SIFAR_SAMPLE_MAX_VOCAB):
+        _refuse(fn, f"no rows of {tokens} x {vocab}")
     n = load().sifar_sample_workspace(tokens, vocab)
     if n < 0:
         _check(fn, n)

@@ -81,6 +81,16 @@ def test_values_at_the_ends_of_their_range(library, eps):
     assert library.calls == 2
 
 
+@pytest.mark.parametrize("tokens,vocab", [
+    (-(1 << 32) + 5, 100), (5, -(1 << 32) + 100), (-(1 << 40), 5), (-(1 << 64), 5), (5, -(1 << 31)),
+])
+def test_workspace_of_sizes_below_32_bits(tokens, vocab):
+    """Not taken for the sizes that their low 32 bits spell."""
+    with pytest.raises(S.SifarError) as e:
+        S.sifar_sample_workspace(tokens, vocab)
+    assert e.value.code == S.SIFAR_EINVAL
+
+
 class Torch:
     """torch, as two threads see it that call at once: the second one calls while the
     first looks up its types."""
