@@ -502,6 +502,8 @@ def _row_stream(stream, dev: int):
 def _operand(fn: str, name: str, t, dtype, shape, dev: int):
     """Address and leading stride of t, which has to be `dtype` of `shape` on
     device `dev` with adjacent elements: the library sees addresses only."""
+    if t is None:
+        _refuse(fn, f"no {name}")
     if t.dtype is dtype and t.shape == shape and t.get_device() == dev:
         if t.is_contiguous():
             return t.data_ptr(), shape[-1]
@@ -521,6 +523,8 @@ def sifar_block_norm(x, residual, residual_out, post_weight=None, gate=None, nor
     fn = "sifar_block_norm"
     if _C is None:
         _torch()
+    if x is None or residual_out is None:
+        _refuse(fn, "no x" if x is None else "no residual_out")
     shape, at = x.shape, x.stride()
     if len(shape) == 2:
         parts, part_stride = 1, 0
@@ -534,8 +538,6 @@ def sifar_block_norm(x, residual, residual_out, post_weight=None, gate=None, nor
         _refuse(fn, f"{parts} x {T} x {H} is too large")
     if at[1] != 1 and H > 1:
         _refuse(fn, "the elements of x's rows are not adjacent")
-    if residual_out is None:
-        _refuse(fn, "no residual_out")
     dev = _gpu(fn, "x", x)
     dt, rdt, vec = x.dtype, residual_out.dtype, shape[1:]
     out, out_stride = _operand(fn, "residual_out", residual_out, rdt, shape, dev)
@@ -576,6 +578,8 @@ def sifar_route(logits, ids, weights, score="softmax", bias=None, groups=1, top_
     fn = "sifar_route"
     if _C is None:
         _torch()
+    if logits is None or ids is None:
+        _refuse(fn, "no logits" if logits is None else "no ids")
     if logits.dim() != 2 or ids.dim() != 2:
         _refuse(fn, "logits or ids do not have 2 dimensions")
     shape, out = logits.shape, ids.shape
@@ -625,6 +629,8 @@ def sifar_sample(logits, uniform, out, workspace, probs=None, temperature=None, 
     fn = "sifar_sample"
     if _C is None:
         _torch()
+    if logits is None or workspace is None:
+        _refuse(fn, "no logits" if logits is None else "no workspace")
     shape = logits.shape
     if len(shape) != 2:
         _refuse(fn, f"logits has {len(shape)} dimensions, not 2")

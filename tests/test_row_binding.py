@@ -81,6 +81,16 @@ def test_values_at_the_ends_of_their_range(library, eps):
     assert library.calls == 2
 
 
+@pytest.mark.parametrize("call,name", [
+    (norm, "x"), (norm, "residual_out"), (route, "logits"), (route, "ids"), (route, "weights"),
+    (sample, "logits"), (sample, "uniform"), (sample, "out"), (sample, "workspace"),
+])
+def test_operands_that_are_missing(library, call, name):
+    with pytest.raises(S.SifarError) as e:
+        call(**{name: None})
+    assert e.value.code == S.SIFAR_EINVAL and f"no {name}" in str(e.value) and not library.calls
+
+
 @pytest.mark.parametrize("tokens,vocab", [
     (-(1 << 32) + 5, 100), (5, -(1 << 32) + 100), (-(1 << 40), 5), (-(1 << 64), 5), (5, -(1 << 31)),
 ])
