@@ -426,8 +426,8 @@ struct Row {
     }
     __device__ __forceinline__ uint64_t units_of(float x) const {
         if (!finite) return uint64_t{1} << kUnitBits;  // the same in every lane
-        const uint64_t u = units_near(max32(x, one), x >= one) - kUnitBase;
-        return u | (x >= one ? 0 : 1);
+        const uint64_t u = units_near(x) - kUnitBase;
+        return u ? u : 1;
     }
 };
 
@@ -1351,11 +1351,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(const SampleArgs n) {
     // tokens would end before its heavy ones.
     const int c = __builtin_amdgcn_readfirstlane(s.chosen);
     Row<D> inside = r;
-    if (plain && r.finite) {  // the same in every lane
-        inside.max64 = static_cast<double>(value_of(s.chunk_key[c]));
-        inside.one = value_of(key_from(inside.max64 - kUnitBits * kLn2 *
-                                                          static_cast<double>(d.temperature)));
-    }
+    if (plain) inside.max64 = static_cast<double>(value_of(s.chunk_key[c]));
     const Raw x = load_chunk<D>(r.logits, r.vocab, c, lane);
     const float low_kept = value_of(keep.key);
     uint64_t w[kVec<D>], sum = 0, rank = s.chosen_ties;
