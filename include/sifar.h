@@ -581,11 +581,13 @@ int sifar_block_norm(const sifar_block_norm_args *a, void *stream);
  *   weights  = s of the chosen (without the bias), divided by their sum if
  *              renorm (0 where the sum is 0), times scale
  *
- * Ties go to the lowest index, of experts and of groups (values of c that agree
- * to 2^-42 of themselves count as equal). An expert is not there for a token
- * whose logit is -inf or NaN, or whose c is -inf or NaN: it is never chosen,
- * and its group's worth counts the others (best two: the one, if there is only
- * one). Where fewer than topk are left, the rest of ids is -1 with weight 0.
+ * Ties go to the lowest index, of experts and of groups. Experts' c are compared
+ * without the ten lowest of their 53 bits, in steps of 2^-42 of themselves or less:
+ * two within a step tie, two that a step's edge parts do not, however close. Groups'
+ * worths are compared as 64-bit numbers. An expert is not there for a token whose
+ * logit is -inf or NaN, or whose c is -inf or NaN: it is never chosen, and its group's
+ * worth counts the others (best two: the one, if there is only one). Where fewer than
+ * topk are left, the rest of ids is -1 with weight 0.
  * Logits of the type's lowest finite value are ordinary logits. Where logits are
  * +inf, softmax shares 1 among them.
  *

@@ -73,8 +73,9 @@ __device__ __forceinline__ uint32_t sign_mask(uint32_t high) {
     return static_cast<uint32_t>(static_cast<int32_t>(high) >> 31);
 }
 
-// A value and an expert as one finite double that sorts by value (to 2^-42 of it),
-// then by the lower index. -inf, of what is not there, sorts behind every score.
+// A value and an expert as one finite double that sorts by value, without its ten
+// lowest bits (in steps of 2^-42 of it or less), then by the lower index. -inf, of what
+// is not there, sorts behind every score.
 __device__ __forceinline__ double wide_key(double value, int expert) {
     value = min64(max64(value + 0.0, -kLargest), kLargest);  // -0 counts as 0
     const uint64_t bits = __builtin_bit_cast(uint64_t, value);
