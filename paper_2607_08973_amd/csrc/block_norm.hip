@@ -5,10 +5,11 @@
 // sum of its partials) for the post-norm, r' = the new residual for the next
 // block's norm. Both passes run on registers: a workgroup holds one row, eight
 // adjacent elements a lane and vector, so each input is read and each output
-// written once. Bound: HBM bytes for many rows; for a few rows the launch, one
-// memory round trip and two workgroup reductions. Measured: 4096 x 5120 bf16 with an
-// fp32 residual 48.0 us a call, 5.2 TB/s, the rate of a copy; in a graph 64 x 8192 over 8
-// partials 5.5 us and 1 x 4096 3.0.
+// written once. Bound: HBM bytes for many rows; for a few rows the launch, two
+// workgroup reductions and dependent memory round trips: the row, each further
+// partial, and the norm's weights behind the second reduction. Measured: 4096 x 5120
+// bf16 with an fp32 residual 47.8 us a call, 5.3 TB/s, the rate of a copy; in a graph
+// 64 x 8192 over 8 partials 5.6 us and 1 x 4096 3.0.
 #include <hip/hip_runtime.h>
 
 #include "rows.h"
@@ -49,8 +50,9 @@ __global__ void __launch_bounds__(kMaxThreads) block_norm_kernel(const NormArgs 
     const bool posted = a.post_weight != nullptr;
     const bool added = a.residual != nullptr;
 
-    // Up to two vectors a lane, everything the row needs is loaded before the
-    // first reduction; longer rows would spill, and load as they go.
+    // Up to two vectors a lane, the post-norm's weights, gate and residual are loaded
+    // before the first reduction; longer rows load them a vector at a time, where they
+    // are used. (The next norm's weights are loaded where they are used in any row.)
     constexpr bool AHEAD = V <= 2;
     int h[V];
     bool on[V];
@@ -72,8 +74,9 @@ __global__ void __launch_bounds__(kMaxThreads) block_norm_kernel(const NormArgs 
         if (gated) gate[v] = load8<D>(a.gate, t * a.gate_stride + h[v]);
         if (added) res[v] = load8<R>(a.residual, t * a.residual_stride + h[v]);
     }
-    // The other partials, up to seven in flight: one after the other each would cost a
-    // memory round trip. (Long rows have enough vectors of one partial for that.)
+    // The other partials. Each load stands under a condition of its own, and the
+    // compiler waits for one before it issues the next: a memory round trip each,
+    // whatever FLIGHT says (1 x 8192 in a graph 4.0 us of one partial, 5.4 of eight).
     constexpr int FLIGHT = V == 1 ? kMaxParts - 1 : V == 2 ? 2 : 1;
     for (int p = 1; p < a.parts; p += FLIGHT) {
         if constexpr (AHEAD) {
@@ -151,11 +154,18 @@ template <int D, int R>
 hipError_t launch_norm(const sifar_block_norm_args &a, hipStream_t s) {
     // Vectors of 8 a lane: as few as 1024 lanes allow. A row of one partial that would take
     // 768 lanes or more takes half of them with twice the vectors, so that another row's
-    // workgroup loads while its waves wait for each other (us a call in a graph, bf16:
-    // 4096 x 8192 43.5 and 39.3, 1 x 8192 3.8 and 3.7; 4096 x 16384 103 and 77, 1 x 16384
-    // 5.0 and 5.6; at 640 lanes 4096 x 5120 39.4 and 42.4). Over several partials more
-    // lanes keep more loads in flight (64 x 8192 over 8 partials 5.5 and 6.1). The batch
-    // has no say: a row's sums do not depend on it.
+    // workgroup loads while its waves wait for each other. us a call in a graph, bf16, with
+    // the fewest vectors and with twice as many, for 1, 512 and 4096 rows:
+    //    5632 (704 lanes)   3.1 3.5   5.0  5.1    32  28     not by the rule
+    //    6144 (768)         3.2 3.5   5.0  5.2    32  30
+    //    7168 (896)         3.7 3.6   6.1  5.5    43  35
+    //    8192 (1024)        3.8 3.7   6.2  5.7    44  40
+    //   12288 (768 x 2)     4.0 5.4   7.3  7.9    57  58
+    //   16384 (1024 x 2)    5.0 5.6  12.4 10.1   104  79
+    // (4096 x 5120 with an fp32 residual 39.4 and 42.4.) So the longest rows of each kind
+    // gain where there are many, and the edge itself costs a few rows a tenth. Over
+    // several partials more lanes keep more loads in flight (64 x 8192 over 8 partials
+    // 5.5 and 6.1). The batch has no say: a row's sums do not depend on it.
     const int vecs = a.hidden / 8;
     int V = vecs <= kMaxThreads ? 1 : vecs <= 2 * kMaxThreads ? 2 : vecs <= 4 * kMaxThreads ? 4 : 8;
     if (a.parts == 1 && V <= 2 && vecs >= 768 * V) V *= 2;

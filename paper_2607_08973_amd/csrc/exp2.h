@@ -64,8 +64,7 @@ SIFAR_HD double exp2_64(double t) {
 
 // 2^(y c + BITS) for y c in [-1000, 0], relative error below 4e-14: for sums in
 // units of 2^-42. Below 2^-900 where it is not kept: one select, of the exponent, does
-// for both words (each further one from a comparison costs gfx950 four times the
-// first).
+// for both words.
 template <int BITS>
 SIFAR_HD double exp2_quick(double y, double c, bool keep = true) {
     constexpr double s = static_cast<double>(1ull << BITS);

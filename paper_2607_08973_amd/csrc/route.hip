@@ -12,10 +12,12 @@
 // logits' own order is the answer, and 16-bit logits fit a 32-bit key together with
 // the index.
 //
-// Bound: for many tokens the instructions of the sort and of the k steps; for one
-// token their latency. Measured, in a graph: 16384 x 512 bf16 softmax, top 10, 12.1 us
-// (3.7 at a copy's rate; in fp32, by 64-bit keys, 15.6), 8192 x 256 with bias and groups, top 8, 11.5 (1.7), one
-// token of it 4.4.
+// Bound: for many tokens the vector instructions of the sort and of the k steps (486 a
+// token for 512 experts of 16 bits, 782 for 256 with bias and groups; at four cycles
+// each they fill the SIMDs for all of the kernel's time); for one token their latency.
+// Measured, in a graph: 16384 x 512 bf16 softmax, top 10, 12.1 us (3.7 at a copy's
+// rate; in fp32, by 64-bit keys, 15.6), 8192 x 256 with bias and groups, top 8, 11.5
+// (1.7), one token of it 4.4.
 #include <hip/hip_runtime.h>
 
 #include "exp2.h"

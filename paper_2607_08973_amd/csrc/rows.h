@@ -172,11 +172,10 @@ __device__ __forceinline__ T choose(bool c, T a, T b) {
     return c ? static_cast<T>(a) : static_cast<T>(b);
 }
 
-// Keeps the branch that it stands in from becoming selects. On gfx950 the first
-// v_cndmask after its comparison issues in 4 cycles and each further one from the
-// same vcc in about 20 (one comparison and eight selects: 138 cycles a wave, 39 with
-// the mask in other scalar registers), so several values under one condition are
-// moved in a branch.
+// Keeps the branch that it stands in from becoming selects. On gfx950 a comparison and
+// the v_cndmasks that read its vcc take a SIMD 9 cycles a wave for one, 14 for two and
+// 138 for eight (39 in the 64-bit encoding, or with the mask in other scalar
+// registers), so several values under one condition are moved in a branch.
 __device__ __forceinline__ void stay_branch() { asm volatile(""); }
 
 struct Add {

@@ -8,7 +8,8 @@
 // chunks whose maximum says that they hold something to keep. A nucleus of many
 // tokens takes two more passes over its row, which a workgroup makes in 60 us for
 // 128256 logits; where few rows would leave the GPU idle meanwhile, two launches
-// between spread them over several workgroups a row.
+// between spread them over several workgroups a row. (Where top-k comes with top-p,
+// for whichever rows, no row's passes are spread.)
 //
 // Weights w = 2^((x - max) log2(e) / temperature) are 64-bit values rounded to
 // units of 2^-42 and added as integers: sums do not depend on the order of
@@ -21,8 +22,9 @@
 //
 // Bound: the 64-bit exponentials for many rows, latency of the two launches and
 // of pick_kernel's barriers and loads for a few. Measured: 256 x 151936 bf16 (15 us at
-// a copy's rate) scan 34 us, pick 85 for flat rows under top-p, of which 18 go to the
-// window's histogram and 47 to the exact pass; 8 x 128256 fp32 under every filter 14
+// a copy's rate) scan 34 us, pick 84 for flat rows under top-p, of which 18 go to the
+// window's histogram and 47 to the exact pass; in both kernels vector instructions of
+// four cycles each fill 85 % of the SIMDs' time. 8 x 128256 fp32 under every filter 15
 // us a call, 1 x 32000 without one 8 in a graph.
 #include <hip/hip_runtime.h>
 
@@ -42,13 +44,16 @@ constexpr int kBins = 64 + 26 * 64;            // log-linear bins of a 32-bit di
 constexpr int kList = 4096;                    // candidates kept in LDS
 constexpr int kSmall = 256;                    // most candidates that are ranked by counting
 constexpr int kPerBit = 64;                    // bins of a halving of the weight
-// Passes over rows are spread for up to 128 rows of 65536 logits or more. A wide
-// nucleus, us a call in one workgroup a row and spread: 1 x 65536 47 and 33, 1 x 128256
-// 69 and 34, 128 x 65536 59 and 58, 128 x 128256 94 and 78. A narrow one, for which
-// the two launches find nothing to do: 1 x 65536 12 and 16.
+// Passes over rows are spread for up to 128 rows of 65536 logits or more, where the call
+// has no top-k. In a graph, us a call in one workgroup a row and spread: a wide nucleus in
+// fp32 1 x 65536 49 and 35, 1 x 128256 75 and 37, 128 x 65536 56 and 55, 128 x 128256 92 and
+// 78; in bf16 47 and 41, 70 and 41, 54 and 52, 83 and 72. A narrow one, for which the
+// two launches find nothing to do: fp32 1 x 65536 12 and 16, 128 x 128256 27 and 33, bf16
+// 1 x 65536 14 and 18. So a third is lost on the one to halve the other, which is not known
+// before the launch.
 constexpr int kSpreadRows = 128;
 constexpr int kSpreadVocab = 65536;
-constexpr int kSpreadMaxima = 160;             // most chunks that hold a narrow nucleus
+constexpr int kSpreadMaxima = 160;             // most chunks, of any type, of a narrow nucleus
 constexpr int kSpreadGroups = 256;             // workgroups of a spread launch: one a CU
 constexpr int kUnitBits = 42;                  // a weight of 1 in units
 constexpr uint64_t kUnitBase = 0x433ull << 52;  // the bits of 2^52: units are its last place
@@ -296,8 +301,9 @@ __global__ void __launch_bounds__(kRowWave *kScanWaves) scan_kernel(const Sample
             const double max = static_cast<double>(m);
             const float least = max32(static_cast<float>(max - kCut * kLn2 * tau), kLowest);
             if ((static_cast<double>(least) - max) * scale < 1.0 - kCut) {
-                // what is below the cut, or not there, counts 2^-60: no more than 2^-51 of
-                // the chunk's weight together, and cheaper than leaving it out
+                // what is below the cut, or not there, counts at the cut, rounded to fp32:
+                // 2^-59 at most, less than 2^-50 of the chunk's weight together, and
+                // cheaper than leaving it out
 #pragma unroll
                 for (int i = 0; i < kVec<D>; ++i)
                     sum[b] += exp2_quick<0>(
@@ -1045,7 +1051,9 @@ __device__ __forceinline__ void weigh_row(Shared &s, const SampleArgs &n, int64_
     // The chunks' maxima bound what is kept: the k-th largest of them (to a bin of the
     // histogram) has k tokens at or above it, and the one at which their own weights
     // reach top-p's share has that much at or above it. A row whose maxima do not reach it
-    // has a wide nucleus.
+    // has a wide nucleus. Under a top-k of as many tokens as there are chunks, or more, no
+    // maximum says anything: the whole row is listed, or sorted out if it does not fit the
+    // list (8 x 32000 bf16, 63 chunks, in a graph: top-k 50 13 us, 62 19, 63 39).
     if ((l.by_k && d.top_k < n.chunks) || (l.by_p && !l.by_k)) {
         for (int c = b.c0; c < b.c1; ++c)
             if (s.chunk_key[c] >= l.keep.key)
@@ -1060,7 +1068,8 @@ __device__ __forceinline__ void weigh_row(Shared &s, const SampleArgs &n, int64_
             l.bound = b.top > last ? b.top - last : 0;
             if (n.hist && !l.by_k) {
                 // more than a few candidates take longer to list and sort out than spread
-                // passes do: 55 us against 39 for 4 x 128256
+                // passes do: 55 us against 39 for 4 x 128256 in fp32. (A chunk of a 16-bit
+                // type has twice the logits: its rows of up to 81920 never count as wide here.)
                 uint64_t mine = 0;
                 for (int c = b.c0; c < b.c1; ++c) mine += s.chunk_key[c] >= l.bound;
                 l.wide = block_sum(s, mine) > kSpreadMaxima;
