@@ -12,6 +12,7 @@
 // 64 x 8192 over 8 partials 5.6 us and 1 x 4096 3.0.
 #include <hip/hip_runtime.h>
 
+#include "operands.h"
 #include "rows.h"
 
 namespace sifar {
@@ -182,25 +183,6 @@ hipError_t launch_norm(const sifar_block_norm_args &a, hipStream_t s) {
         default: block_norm_kernel<D, R, 8><<<grid, block, 0, s>>>(n); break;
     }
     return hipGetLastError();
-}
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-uint64_t size_of(int32_t dtype) { return dtype == SIFAR_FP32 ? 4 : 2; }
-
-Rows rows_of(const void *p, int32_t dtype, int64_t tokens, int64_t stride, int64_t hidden) {
-    Rows r;
-    r.at = reinterpret_cast<uintptr_t>(p);
-    r.rows = static_cast<uint64_t>(stride == 0 ? 1 : tokens);
-    r.stride = static_cast<uint64_t>(stride) * size_of(dtype);
-    r.size = static_cast<uint64_t>(hidden) * size_of(dtype);
-    return r;
-}
-
-// A row stride, which only several tokens use: a multiple of 8 that keeps them apart.
-bool good_stride(int64_t stride, int32_t tokens, int32_t hidden) {
-    return tokens <= 1 ||
-           (stride % 8 == 0 && stride >= hidden && stride <= (int64_t{1} << 40));
 }
 
 bool good(const sifar_block_norm_args &a) {

@@ -39,10 +39,13 @@ __host__ __device__ inline DivU32 make_div(uint32_t d) {
     return v;
 }
 
-__host__ __device__ inline uint32_t mod_u32(uint32_t x, const DivU32 &v) {
+__host__ __device__ inline uint32_t div_u32(uint32_t x, const DivU32 &v) {
     const uint32_t t = static_cast<uint32_t>((static_cast<uint64_t>(v.m) * x) >> 32);
-    const uint32_t q = (t + ((x - t) >> v.sh1)) >> v.sh2;
-    return x - q * v.d;
+    return (t + ((x - t) >> v.sh1)) >> v.sh2;
+}
+
+__host__ __device__ inline uint32_t mod_u32(uint32_t x, const DivU32 &v) {
+    return x - div_u32(x, v) * v.d;
 }
 
 // Token rows of a persistent plain step's planes: a plane of `tokens` rows of
