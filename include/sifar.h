@@ -690,6 +690,223 @@ int sifar_sample(const sifar_sample_args *a, void *stream);
  * tokens or a larger vocabulary: a workspace for the largest batch serves all. */
 int64_t sifar_sample_workspace(int32_t tokens, int32_t vocab);
 
+/* ---- Blocks of a decode layer --------------------------------------------------
+ * What a rank computes between two all-reduces: it appends the new tokens' keys and
+ * values to the cache (sifar_cache_append), attends over it
+ * (sifar_paged_attention), and runs the experts that sifar_route chose
+ * (sifar_experts). The outputs of the attention's projection and of the experts are
+ * the partials that an all-reduce sums. Conventions, element types, streams and
+ * errors are those of the row operators.
+ *
+ * Paged cache: keys and values of one layer lie in num_pages pages of page_size
+ * slots. Element d of head h in slot s of page p is at
+ *     p * page_stride + s * slot_stride + h * head_stride + d
+ * of k_cache and of v_cache: pages of whole slots ([pages][page_size][heads][dim]),
+ * pages of heads ([pages][heads][page_size][dim]) and both caches in one buffer are
+ * all described so. Strides are multiples of 8 elements and keep elements apart.
+ * pages[q * pages_stride + i] is the page of positions i * page_size and on of
+ * sequence q. A position whose page is not in 0..num_pages-1, or that lies behind
+ * max_pages pages, is not there: it is neither written nor read. */
+
+/* Appending to a paged cache, with the position rotation applied on the way. Token t
+ * has position P = positions[t] in sequence q = sequence[t] (sequence NULL: q = t):
+ *
+ *   angle_i = P * inv_freq[i]            in 64 bits, 0 <= i < rotary_dim / 2
+ *   (a, b)  = (x[i], x[i + rotary_dim / 2]), or interleaved (x[2 i], x[2 i + 1])
+ *   a' = rotary_scale * (a cos(angle_i) - b sin(angle_i))
+ *   b' = rotary_scale * (a sin(angle_i) + b cos(angle_i))
+ *
+ * in fp32, rounded once; elements from rotary_dim on are copied. q_out takes the
+ * rotated queries; the rotated keys and the values as they are go to the slot of
+ * position P. A token with P < 0 is padding: nothing of it is written. Where the
+ * sequence is not in 0..sequences-1, or P's page is not there, q_out is written and
+ * the cache is not. Of tokens that name the same slot, either's elements are left in
+ * it.
+ *
+ *   q, q_out  [tokens][q_heads][head_dim] dtype, heads adjacent, rows ..._stride
+ *             apart; both NULL with q_heads 0. q_out may be q (same address and
+ *             stride)
+ *   k, v      [tokens][kv_heads][head_dim], likewise
+ *   positions, sequence  [tokens] int32
+ *   pages     [sequences][max_pages] int32, rows pages_stride apart
+ *   inv_freq  [rotary_dim / 2] fp32; NULL with rotary_dim 0
+ *
+ * Limits: head_dim a multiple of 8 in 8..SIFAR_CACHE_MAX_DIM; rotary_dim even and at
+ * most head_dim; kv_heads 1..SIFAR_CACHE_MAX_HEADS, q_heads 0..that; page_size
+ * 1..SIFAR_CACHE_MAX_PAGE; num_pages, max_pages and sequences at least 1; 0 <=
+ * tokens <= SIFAR_ROWS_MAX_TOKENS (at most sequences where sequence is NULL); row
+ * strides, where there is more than one token, multiples of 8 and at least a row;
+ * rows and caches 16-byte aligned. Outputs that overlap each other (the two caches:
+ * in an element) or an input are refused. One launch. */
+#define SIFAR_CACHE_MAX_DIM 256
+#define SIFAR_CACHE_MAX_HEADS 1024
+#define SIFAR_CACHE_MAX_PAGE 65536
+typedef struct {
+    int32_t dtype;
+    int32_t tokens;
+    int32_t q_heads;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t rotary_dim;
+    int32_t interleaved;
+    int32_t page_size;
+    int32_t num_pages;
+    int32_t sequences;
+    int32_t max_pages;
+    float rotary_scale;
+    const void *q;
+    int64_t q_stride;
+    void *q_out;
+    int64_t q_out_stride;
+    const void *k;
+    int64_t k_stride;
+    const void *v;
+    int64_t v_stride;
+    const int32_t *positions;
+    const int32_t *sequence;
+    const int32_t *pages;
+    int64_t pages_stride;
+    const float *inv_freq;
+    void *k_cache;
+    void *v_cache;
+    int64_t page_stride;
+    int64_t slot_stride;
+    int64_t head_stride;
+} sifar_cache_append_args;
+int sifar_cache_append(const sifar_cache_append_args *a, void *stream);
+
+/* Attention of one new token of each sequence over the paged cache. Token t is
+ * sequence t; query head h reads the cache's head h / (q_heads / kv_heads). With
+ * n = lengths[t] cut to 0..min(max_length, max_pages * page_size), over the positions
+ * p that are there of max(0, n - window) <= p < n (window 0: all below n):
+ *
+ *   s_p = scale * (q . k_p);   softcap > 0: softcap * tanh(s_p / softcap)
+ *   Z   = sum_p exp(s_p) + exp(sinks[h])         (sinks NULL: without)
+ *   out = sum_p exp(s_p) v_p / Z,   lse = log Z
+ *
+ * lengths counts the new token, once it was appended. Products, sums and weights are
+ * in fp32; out is rounded once. A row without any position has out 0 and lse -inf
+ * (with a sink: the sink). A position whose score is -inf has no weight; a score that
+ * is NaN or +inf makes its row NaN. What the cache holds in slots that are not read
+ * (behind a length, outside the window) has no influence, NaN included.
+ *
+ *   q, out   [tokens][q_heads][head_dim] dtype, heads adjacent, rows ..._stride apart.
+ *            out may be q (same address and stride)
+ *   lengths  [tokens] int32;  pages [tokens][max_pages] int32, rows pages_stride apart
+ *   sinks    [q_heads] fp32, finite or -inf, or NULL;  lse [tokens][q_heads] fp32, or NULL
+ *   max_length  what no length exceeds, known to the host: sizes, with the window, how
+ *            many workgroups share a sequence, and the workspace. The caches' capacity
+ *            is always right; calls that are to give equal bits need equal ones.
+ *   workspace   at least sifar_paged_attention_workspace(...) bytes, 16-byte aligned,
+ *            caller-owned, in any state before and after; NULL where that is 0. Calls
+ *            that may run at the same time need one each.
+ *
+ * Limits: head_dim a multiple of 8 in 8..SIFAR_CACHE_MAX_DIM; q_heads a multiple of
+ * kv_heads, both in 1..SIFAR_CACHE_MAX_HEADS; page_size, num_pages and max_pages as
+ * above; 0 <= tokens <= SIFAR_ATTENTION_MAX_TOKENS; 1 <= max_length <=
+ * SIFAR_ATTENTION_MAX_LENGTH; window and softcap not negative, scale finite; row
+ * strides, where there is more than one token, multiples of 8 and at least a row;
+ * rows and caches 16-byte aligned. Outputs and workspace that overlap each other or an
+ * input are refused. One launch, or two where sequences are shared. */
+#define SIFAR_ATTENTION_MAX_TOKENS 32768
+#define SIFAR_ATTENTION_MAX_LENGTH 16777216
+typedef struct {
+    int32_t dtype;
+    int32_t tokens;
+    int32_t q_heads;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t page_size;
+    int32_t num_pages;
+    int32_t max_pages;
+    int32_t max_length;
+    int32_t window;
+    float scale;
+    float softcap;
+    const void *q;
+    int64_t q_stride;
+    const void *k_cache;
+    const void *v_cache;
+    int64_t page_stride;
+    int64_t slot_stride;
+    int64_t head_stride;
+    const int32_t *pages;
+    int64_t pages_stride;
+    const int32_t *lengths;
+    const float *sinks;
+    void *out;
+    int64_t out_stride;
+    float *lse;
+    void *workspace;
+    int64_t workspace_bytes;
+} sifar_paged_attention_args;
+int sifar_paged_attention(const sifar_paged_attention_args *a, void *stream);
+
+/* Bytes of workspace that sifar_paged_attention needs, or SIFAR_EINVAL. Never less for
+ * more tokens or a larger max_length: a workspace for the largest batch serves all. */
+int64_t sifar_paged_attention_workspace(int32_t tokens, int32_t q_heads, int32_t kv_heads,
+                                        int32_t head_dim, int32_t max_length);
+
+/* A mixture-of-experts layer for a few tokens. Slot j of token t names an expert
+ * ids[t][j] and its weight, as sifar_route leaves them. With e = ids[t][j] -
+ * first_expert, over the slots with 0 <= e < experts (the experts that this rank
+ * holds; -1, an empty slot, never is one), slots in ascending order:
+ *
+ *   g = w_in[e][0..inter) x_t,   u = w_in[e][inter..2 inter) x_t
+ *   h = act(g) * u      act: SiLU, g / (1 + exp(-g)), or GELU in its tanh form
+ *   out_t = sum_j weights[t][j] * (w_out[e] h)
+ *
+ * in fp32 (h is held to 16 bits of mantissa between the two products, 24 with fp32),
+ * rounded once. A token without a slot here has out 0. The sum over ranks of their
+ * experts' outputs is what the all-reduce makes of them.
+ *
+ *   x, out   [tokens][hidden] dtype, rows ..._stride apart
+ *   ids, weights  [tokens][topk] int32 and fp32, contiguous
+ *   w_in     [experts][2 * inter][hidden] dtype, experts w_in_stride apart
+ *   w_out    [experts][hidden][inter] dtype, experts w_out_stride apart
+ *   workspace  at least sifar_experts_workspace(tokens, topk, inter) bytes, 16-byte
+ *            aligned, caller-owned, in any state before and after. Calls that may run
+ *            at the same time need one each.
+ *
+ * Limits: hidden and inter multiples of 8 in 8..65536; experts 1..
+ * SIFAR_ROUTE_MAX_EXPERTS; topk 1..SIFAR_ROUTE_MAX_TOPK; 0 <= tokens <=
+ * SIFAR_EXPERTS_MAX_TOKENS and tokens * topk <= SIFAR_EXPERTS_MAX_SLOTS; first_expert
+ * not negative; row strides, where there is more than one token, and the experts',
+ * where there is more than one, multiples of 8 and at least what they step over;
+ * x, out and weight matrices 16-byte aligned. Outputs and workspace that overlap each
+ * other or an input are refused. Two launches. */
+#define SIFAR_EXPERTS_SILU 0
+#define SIFAR_EXPERTS_GELU 1
+#define SIFAR_EXPERTS_MAX_TOKENS 128
+#define SIFAR_EXPERTS_MAX_SLOTS 1024
+typedef struct {
+    int32_t dtype;
+    int32_t tokens;
+    int32_t hidden;
+    int32_t inter;
+    int32_t experts;
+    int32_t topk;
+    int32_t first_expert;
+    int32_t activation;
+    const void *x;
+    int64_t x_stride;
+    const int32_t *ids;
+    const float *weights;
+    const void *w_in;
+    int64_t w_in_stride;
+    const void *w_out;
+    int64_t w_out_stride;
+    void *out;
+    int64_t out_stride;
+    void *workspace;
+    int64_t workspace_bytes;
+} sifar_experts_args;
+int sifar_experts(const sifar_experts_args *a, void *stream);
+
+/* Bytes of workspace that sifar_experts needs, or SIFAR_EINVAL. Never less for more
+ * tokens or slots: a workspace for the largest batch serves all. */
+int64_t sifar_experts_workspace(int32_t tokens, int32_t topk, int32_t inter);
+
 #ifdef __cplusplus
 }
 #endif

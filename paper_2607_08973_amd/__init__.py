@@ -78,6 +78,18 @@ SIFAR_ROUTE_MAX_EXPERTS = 1024
 SIFAR_ROUTE_MAX_GROUPS = 32
 SIFAR_ROUTE_MAX_TOPK = 32
 SIFAR_SAMPLE_MAX_VOCAB = 1048576
+
+# the blocks of a decode layer: largest sizes, activations
+SIFAR_CACHE_MAX_DIM = 256
+SIFAR_CACHE_MAX_HEADS = 1024
+SIFAR_CACHE_MAX_PAGE = 65536
+SIFAR_ATTENTION_MAX_TOKENS = 32768
+SIFAR_ATTENTION_MAX_LENGTH = 16777216
+SIFAR_EXPERTS_SILU = 0
+SIFAR_EXPERTS_GELU = 1
+SIFAR_EXPERTS_MAX_TOKENS = 128
+SIFAR_EXPERTS_MAX_SLOTS = 1024
+EXPERTS_ACTIVATION = {"silu": 0, "gelu": 1}
 ROUTE_SCORE = {"softmax": 0, "sigmoid": 1}
 
 CHUNK = 512  # elements per chunk (one 64-lane wave, 16 bytes per lane)
@@ -90,7 +102,9 @@ EXPORTS = (
     "sifar_read_log", "sifar_read_stamp_log", "sifar_read_placement",
     "sifar_epochs", "sifar_status", "sifar_error_info", "sifar_strerror", "sifar_floor",
     "sifar_litmus", "sifar_allreduce_noalloc", "sifar_block_norm",
-    "sifar_route", "sifar_sample", "sifar_sample_workspace",
+    "sifar_route", "sifar_sample", "sifar_sample_workspace", "sifar_cache_append",
+    "sifar_paged_attention", "sifar_paged_attention_workspace", "sifar_experts",
+    "sifar_experts_workspace",
 )
 
 
@@ -207,6 +221,99 @@ class sifar_sample_args(ctypes.Structure):
     ]
 
 
+class sifar_cache_append_args(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("tokens", ctypes.c_int32),
+        ("q_heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("sequences", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("rotary_scale", ctypes.c_float),
+        ("q", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64),
+        ("q_out", ctypes.c_void_p),
+        ("q_out_stride", ctypes.c_int64),
+        ("k", ctypes.c_void_p),
+        ("k_stride", ctypes.c_int64),
+        ("v", ctypes.c_void_p),
+        ("v_stride", ctypes.c_int64),
+        ("positions", ctypes.c_void_p),
+        ("sequence", ctypes.c_void_p),
+        ("pages", ctypes.c_void_p),
+        ("pages_stride", ctypes.c_int64),
+        ("inv_freq", ctypes.c_void_p),
+        ("k_cache", ctypes.c_void_p),
+        ("v_cache", ctypes.c_void_p),
+        ("page_stride", ctypes.c_int64),
+        ("slot_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+    ]
+
+
+class sifar_paged_attention_args(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("tokens", ctypes.c_int32),
+        ("q_heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("max_length", ctypes.c_int32),
+        ("window", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("softcap", ctypes.c_float),
+        ("q", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64),
+        ("k_cache", ctypes.c_void_p),
+        ("v_cache", ctypes.c_void_p),
+        ("page_stride", ctypes.c_int64),
+        ("slot_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+        ("pages", ctypes.c_void_p),
+        ("pages_stride", ctypes.c_int64),
+        ("lengths", ctypes.c_void_p),
+        ("sinks", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("out_stride", ctypes.c_int64),
+        ("lse", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
+class sifar_experts_args(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("tokens", ctypes.c_int32),
+        ("hidden", ctypes.c_int32),
+        ("inter", ctypes.c_int32),
+        ("experts", ctypes.c_int32),
+        ("topk", ctypes.c_int32),
+        ("first_expert", ctypes.c_int32),
+        ("activation", ctypes.c_int32),
+        ("x", ctypes.c_void_p),
+        ("x_stride", ctypes.c_int64),
+        ("ids", ctypes.c_void_p),
+        ("weights", ctypes.c_void_p),
+        ("w_in", ctypes.c_void_p),
+        ("w_in_stride", ctypes.c_int64),
+        ("w_out", ctypes.c_void_p),
+        ("w_out_stride", ctypes.c_int64),
+        ("out", ctypes.c_void_p),
+        ("out_stride", ctypes.c_int64),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
 class SifarError(RuntimeError):
     def __init__(self, fn: str, code: int, info=None):
         msg = f"{fn} failed: {code} ({strerror(code)})"
@@ -263,6 +370,11 @@ def load(path: str = LIB_PATH):
         "sifar_route": (ctypes.c_int, [P, P]),
         "sifar_sample": (ctypes.c_int, [P, P]),
         "sifar_sample_workspace": (I64, [I32, I32]),
+        "sifar_cache_append": (ctypes.c_int, [P, P]),
+        "sifar_paged_attention": (ctypes.c_int, [P, P]),
+        "sifar_paged_attention_workspace": (I64, [I32, I32, I32, I32, I32]),
+        "sifar_experts": (ctypes.c_int, [P, P]),
+        "sifar_experts_workspace": (I64, [I32, I32, I32]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -653,6 +765,260 @@ def sifar_sample(logits, uniform, out, workspace, probs=None, temperature=None, 
     rc = (_lib or load()).sifar_sample(
         _SAMPLE.pack(_dtype(fn, logits.dtype), T, V, x, x_stride, u, t, k, tp, mp, o, p, ws,
                      workspace.shape[0]), _row_stream(stream, dev))
+    if rc:
+        _check(fn, rc)
+
+
+# ---- blocks of a decode layer: tensors in, as for the row operators -----------
+
+_APPEND = struct.Struct("<11if" "Qq" "Qq" "Qq" "Qq" "3Qq" "3Q3q")
+_ATTENTION = struct.Struct("<10i2f" "Qq" "2Q3q" "Qq" "2Q" "Qq" "2Qq")
+_EXPERTS = struct.Struct("<8i" "Qq" "2Q" "Qq" "Qq" "Qq" "Qq")
+
+
+def _heads(fn: str, name: str, t, dtype, shape, dev: int):
+    """Address and row stride of t [tokens][heads][dim], whose heads are adjacent."""
+    if t is None:
+        _refuse(fn, f"no {name}")
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev:
+        if t.is_contiguous():
+            return t.data_ptr(), shape[1] * shape[2]
+        at = t.stride()
+        if at[2] == 1 and (at[1] == shape[2] or shape[1] == 1):
+            return t.data_ptr(), at[0]
+    _refuse(fn, f"{name} is {t.dtype} {tuple(t.shape)} on {t.device} at strides {t.stride()}, not "
+                f"{dtype} {tuple(shape)} on the current GPU with adjacent heads")
+
+
+def _caches(fn: str, k_cache, v_cache, dtype, heads: int, dim: int, dev: int):
+    """Shape and strides of two caches [pages][page_size][heads][dim] that are laid out alike."""
+    if k_cache is None or v_cache is None:
+        _refuse(fn, "no k_cache" if k_cache is None else "no v_cache")
+    shape, at = k_cache.shape, k_cache.stride()
+    if len(shape) != 4 or shape[2:] != (heads, dim) or at[3] != 1:
+        _refuse(fn, f"k_cache is {tuple(shape)} at strides {at}, not [pages][page_size][{heads}]"
+                    f"[{dim}] with adjacent elements")
+    if v_cache.shape != shape or v_cache.stride() != at:
+        _refuse(fn, "k_cache and v_cache are not laid out alike")
+    for c in (k_cache, v_cache):
+        if c.dtype is not dtype or c.get_device() != dev:
+            _refuse(fn, f"a cache is {c.dtype} on {c.device}, not {dtype} on the current GPU")
+    if shape[0] > 0x7FFFFFFF or shape[1] > SIFAR_CACHE_MAX_PAGE:
+        _refuse(fn, f"{shape[0]} pages of {shape[1]} are too large")
+    return shape, at
+
+
+def _table(fn: str, pages, dev: int):
+    """Address, rows, columns and row stride of the table of pages."""
+    if pages is None or pages.dim() != 2:
+        _refuse(fn, "no pages" if pages is None else f"pages has {pages.dim()} dimensions, not 2")
+    shape = pages.shape
+    if shape[0] > 0x7FFFFFFF or shape[1] > 0x7FFFFFFF:
+        _refuse(fn, f"a table of {shape[0]} x {shape[1]} pages is too large")
+    at, stride = _operand(fn, "pages", pages, _I32, shape, dev)
+    return at, shape[0], shape[1], stride
+
+
+def sifar_cache_append(k, v, positions, pages, k_cache, v_cache, q=None, q_out=None, inv_freq=None,
+                       interleaved=False, rotary_scale=1.0, sequence=None, stream=None) -> None:
+    """k, v [tokens][kv_heads][dim], q and q_out (or neither) [tokens][q_heads][dim]: views of one
+    projection's rows will do; positions and sequence (or None) int32 [tokens]; pages int32
+    [sequences][max_pages]; k_cache, v_cache [pages][page_size][kv_heads][dim] at any strides, alike
+    in both; inv_freq float32 [rotary_dim / 2], or None for no rotation."""
+    fn = "sifar_cache_append"
+    if _C is None:
+        _torch()
+    if k is None or positions is None:
+        _refuse(fn, "no k" if k is None else "no positions")
+    shape = k.shape
+    if len(shape) != 3:
+        _refuse(fn, f"k has {len(shape)} dimensions, not 3")
+    T, H, D = shape
+    if T > SIFAR_ROWS_MAX_TOKENS or H > SIFAR_CACHE_MAX_HEADS or D > SIFAR_CACHE_MAX_DIM:
+        _refuse(fn, f"{T} x {H} x {D} is too large")
+    dev = _gpu(fn, "k", k)
+    dt, rows = k.dtype, shape[:1]
+    code = _dtype(fn, dt)
+    kp, k_stride = _heads(fn, "k", k, dt, shape, dev)
+    vp, v_stride = _heads(fn, "v", v, dt, shape, dev)
+    if (q is None) != (q_out is None):
+        _refuse(fn, "q and q_out go together")
+    qp = q_stride = op = o_stride = heads = 0
+    if q is not None:
+        if q.dim() != 3 or q.shape[0] != T or q.shape[2] != D or not (
+                0 < q.shape[1] <= SIFAR_CACHE_MAX_HEADS):
+            _refuse(fn, f"q is {tuple(q.shape)}, not [{T}][heads][{D}]")
+        heads = q.shape[1]
+        qp, q_stride = _heads(fn, "q", q, dt, q.shape, dev)
+        op, o_stride = _heads(fn, "q_out", q_out, dt, q.shape, dev)
+    at, _ = _operand(fn, "positions", positions, _I32, rows, dev)
+    seq = 0 if sequence is None else _operand(fn, "sequence", sequence, _I32, rows, dev)[0]
+    table, sequences, width, table_stride = _table(fn, pages, dev)
+    freq = pairs = 0
+    if inv_freq is not None:
+        if inv_freq.dim() != 1 or not 0 < inv_freq.shape[0] <= SIFAR_CACHE_MAX_DIM // 2:
+            _refuse(fn, f"inv_freq is {tuple(inv_freq.shape)}")
+        pairs = inv_freq.shape[0]
+        freq, _ = _operand(fn, "inv_freq", inv_freq, _F32, inv_freq.shape, dev)
+    cache, cs = _caches(fn, k_cache, v_cache, dt, H, D, dev)
+    try:
+        args = _APPEND.pack(
+            code, T, heads, H, D, 2 * pairs, 1 if interleaved else 0, cache[1], cache[0],
+            sequences, width, rotary_scale, qp, q_stride, op, o_stride, kp, k_stride, vp, v_stride,
+            at, seq, table, table_stride, freq, k_cache.data_ptr(), v_cache.data_ptr(), cs[0],
+            cs[1], cs[2])
+    except _UNPACKABLE as e:
+        _refuse(fn, f"rotary_scale: {e}")
+    rc = (_lib or load()).sifar_cache_append(args, _row_stream(stream, dev))
+    if rc:
+        _check(fn, rc)
+
+
+def _small(fn: str, **sizes) -> None:
+    """Sizes that a 32-bit field holds as they are."""
+    for name, n in sizes.items():
+        if not isinstance(n, int) or not 0 <= n <= 0x7FFFFFFF:
+            _refuse(fn, f"{name} is {n!r}")
+
+
+def sifar_paged_attention_workspace(tokens: int, q_heads: int, kv_heads: int, head_dim: int,
+                                    max_length: int) -> int:
+    """Bytes of workspace that sifar_paged_attention needs (0: none)."""
+    fn = "sifar_paged_attention_workspace"
+    _small(fn, tokens=tokens, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim,
+           max_length=max_length)
+    n = load().sifar_paged_attention_workspace(tokens, q_heads, kv_heads, head_dim, max_length)
+    if n < 0:
+        _check(fn, n)
+    return n
+
+
+def sifar_paged_attention(q, k_cache, v_cache, pages, lengths, out, workspace=None,
+                          max_length=None, scale=None, window=0, softcap=0.0, sinks=None, lse=None,
+                          stream=None) -> None:
+    """q and out [tokens][q_heads][dim]; k_cache, v_cache [pages][page_size][kv_heads][dim] at any
+    strides, alike in both; pages int32 [tokens][max_pages]; lengths int32 [tokens], none above
+    max_length (None: max_pages * page_size); scale None: dim ** -0.5; sinks float32 [q_heads]; lse
+    float32 [tokens][q_heads], contiguous; workspace: a contiguous uint8 tensor of
+    sifar_paged_attention_workspace(...) bytes, not shared by calls that may overlap."""
+    fn = "sifar_paged_attention"
+    if _C is None:
+        _torch()
+    if q is None or k_cache is None:
+        _refuse(fn, "no q" if q is None else "no k_cache")
+    shape = q.shape
+    if len(shape) != 3 or k_cache.dim() != 4:
+        _refuse(fn, f"q has {len(shape)} dimensions, not 3, or k_cache {k_cache.dim()}, not 4")
+    T, H, D = shape
+    Hk = k_cache.shape[2]
+    if (T > SIFAR_ATTENTION_MAX_TOKENS or H > SIFAR_CACHE_MAX_HEADS or Hk > SIFAR_CACHE_MAX_HEADS
+            or D > SIFAR_CACHE_MAX_DIM):
+        _refuse(fn, f"{T} x {H} x {D} over {Hk} heads is too large")
+    dev = _gpu(fn, "q", q)
+    dt = q.dtype
+    code = _dtype(fn, dt)
+    qp, q_stride = _heads(fn, "q", q, dt, shape, dev)
+    op, o_stride = _heads(fn, "out", out, dt, shape, dev)
+    cache, cs = _caches(fn, k_cache, v_cache, dt, Hk, D, dev)
+    table, rows, width, table_stride = _table(fn, pages, dev)
+    if rows != T:
+        _refuse(fn, f"pages has {rows} rows, q {T}")
+    n, _ = _operand(fn, "lengths", lengths, _I32, shape[:1], dev)
+    s = 0 if sinks is None else _operand(fn, "sinks", sinks, _F32, shape[1:2], dev)[0]
+    lp = 0
+    if lse is not None:
+        lp, l_stride = _operand(fn, "lse", lse, _F32, shape[:2], dev)
+        if T > 1 and l_stride != H:
+            _refuse(fn, "the rows of lse are not adjacent")
+    ws = size = 0
+    if workspace is not None:
+        if workspace.dim() != 1:
+            _refuse(fn, f"workspace has {workspace.dim()} dimensions, not 1")
+        size = workspace.shape[0]
+        ws, _ = _operand(fn, "workspace", workspace, _U8, workspace.shape, dev)
+    if max_length is None:
+        max_length = min(width * cache[1], SIFAR_ATTENTION_MAX_LENGTH)
+    try:
+        args = _ATTENTION.pack(
+            code, T, H, Hk, D, cache[1], cache[0], width, max_length, window,
+            D ** -0.5 if scale is None else scale, softcap, qp, q_stride, k_cache.data_ptr(),
+            v_cache.data_ptr(), cs[0], cs[1], cs[2], table, table_stride, n, s, op, o_stride, lp,
+            ws, size)
+    except (*_UNPACKABLE, ZeroDivisionError) as e:
+        _refuse(fn, f"max_length, window, scale or softcap: {e}")
+    rc = (_lib or load()).sifar_paged_attention(args, _row_stream(stream, dev))
+    if rc:
+        _check(fn, rc)
+
+
+def sifar_experts_workspace(tokens: int, topk: int, inter: int) -> int:
+    """Bytes of workspace that sifar_experts needs."""
+    fn = "sifar_experts_workspace"
+    _small(fn, tokens=tokens, topk=topk, inter=inter)
+    n = load().sifar_experts_workspace(tokens, topk, inter)
+    if n < 0:
+        _check(fn, n)
+    return n
+
+
+def _matrices(fn: str, name: str, t, dtype, shape, dev: int):
+    """Address and stride of t [experts][rows][columns], whose matrices are contiguous."""
+    if t is None:
+        _refuse(fn, f"no {name}")
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev:
+        at = t.stride()
+        if at[2] == 1 and at[1] == shape[2]:
+            return t.data_ptr(), at[0]
+    _refuse(fn, f"{name} is {t.dtype} {tuple(t.shape)} on {t.device} at strides {t.stride()}, not "
+                f"{dtype} {tuple(shape)} on the current GPU with contiguous matrices")
+
+
+def sifar_experts(x, ids, weights, w_in, w_out, out, workspace, activation="silu", first_expert=0,
+                  stream=None) -> None:
+    """x and out [tokens][hidden]; ids (int32) and weights (float32) [tokens][topk], contiguous, as
+    sifar_route leaves them; w_in [experts][2 * inter][hidden], gate rows first; w_out
+    [experts][hidden][inter]; the experts are those from first_expert on; activation "silu" or
+    "gelu"; workspace: a contiguous uint8 tensor of sifar_experts_workspace(tokens, topk, inter)
+    bytes, not shared by calls that may overlap."""
+    fn = "sifar_experts"
+    if _C is None:
+        _torch()
+    for name, t, dims in (("x", x, 2), ("ids", ids, 2), ("w_out", w_out, 3),
+                          ("workspace", workspace, 1)):
+        if t is None:
+            _refuse(fn, f"no {name}")
+        if t.dim() != dims:
+            _refuse(fn, f"{name} has {t.dim()} dimensions, not {dims}")
+    shape, out_shape = x.shape, ids.shape
+    T, H = shape
+    E, _, I = w_out.shape
+    k = out_shape[1]
+    if (T > SIFAR_EXPERTS_MAX_TOKENS or H > 65536 or I > 65536 or E > SIFAR_ROUTE_MAX_EXPERTS
+            or k > SIFAR_ROUTE_MAX_TOPK):
+        _refuse(fn, f"{T} x {H}, top {k} of {E} experts of {I}, is too large")
+    if out_shape[0] != T:
+        _refuse(fn, f"ids has {out_shape[0]} rows, x {T}")
+    dev = _gpu(fn, "x", x)
+    dt = x.dtype
+    code = _dtype(fn, dt)
+    xp, x_stride = _operand(fn, "x", x, dt, shape, dev)
+    op, o_stride = _operand(fn, "out", out, dt, shape, dev)
+    i, i_stride = _operand(fn, "ids", ids, _I32, out_shape, dev)
+    w, w_stride = _operand(fn, "weights", weights, _F32, out_shape, dev)
+    if T > 1 and (i_stride != k or w_stride != k):
+        _refuse(fn, "the rows of ids or weights are not adjacent")
+    a, a_stride = _matrices(fn, "w_in", w_in, dt, (E, 2 * I, H), dev)
+    b, b_stride = _matrices(fn, "w_out", w_out, dt, (E, H, I), dev)
+    ws, _ = _operand(fn, "workspace", workspace, _U8, workspace.shape, dev)
+    mode = EXPERTS_ACTIVATION.get(activation, activation)
+    if mode not in (SIFAR_EXPERTS_SILU, SIFAR_EXPERTS_GELU):
+        _refuse(fn, f"no activation {activation!r}")
+    try:
+        args = _EXPERTS.pack(code, T, H, I, E, k, first_expert, mode, xp, x_stride, i, w, a,
+                             a_stride, b, b_stride, op, o_stride, ws, workspace.shape[0])
+    except _UNPACKABLE as e:
+        _refuse(fn, f"first_expert: {e}")
+    rc = (_lib or load()).sifar_experts(args, _row_stream(stream, dev))
     if rc:
         _check(fn, rc)
 

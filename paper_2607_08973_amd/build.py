@@ -17,7 +17,9 @@ LIB = os.path.join(PKG, "libsifar.so")
 SOURCES = [os.path.join(CSRC, "kernels.hip"), os.path.join(CSRC, "floors.hip"),
            os.path.join(CSRC, "litmus.hip"), os.path.join(CSRC, "noalloc.hip"),
            os.path.join(CSRC, "block_norm.hip"), os.path.join(CSRC, "route.hip"),
-           os.path.join(CSRC, "sample.hip"), os.path.join(CSRC, "api.cpp")]
+           os.path.join(CSRC, "sample.hip"), os.path.join(CSRC, "cache_append.hip"),
+           os.path.join(CSRC, "attention.hip"), os.path.join(CSRC, "experts.hip"),
+           os.path.join(CSRC, "api.cpp")]
 ARCH = "gfx950"
 
 FLAGS = [

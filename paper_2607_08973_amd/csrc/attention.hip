@@ -1,0 +1,612 @@
+// Attention of one new token of each sequence over a paged cache:
+// sifar_paged_attention. gfx950 (MI355X) only.
+//
+// Every key and value that is there has to be read once, and 4 operations per element of
+// them for each query head that shares it: bound by HBM bytes, for short sequences by
+// the launch and the chain length -> page -> keys -> values. So keys and values go from
+// memory straight into the registers that the matrix instructions read, and the query
+// heads of one cache head (up to 16) are the columns of one tile, so that the cache is
+// read once for all of them.
+//
+// With S = K Q^T (positions x heads), P = exp2(S - m) and O = V^T P (elements x heads):
+//  - K's tile is read as it lies: a lane holds 16 bytes of one position's row.
+//  - S's tile leaves in each lane 4 positions of one head, which are as they stand
+//    the summands that a lane holds of P in V^T P: positions need no order, as long as
+//    V's rows come in the same one. Nothing crosses lanes but the maximum.
+//  - A lane loads 16 bytes of each of its positions' values, 16 lanes a whole row; for
+//    16-bit elements a byte permute per word turns them into columns.
+//  - The running maximum m, the sums and O stay in registers, all for the head of
+//    the lane's column, so rescaling O is a product in each lane, done only when some
+//    head's maximum has grown.
+// P is split into two 16-bit elements (what the first leaves goes into the second), so
+// weights are good to 2^-17 and the output's one rounding is its last; the second
+// product costs matrix time that the bytes leave free.
+//
+// A workgroup takes one cache head of one sequence, or a chunk of its positions where
+// that leaves too few workgroups; its four waves take every fourth tile and join in LDS.
+// Chunks' sums go to the workspace, unscaled, and a second launch joins them.
+#include <hip/hip_runtime.h>
+
+#include "paged.h"
+#include "rows.h"
+#include "sifar_kernels.h"
+#include "tiles.h"
+
+namespace sifar {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kRowWave;
+constexpr int kMinChunk = 256;   // positions of a shared sequence's chunk, at least
+constexpr int kMaxChunk = 2048;  // and at most: their places fill 16 KB of LDS
+constexpr int kRound = 128;      // chunks are whole tiles of all waves
+constexpr int kWorkgroups = 2048;  // sequences are shared until there are so many
+constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e430p-1f;
+constexpr float kLowest = -0x1.fffffep127f;  // below every finite score
+
+struct AttendArgs {
+    sifar_paged_attention_args a;
+    DivU32 page;    // by page_size
+    DivU32 splits;  // by the most chunks of a sequence
+    int32_t group;  // query heads of a cache head
+    int32_t reach;  // lengths are cut to this
+    int64_t parts;  // from the workspace's start to the chunks' outputs, in floats
+};
+
+// Which positions a sequence has, and how long its chunks are.
+struct Stretch {
+    int first, count, chunk;
+};
+__device__ __forceinline__ Stretch stretch(const AttendArgs &n, int64_t t) {
+    const int most = n.reach;
+    int length = n.a.lengths[t];
+    length = length < 0 ? 0 : length > most ? most : length;
+    Stretch s;
+    s.first = n.a.window > 0 && length > n.a.window ? length - n.a.window : 0;
+    s.count = length - s.first;
+    const int share =
+        static_cast<int>(div_u32(static_cast<uint32_t>(s.count) + n.splits.d - 1, n.splits));
+    s.chunk = (share + kRound - 1) / kRound * kRound;
+    if (s.chunk < kMinChunk) s.chunk = kMinChunk;
+    return s;
+}
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
+
+// tanh: its series where 1 - 2 / (e^2y + 1) would cancel (off by 2e-8 at 0.35).
+__device__ __forceinline__ float tanh_of(float y) {
+    const float a = __builtin_fabsf(y), z = y * y;
+    float p = -0x1.226e36p-7f;  // -1382 / 155925
+    p = __builtin_fmaf(p, z, 0x1.664f48p-6f);
+    p = __builtin_fmaf(p, z, -0x1.ba1ba2p-5f);
+    p = __builtin_fmaf(p, z, 0x1.111112p-3f);
+    p = __builtin_fmaf(p, z, -0x1.555556p-2f);
+    const float near = __builtin_fmaf(p * z, y, y);
+    const float far =
+        __builtin_copysignf(1.f - 2.f / (exp2_of(2.f * kLog2e * a) + 1.f), y);
+    return a < 0.35f ? near : far;
+}
+
+// Four adjacent outputs.
+template <int D>
+__device__ __forceinline__ void store4(void *row, int64_t at, const F4 &f) {
+    Stored<D> *p = static_cast<Stored<D> *>(row) + at;
+    if constexpr (D == SIFAR_FP32) {
+        *reinterpret_cast<F4 *>(p) = f;
+    } else {
+        typedef uint32_t U2 __attribute__((ext_vector_type(2)));
+        *reinterpret_cast<U2 *>(p) = U2{pack16<D>(f[0], f[1]), pack16<D>(f[2], f[3])};
+    }
+}
+
+// What a row's sum of weights l, relative to 2^m, makes of its output and of lse.
+struct Close {
+    float inverse, lse;
+};
+__device__ __forceinline__ Close close_row(const AttendArgs &n, int head, float m, float l) {
+    if (n.a.sinks) {
+        const float sink = n.a.sinks[head] * kLog2e;
+        const float top = sink > m ? sink : m;
+        const float scale = exp2_of(m - top);
+        const float whole = l * scale + exp2_of(sink - top);
+        return {whole == 0.f ? 0.f : scale / whole, (top + log2_of(whole)) * kLn2};
+    }
+    return {l == 0.f ? 0.f : 1.f / l, (l == 0.f ? -__builtin_inff() : (m + log2_of(l)) * kLn2)};
+}
+
+// D: element type. DIM: 64, 128 or 256, head_dim or the next above it (PAD).
+template <int D, int DIM, bool PAD>
+__global__ void __launch_bounds__(kThreads, D == SIFAR_FP32 && DIM > 128 ? 1 : 2)
+attend_kernel(const AttendArgs n) {
+    constexpr int SIZE = D == SIFAR_FP32 ? 4 : 2;
+    constexpr int STEPS = DIM * SIZE / 64;          // of 64 bytes of a row of keys
+    // positions: half as many where keys, values and O would not fit the registers
+    constexpr int TILE = D == SIFAR_FP32 || DIM > 128 ? 16 : 32;
+    constexpr int SUBS = TILE / 16;
+    constexpr int MINE = TILE / 4;                  // positions whose values a lane loads
+    // 16 lanes hold a row of values in panels, up to 16 bytes a lane each
+    constexpr int BYTES = DIM * SIZE / 16 < 16 ? DIM * SIZE / 16 : 16;
+    constexpr int EACH = BYTES / SIZE, WORDS = BYTES / 4;
+    constexpr int PANELS = DIM / (16 * EACH);
+    constexpr int ROW = DIM + 4;  // floats of a head's output in LDS, off the banks' period
+    // fp16 weights are taken 2^14 times as large, which l's share undoes: small ones then
+    // keep their bits. bf16 has fp32's exponents.
+    constexpr float UP = D == SIFAR_FP16 ? 14.f : 0.f;
+
+    constexpr int kPlaces = kMaxChunk * 8, kOut = kWaves * 16 * ROW * 4;
+    __shared__ alignas(16) unsigned char lds[kPlaces > kOut ? kPlaces : kOut];
+    __shared__ float top[kWaves][16], sum[kWaves][16];
+    int64_t *place = reinterpret_cast<int64_t *>(lds);
+    float *outs = reinterpret_cast<float *>(lds);
+
+    const sifar_paged_attention_args &a = n.a;
+    const int64_t t = blockIdx.z;
+    const int piece = blockIdx.y, splits = gridDim.y;
+    const int kv = blockIdx.x % a.kv_heads, tile16 = blockIdx.x / a.kv_heads;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int column = lane & 15, quarter = lane >> 4;
+    const int heads = n.group - 16 * tile16 < 16 ? n.group - 16 * tile16 : 16;  // columns in use
+    const int first_head = kv * n.group + 16 * tile16;
+
+    const Stretch s = stretch(n, t);
+    const int from = piece * s.chunk;  // behind s.first
+    const int count = s.count - from < s.chunk ? s.count - from : s.chunk;
+    if (count <= 0) {  // the same for the workgroup
+        if (splits > 1) return;  // not a chunk: the second launch knows
+        for (int i = threadIdx.x; i < heads * (a.head_dim / 4); i += kThreads) {
+            const int h = i / (a.head_dim / 4);
+            store4<D>(a.out, t * a.out_stride + static_cast<int64_t>(first_head) * a.head_dim +
+                                 4 * i, F4{0.f, 0.f, 0.f, 0.f});
+            if (a.lse && i - h * (a.head_dim / 4) == 0)
+                a.lse[t * a.q_heads + first_head + h] =
+                    close_row(n, first_head + h, kLowest, 0.f).lse;
+        }
+        return;
+    }
+
+    // Where the chunk's positions lie, in bytes from the caches' start; a position that is
+    // not there gets the place of the first slot, which is, and bit 0.
+    const int64_t head_at = static_cast<int64_t>(kv) * a.head_stride;
+    const int tiles = (count + TILE - 1) / TILE;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < tiles * TILE; i += kThreads) {
+        const uint32_t p = static_cast<uint32_t>(s.first + from + (i < count ? i : count - 1));
+        const uint32_t nth = div_u32(p, n.page);
+        const int page = a.pages[t * a.pages_stride + nth];
+        const bool there =
+            i < count && static_cast<uint32_t>(page) < static_cast<uint32_t>(a.num_pages);
+        const int64_t at = (there ? page : 0) * a.page_stride +
+                           static_cast<int64_t>(there ? p - nth * n.page.d : 0) * a.slot_stride +
+                           head_at;
+        place[i] = at * SIZE | (there ? 0 : 1);
+    }
+
+    // The queries' operand: in registers, or, where keys, values and O leave no room for
+    // it, in LDS, the same for all waves.
+    constexpr bool SHARED = DIM > 128;
+    __shared__ U4 q_lds[SHARED ? STEPS * kRowWave : 1];
+    U4 q[STEPS];
+    {
+        const unsigned char *row =
+            static_cast<const unsigned char *>(a.q) +
+            (t * a.q_stride +
+             static_cast<int64_t>(first_head + (column < heads ? column : 0)) * a.head_dim) * SIZE;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int at = 64 * i + 16 * quarter;
+            const bool in = !PAD || at < a.head_dim * SIZE;
+            q[i] = *reinterpret_cast<const U4 *>(row + (in ? at : 0));
+            if (column >= heads || !in) q[i] = U4{0, 0, 0, 0};
+            if (SHARED && wave == 0) q_lds[i * kRowWave + lane] = q[i];
+        }
+    }
+    __syncthreads();
+
+    const unsigned char *k_cache = static_cast<const unsigned char *>(a.k_cache);
+    const unsigned char *v_cache = static_cast<const unsigned char *>(a.v_cache);
+    const int row_bytes = a.head_dim * SIZE;
+    U4 k[SUBS][STEPS];
+    uint32_t v[MINE][PANELS][WORDS];
+    const auto load_keys = [&](int tile) {
+#pragma unroll
+        for (int j = 0; j < SUBS; ++j) {
+            const unsigned char *row = k_cache + (place[tile * TILE + 16 * j + column] & ~int64_t{1});
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                const int at = 64 * i + 16 * quarter;
+                k[j][i] = *reinterpret_cast<const U4 *>(row + (!PAD || at < row_bytes ? at : 0));
+            }
+        }
+    };
+    bool gone[MINE];  // positions that are not there
+    bool any_gone;
+    const auto load_values = [&](int tile) {
+        any_gone = false;
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            const int64_t at = place[tile * TILE + 16 * (j / 4) + 4 * quarter + (j & 3)];
+            gone[j] = at & 1;
+            any_gone |= gone[j];
+            const unsigned char *row = v_cache + (at & ~int64_t{1});
+#pragma unroll
+            for (int p = 0; p < PANELS; ++p) {
+                const int in_row = (16 * p + column) * BYTES;
+                __builtin_memcpy(v[j][p],
+                                 __builtin_assume_aligned(
+                                     row + (!PAD || in_row < row_bytes ? in_row : 0), BYTES),
+                                 BYTES);
+            }
+        }
+    };
+
+    float m = kLowest, l = 0.f;
+    F4 o[PANELS * EACH];
+#pragma unroll
+    for (int i = 0; i < PANELS * EACH; ++i) o[i] = F4{0.f, 0.f, 0.f, 0.f};
+
+    int tile = wave;
+    if (tile < tiles) {
+        load_keys(tile);
+        load_values(tile);
+    }
+    while (tile < tiles) {
+        const int next = tile + kWaves;
+        if (SHARED) {
+            asm volatile("" ::: "memory");  // loaded here, not kept from before the loop
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) q[i] = q_lds[i * kRowWave + lane];
+        }
+        // S: positions x heads
+        F4 x[SUBS];
+#pragma unroll
+        for (int j = 0; j < SUBS; ++j) {
+            x[j] = F4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                U4 w = k[j][i];
+                // behind the head's elements a lane holds others', which may be NaN
+                if (PAD && 64 * i + 16 * quarter >= row_bytes) w = U4{0, 0, 0, 0};
+                x[j] = mma<D>(w, q[i], x[j]);
+            }
+        }
+        if (next < tiles) load_keys(next);
+
+#pragma unroll
+        for (int j = 0; j < SUBS; ++j) {
+            if (a.softcap > 0.f) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    x[j][r] = a.softcap * kLog2e * tanh_of(x[j][r] * a.scale / a.softcap);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * kLog2e;
+            }
+        }
+        if (__builtin_amdgcn_ballot_w64(any_gone)) {
+#pragma unroll
+            for (int j = 0; j < MINE; ++j) {
+                x[j / 4][j & 3] = gone[j] ? -__builtin_inff() : x[j / 4][j & 3];
+                // weight 0 times what the slot holds would be NaN if that is not finite
+                const uint32_t keep = gone[j] ? 0u : ~0u;
+#pragma unroll
+                for (int p = 0; p < PANELS; ++p)
+#pragma unroll
+                    for (int w = 0; w < WORDS; ++w) v[j][p][w] &= keep;
+            }
+        }
+        float high = x[0][0];
+#pragma unroll
+        for (int j = 0; j < SUBS; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) high = __builtin_fmaxf(high, x[j][r]);
+        const auto up = [](Pair<float> p) { return __builtin_fmaxf(p.a, p.b); };
+        high = up(pair<16>(high));
+        high = up(pair<32>(high));
+        high = __builtin_fmaxf(high, m);
+        if (__builtin_amdgcn_ballot_w64(high > m)) {
+            const float shrink = exp2_of(m - high);
+            m = high;
+            l *= shrink;
+#pragma unroll
+            for (int i = 0; i < PANELS * EACH; ++i) o[i] *= shrink;
+        }
+#pragma unroll
+        for (int j = 0; j < SUBS; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[j][r] = exp2_of(x[j][r] - m + UP);
+                l += x[j][r];
+            }
+
+        // O: elements x heads
+        if constexpr (D == SIFAR_FP32) {
+#pragma unroll
+            for (int p = 0; p < PANELS; ++p)
+#pragma unroll
+                for (int i = 0; i < EACH; ++i)
+#pragma unroll
+                    for (int j = 0; j < MINE; ++j)
+                        o[p * EACH + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                            __uint_as_float(v[j][p][i]), x[0][j], o[p * EACH + i], 0, 0, 0);
+        } else {
+            Half<MINE / 2> hi, lo;
+#pragma unroll
+            for (int j = 0; j < MINE / 2; ++j) {
+                const Split w = split<D>(x[j / 2][2 * (j & 1)], x[j / 2][2 * (j & 1) + 1]);
+                hi.w[j] = w.high;
+                lo.w[j] = w.low;
+            }
+#pragma unroll
+            for (int p = 0; p < PANELS; ++p)
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) {
+                    Half<MINE / 2> even, odd;  // columns 2 i and 2 i + 1 of this lane's positions
+#pragma unroll
+                    for (int j = 0; j < MINE / 2; ++j) {
+                        even.w[j] = __builtin_amdgcn_perm(v[2 * j + 1][p][i], v[2 * j][p][i],
+                                                          0x05040100u);
+                        odd.w[j] = __builtin_amdgcn_perm(v[2 * j + 1][p][i], v[2 * j][p][i],
+                                                         0x07060302u);
+                    }
+                    F4 &e = o[p * EACH + 2 * i], &d = o[p * EACH + 2 * i + 1];
+                    e = mma_half<D>(even, hi, e);
+                    d = mma_half<D>(odd, hi, d);
+                    e = mma_half<D>(even, lo, e);
+                    d = mma_half<D>(odd, lo, d);
+                }
+        }
+        if (next < tiles) load_values(next);
+        tile = next;
+    }
+
+    // The waves' sums, joined relative to the largest of their maxima.
+    const auto add = [](Pair<float> p) { return p.a + p.b; };
+    l = add(pair<16>(l));
+    l = add(pair<32>(l));
+    if (quarter == 0) {
+        top[wave][column] = m;
+        sum[wave][column] = l;
+    }
+    __syncthreads();  // also: no wave reads places any more
+    const int busy = tiles < kWaves ? tiles : kWaves;  // waves that had a tile
+    if (wave < busy && column < heads) {
+        float most = top[0][column];
+        for (int w = 1; w < busy; ++w) most = __builtin_fmaxf(most, top[w][column]);
+        const float share = exp2_of(m - most);
+        float *to = outs + (wave * 16 + column) * ROW;
+#pragma unroll
+        for (int p = 0; p < PANELS; ++p)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < EACH; i += 4) {
+                    const int e = p * EACH + i;
+                    *reinterpret_cast<F4 *>(to + p * 16 * EACH + (4 * quarter + r) * EACH + i) =
+                        F4{o[e][r], o[e + 1][r], o[e + 2][r], o[e + 3][r]} * share;
+                }
+    }
+    __syncthreads();
+    const int fours = a.head_dim / 4;
+    for (int i = threadIdx.x; i < heads * fours; i += kThreads) {
+        const int h = i / fours, at = 4 * (i - h * fours);
+        float most = top[0][h];
+        for (int w = 1; w < busy; ++w) most = __builtin_fmaxf(most, top[w][h]);
+        float whole = 0.f;
+        F4 f = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < busy; ++w) {
+            whole += sum[w][h] * exp2_of(top[w][h] - most);
+            f += *reinterpret_cast<const F4 *>(outs + (w * 16 + h) * ROW + at);
+        }
+        const int64_t row = t * a.q_heads + first_head + h;
+        if (splits > 1) {
+            float *ws = static_cast<float *>(a.workspace);
+            const int64_t part = row * splits + piece;
+            *reinterpret_cast<F4 *>(ws + n.parts + part * a.head_dim + at) = f;
+            if (at == 0) {
+                ws[2 * part] = most - UP;
+                ws[2 * part + 1] = whole;
+            }
+        } else {
+            const Close c = close_row(n, first_head + h, most - UP, whole);
+            store4<D>(a.out, t * a.out_stride + static_cast<int64_t>(first_head + h) * a.head_dim +
+                                 at, f * c.inverse);
+            if (a.lse && at == 0) a.lse[row] = c.lse;
+        }
+    }
+}
+
+// A row's chunks, joined in ascending order: sixteen bytes of the output a lane, chunks
+// dealt to as many groups of lanes as there are.
+template <int D>
+__global__ void __launch_bounds__(kThreads) join_kernel(const AttendArgs n, const int wide) {
+    __shared__ float part[2 * kWaves];
+    __shared__ alignas(16) F4 sums[kThreads];
+    const sifar_paged_attention_args &a = n.a;
+    const int64_t t = blockIdx.y;
+    const int head = blockIdx.x, wave = threadIdx.x / 64;
+    const int splits = static_cast<int>(n.splits.d);
+    const Stretch s = stretch(n, t);
+    const int chunks = (s.count + s.chunk - 1) / s.chunk;
+    const int64_t row = t * a.q_heads + head;
+    const float *ml = static_cast<const float *>(a.workspace) + 2 * row * splits;
+    const float *outs = static_cast<const float *>(a.workspace) + n.parts + row * splits * a.head_dim;
+
+    float m = kLowest;
+    for (int i = threadIdx.x; i < chunks; i += kThreads) m = __builtin_fmaxf(m, ml[2 * i]);
+    m = wave_reduce(m, [](float x, float y) { return __builtin_fmaxf(x, y); });
+    if ((threadIdx.x & 63) == 0) part[wave] = m;
+    __syncthreads();
+    m = part[0];
+    for (int w = 1; w < kWaves; ++w) m = __builtin_fmaxf(m, part[w]);
+    float l = 0.f;
+    for (int i = threadIdx.x; i < chunks; i += kThreads) l += ml[2 * i + 1] * exp2_of(ml[2 * i] - m);
+    l = wave_reduce(l, Add{});
+    if ((threadIdx.x & 63) == 0) part[kWaves + wave] = l;
+
+    const int lane = threadIdx.x & (wide - 1), group = threadIdx.x / wide;
+    const int groups = kThreads / wide;
+    const int at = 4 * lane < a.head_dim ? 4 * lane : 0;
+    F4 f = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = group; i < chunks; i += groups)
+        f += *reinterpret_cast<const F4 *>(outs + static_cast<int64_t>(i) * a.head_dim + at) *
+             exp2_of(ml[2 * i] - m);
+    sums[threadIdx.x] = f;
+    __syncthreads();
+    if (group != 0 || 4 * lane >= a.head_dim) return;
+    l = part[kWaves];
+    for (int w = 1; w < kWaves; ++w) l += part[kWaves + w];
+    for (int g = 1; g < groups; ++g) f += sums[g * wide + lane];
+    const Close c = close_row(n, head, m, l);
+    store4<D>(a.out, t * a.out_stride + static_cast<int64_t>(head) * a.head_dim + at, f * c.inverse);
+    if (a.lse && lane == 0) a.lse[row] = c.lse;
+}
+
+// The most chunks that a sequence is cut into: as many as fill the GPU, none below
+// kMinChunk positions or above kMaxChunk.
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int64_t tiles_of(int64_t q_heads, int64_t kv_heads) { return ceil_div(q_heads / kv_heads, 16); }
+
+int64_t splits_of(int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t reach) {
+    const int64_t groups = tokens * kv_heads * tiles_of(q_heads, kv_heads);
+    const int64_t fill = ceil_div(kWorkgroups, groups), fine = ceil_div(reach, kMinChunk),
+                  coarse = ceil_div(reach, kMaxChunk);
+    const int64_t want = fill < fine ? fill : fine;
+    return want > coarse ? want : coarse;
+}
+
+// Floats of a chunk's row in the workspace: its maximum, its sum, its output.
+int64_t part_floats(int64_t head_dim) { return head_dim + 2; }
+
+template <int D, int DIM>
+void launch_attend(const AttendArgs &n, dim3 grid, hipStream_t s) {
+    if (n.a.head_dim == DIM) attend_kernel<D, DIM, false><<<grid, kThreads, 0, s>>>(n);
+    else attend_kernel<D, DIM, true><<<grid, kThreads, 0, s>>>(n);
+}
+
+int64_t reach_of(const sifar_paged_attention_args &a) {
+    const int64_t slots = static_cast<int64_t>(a.max_pages) * a.page_size;
+    return a.max_length < slots ? a.max_length : slots;
+}
+
+int64_t most_of(const sifar_paged_attention_args &a) {
+    const int64_t reach = reach_of(a);
+    return a.window > 0 && a.window < reach ? a.window : reach;
+}
+
+template <int D>
+hipError_t launch(const sifar_paged_attention_args &a, hipStream_t s) {
+    const int64_t splits = splits_of(a.tokens, a.q_heads, a.kv_heads, most_of(a));
+    AttendArgs n{};
+    n.a = a;
+    n.page = make_div(static_cast<uint32_t>(a.page_size));
+    n.splits = make_div(static_cast<uint32_t>(splits));
+    n.group = a.q_heads / a.kv_heads;
+    n.reach = static_cast<int32_t>(reach_of(a));
+    // 16-byte aligned
+    n.parts = (2 * static_cast<int64_t>(a.tokens) * a.q_heads * splits + 3) / 4 * 4;
+    const dim3 grid(a.kv_heads * tiles_of(a.q_heads, a.kv_heads), splits, a.tokens);
+    const int wide = a.head_dim <= 64 ? 64 : a.head_dim <= 128 ? 128 : 256;
+    if (wide == 64) launch_attend<D, 64>(n, grid, s);
+    else if (wide == 128) launch_attend<D, 128>(n, grid, s);
+    else launch_attend<D, 256>(n, grid, s);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || splits == 1) return e;
+    join_kernel<D><<<dim3(a.q_heads, a.tokens), kThreads, 0, s>>>(n, wide / 4);
+    return hipGetLastError();
+}
+
+bool good_sizes(int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                int64_t max_length) {
+    return tokens >= 0 && tokens <= SIFAR_ATTENTION_MAX_TOKENS && kv_heads >= 1 &&
+           kv_heads <= SIFAR_CACHE_MAX_HEADS && q_heads >= 1 && q_heads <= SIFAR_CACHE_MAX_HEADS &&
+           q_heads % kv_heads == 0 && head_dim >= 8 && head_dim <= SIFAR_CACHE_MAX_DIM &&
+           head_dim % 8 == 0 && max_length >= 1 && max_length <= SIFAR_ATTENTION_MAX_LENGTH;
+}
+
+bool good(const sifar_paged_attention_args &a) {
+    if (!good_dtype(a.dtype) ||
+        !good_sizes(a.tokens, a.q_heads, a.kv_heads, a.head_dim, a.max_length))
+        return false;
+    if (a.page_size < 1 || a.page_size > SIFAR_CACHE_MAX_PAGE || a.num_pages < 1 ||
+        a.max_pages < 1)
+        return false;
+    if (a.window < 0 || !__builtin_isfinite(a.scale) || !(a.softcap >= 0.f) ||
+        !__builtin_isfinite(a.softcap))
+        return false;
+    const Paged cache = paged(a.num_pages, a.page_size, a.kv_heads, a.page_stride, a.slot_stride,
+                              a.head_stride, a.head_dim);
+    const int64_t elements = extent(cache);
+    if (elements == 0) return false;
+    if (a.pages_stride < 0 || a.pages_stride > kMaxStride) return false;
+    if (a.tokens == 0) return true;
+    if (!a.q || !a.k_cache || !a.v_cache || !a.pages || !a.lengths || !a.out) return false;
+    for (const void *p : {a.q, a.k_cache, a.v_cache, static_cast<const void *>(a.out),
+                          static_cast<const void *>(a.workspace)})
+        if (!aligned16(p)) return false;
+    for (const void *p : {static_cast<const void *>(a.pages), static_cast<const void *>(a.lengths),
+                          static_cast<const void *>(a.sinks), static_cast<const void *>(a.lse)})
+        if (!aligned4(p)) return false;
+    const int64_t width = static_cast<int64_t>(a.q_heads) * a.head_dim;
+    if (!good_stride(a.q_stride, a.tokens, width) || !good_stride(a.out_stride, a.tokens, width))
+        return false;
+    const int64_t splits = splits_of(a.tokens, a.q_heads, a.kv_heads, most_of(a));
+    const int64_t need = sifar_paged_attention_workspace(a.tokens, a.q_heads, a.kv_heads,
+                                                         a.head_dim, a.max_length);
+    if (splits > 1 && (!a.workspace || a.workspace_bytes < need)) return false;
+
+    const uint64_t size = size_of(a.dtype), tokens = static_cast<uint64_t>(a.tokens);
+    const Rows q = rows_of(a.q, a.dtype, a.tokens, a.q_stride, width);
+    const Rows out[] = {rows_of(a.out, a.dtype, a.tokens, a.out_stride, width),
+                        span_of(a.lse, a.lse ? 4 * tokens * a.q_heads : 0),
+                        span_of(a.workspace, splits > 1 ? static_cast<uint64_t>(need) : 0)};
+    const Rows in[] = {span_of(a.k_cache, static_cast<uint64_t>(elements) * size),
+                       span_of(a.v_cache, static_cast<uint64_t>(elements) * size),
+                       span_of(a.pages, 4 * ((tokens - 1) * a.pages_stride + a.max_pages)),
+                       span_of(a.lengths, 4 * tokens),
+                       span_of(a.sinks, a.sinks ? 4ull * a.q_heads : 0)};
+    for (int o = 0; o < 3; ++o) {
+        for (const Rows &i : in)
+            if (may_overlap(out[o], i)) return false;
+        for (int p = 0; p < o; ++p)
+            if (may_overlap(out[o], out[p])) return false;
+        if (may_overlap(out[o], q) && !(o == 0 && same_rows(out[o], q))) return false;
+    }
+    return true;
+}
+
+}  // namespace
+}  // namespace sifar
+
+extern "C" int64_t sifar_paged_attention_workspace(int32_t tokens, int32_t q_heads,
+                                                   int32_t kv_heads, int32_t head_dim,
+                                                   int32_t max_length) {
+    using namespace sifar;
+    if (!good_sizes(tokens, q_heads, kv_heads, head_dim, max_length)) return SIFAR_EINVAL;
+    // Chunks of all sequences: no more than fine ones make, nor than fill the GPU and one
+    // for each, or coarse ones make. Each bound grows with tokens and max_length.
+    const int64_t groups = static_cast<int64_t>(tokens) * kv_heads * tiles_of(q_heads, kv_heads);
+    const int64_t fine = groups * ceil_div(max_length, kMinChunk);
+    const int64_t fill = kWorkgroups + groups, coarse = groups * ceil_div(max_length, kMaxChunk);
+    const int64_t more = fill > coarse ? fill : coarse;
+    const int64_t chunks = fine < more ? fine : more;
+    if (max_length <= kMinChunk || tokens == 0) return 0;
+    // a group's chunk holds a row for each of its query heads (16 at most)
+    const int64_t rows = q_heads / kv_heads < 16 ? q_heads / kv_heads : 16;
+    return (chunks * rows * part_floats(head_dim) + 4) * 4;
+}
+
+extern "C" int sifar_paged_attention(const sifar_paged_attention_args *args, void *stream) {
+    using namespace sifar;
+    if (!args || !good(*args)) return SIFAR_EINVAL;
+    const sifar_paged_attention_args &a = *args;
+    if (a.tokens == 0) return SIFAR_OK;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const hipError_t e = a.dtype == SIFAR_FP32   ? launch<SIFAR_FP32>(a, s)
+                         : a.dtype == SIFAR_BF16 ? launch<SIFAR_BF16>(a, s)
+                                                 : launch<SIFAR_FP16>(a, s);
+    return e == hipSuccess ? SIFAR_OK : SIFAR_EHIP;
+}
