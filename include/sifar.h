@@ -741,6 +741,7 @@ int64_t sifar_sample_workspace(int32_t tokens, int32_t vocab);
 #define SIFAR_CACHE_MAX_DIM 256
 #define SIFAR_CACHE_MAX_HEADS 1024
 #define SIFAR_CACHE_MAX_PAGE 65536
+#define SIFAR_CACHE_MAX_ELEMENTS 34359738368
 typedef struct {
     int32_t dtype;
     int32_t tokens;

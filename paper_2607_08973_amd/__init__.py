@@ -83,6 +83,7 @@ SIFAR_SAMPLE_MAX_VOCAB = 1048576
 SIFAR_CACHE_MAX_DIM = 256
 SIFAR_CACHE_MAX_HEADS = 1024
 SIFAR_CACHE_MAX_PAGE = 65536
+SIFAR_CACHE_MAX_ELEMENTS = 34359738368
 SIFAR_ATTENTION_MAX_TOKENS = 32768
 SIFAR_ATTENTION_MAX_LENGTH = 16777216
 SIFAR_EXPERTS_SILU = 0

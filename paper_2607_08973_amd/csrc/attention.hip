@@ -22,9 +22,10 @@
 // weights are good to 2^-17 and the output's one rounding is its last; the second
 // product costs matrix time that the bytes leave free.
 //
-// A workgroup takes one cache head of one sequence, or a chunk of its positions where
-// that leaves too few workgroups; its four waves take every fourth tile and join in LDS.
-// Chunks' sums go to the workspace, unscaled, and a second launch joins them.
+// A workgroup takes one cache head of one sequence, or a chunk of its positions where that
+// leaves too few workgroups or too uneven ones; its four waves take every fourth tile and
+// join in LDS. Chunks' sums go to the workspace, not yet divided, and a second launch joins
+// them.
 #include <hip/hip_runtime.h>
 
 #include "paged.h"
@@ -37,10 +38,10 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kRowWave;
-constexpr int kMinChunk = 256;   // positions of a shared sequence's chunk, at least
-constexpr int kMaxChunk = 2048;  // and at most: their places fill 16 KB of LDS
-constexpr int kRound = 128;      // chunks are whole tiles of all waves
-constexpr int kWorkgroups = 2048;  // sequences are shared until there are so many
+constexpr int kMinChunk = 128;   // positions of a shared sequence's chunk, at least
+constexpr int kMaxChunk = 1536;  // and at most
+constexpr int kCus = 256;
+constexpr int64_t kSmall = 262144;  // bytes of a workgroup's keys and values
 constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e430p-1f;
 constexpr float kLowest = -0x1.fffffep127f;  // below every finite score
 
@@ -50,7 +51,8 @@ struct AttendArgs {
     DivU32 splits;  // by the most chunks of a sequence
     int32_t group;  // query heads of a cache head
     int32_t reach;  // lengths are cut to this
-    int64_t parts;  // from the workspace's start to the chunks' outputs, in floats
+    int32_t round;  // chunks are multiples of this, a power of two
+    int64_t at_outs;  // the chunks' outputs from the workspace's start, in floats
 };
 
 // Which positions a sequence has, and how long its chunks are.
@@ -58,15 +60,14 @@ struct Stretch {
     int first, count, chunk;
 };
 __device__ __forceinline__ Stretch stretch(const AttendArgs &n, int64_t t) {
-    const int most = n.reach;
     int length = n.a.lengths[t];
-    length = length < 0 ? 0 : length > most ? most : length;
+    length = length < 0 ? 0 : length > n.reach ? n.reach : length;
     Stretch s;
     s.first = n.a.window > 0 && length > n.a.window ? length - n.a.window : 0;
     s.count = length - s.first;
     const int share =
         static_cast<int>(div_u32(static_cast<uint32_t>(s.count) + n.splits.d - 1, n.splits));
-    s.chunk = (share + kRound - 1) / kRound * kRound;
+    s.chunk = (share + n.round - 1) & -n.round;
     if (s.chunk < kMinChunk) s.chunk = kMinChunk;
     return s;
 }
@@ -86,6 +87,17 @@ __device__ __forceinline__ float tanh_of(float y) {
     const float far =
         __builtin_copysignf(1.f - 2.f / (exp2_of(2.f * kLog2e * a) + 1.f), y);
     return a < 0.35f ? near : far;
+}
+
+template <int N>
+using Words = uint32_t __attribute__((ext_vector_type(N)));
+
+// Keys and values: ONCE, past the caches, where there are more of them than the caches keep
+// until the next call.
+template <class T, bool ONCE>
+__device__ __forceinline__ T load_cache(const unsigned char *p) {
+    const T *at = reinterpret_cast<const T *>(p);
+    return ONCE ? __builtin_nontemporal_load(at) : *at;
 }
 
 // Four adjacent outputs.
@@ -115,14 +127,33 @@ __device__ __forceinline__ Close close_row(const AttendArgs &n, int head, float 
     return {l == 0.f ? 0.f : 1.f / l, (l == 0.f ? -__builtin_inff() : (m + log2_of(l)) * kLn2)};
 }
 
+// The lane's index, as a value of its own: what a loop's body derives from it is computed
+// there, and not kept in registers around the loops inside, where keys, values and sums
+// need them.
+__device__ __forceinline__ int own_thread() {
+    int i = threadIdx.x;
+    asm volatile("" : "+v"(i));
+    return i;
+}
+
+// Positions of a tile.
+constexpr int tile_of(int dtype, int dim) { return dtype == SIFAR_FP32 || dim > 128 ? 16 : 32; }
+
+// Workgroups that a CU holds at once, as the registers allow.
+constexpr int held_by_a_cu(int dtype, int dim, bool padded) {
+    return dim == 64    ? (dtype == SIFAR_FP32 && !padded ? 5 : 4)
+           : dim == 128 ? 3
+                        : (dtype == SIFAR_FP32 ? 1 : 2);
+}
+
 // D: element type. DIM: 64, 128 or 256, head_dim or the next above it (PAD).
-template <int D, int DIM, bool PAD>
-__global__ void __launch_bounds__(kThreads, D == SIFAR_FP32 && DIM > 128 ? 1 : 2)
+template <int D, int DIM, bool PAD, bool ONCE>
+__global__ void __launch_bounds__(kThreads, held_by_a_cu(D, DIM, PAD))
 attend_kernel(const AttendArgs n) {
     constexpr int SIZE = D == SIFAR_FP32 ? 4 : 2;
     constexpr int STEPS = DIM * SIZE / 64;          // of 64 bytes of a row of keys
     // positions: half as many where keys, values and O would not fit the registers
-    constexpr int TILE = D == SIFAR_FP32 || DIM > 128 ? 16 : 32;
+        constexpr int TILE = tile_of(D, DIM);
     constexpr int SUBS = TILE / 16;
     constexpr int MINE = TILE / 4;                  // positions whose values a lane loads
     // 16 lanes hold a row of values in panels, up to 16 bytes a lane each
@@ -134,60 +165,91 @@ attend_kernel(const AttendArgs n) {
     // keep their bits. bf16 has fp32's exponents.
     constexpr float UP = D == SIFAR_FP16 ? 14.f : 0.f;
 
-    constexpr int kPlaces = kMaxChunk * 8, kOut = kWaves * 16 * ROW * 4;
-    __shared__ alignas(16) unsigned char lds[kPlaces > kOut ? kPlaces : kOut];
+    constexpr int kPlaceBytes = kMaxChunk * 4, kOutBytes = kWaves * 16 * ROW * 4;
+    __shared__ alignas(16) unsigned char lds[kPlaceBytes > kOutBytes ? kPlaceBytes : kOutBytes];
     __shared__ float top[kWaves][16], sum[kWaves][16];
-    int64_t *place = reinterpret_cast<int64_t *>(lds);
+    __shared__ uint32_t gone[kMaxChunk / 32];  // a bit for each position that is not there
+    uint32_t *place = reinterpret_cast<uint32_t *>(lds);
     float *outs = reinterpret_cast<float *>(lds);
 
     const sifar_paged_attention_args &a = n.a;
     const int64_t t = blockIdx.z;
-    const int piece = blockIdx.y, splits = gridDim.y;
-    const int kv = blockIdx.x % a.kv_heads, tile16 = blockIdx.x / a.kv_heads;
+    const int piece = blockIdx.x, splits = gridDim.x;
+    const int kv = blockIdx.y % a.kv_heads, tile16 = blockIdx.y / a.kv_heads;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int column = lane & 15, quarter = lane >> 4;
     const int heads = n.group - 16 * tile16 < 16 ? n.group - 16 * tile16 : 16;  // columns in use
     const int first_head = kv * n.group + 16 * tile16;
+    const int fours = a.head_dim / 4;
 
     const Stretch s = stretch(n, t);
     const int from = piece * s.chunk;  // behind s.first
     const int count = s.count - from < s.chunk ? s.count - from : s.chunk;
     if (count <= 0) {  // the same for the workgroup
         if (splits > 1) return;  // not a chunk: the second launch knows
-        for (int i = threadIdx.x; i < heads * (a.head_dim / 4); i += kThreads) {
-            const int h = i / (a.head_dim / 4);
+        for (int i = threadIdx.x; i < heads * fours; i += kThreads) {
             store4<D>(a.out, t * a.out_stride + static_cast<int64_t>(first_head) * a.head_dim +
                                  4 * i, F4{0.f, 0.f, 0.f, 0.f});
-            if (a.lse && i - h * (a.head_dim / 4) == 0)
-                a.lse[t * a.q_heads + first_head + h] =
-                    close_row(n, first_head + h, kLowest, 0.f).lse;
+            if (a.lse && i < heads)
+                a.lse[t * a.q_heads + first_head + i] =
+                    close_row(n, first_head + i, kLowest, 0.f).lse;
         }
         return;
     }
 
-    // Where the chunk's positions lie, in bytes from the caches' start; a position that is
-    // not there gets the place of the first slot, which is, and bit 0.
-    const int64_t head_at = static_cast<int64_t>(kv) * a.head_stride;
-    const int tiles = (count + TILE - 1) / TILE;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < tiles * TILE; i += kThreads) {
-        const uint32_t p = static_cast<uint32_t>(s.first + from + (i < count ? i : count - 1));
-        const uint32_t nth = div_u32(p, n.page);
-        const int page = a.pages[t * a.pages_stride + nth];
-        const bool there =
-            i < count && static_cast<uint32_t>(page) < static_cast<uint32_t>(a.num_pages);
-        const int64_t at = (there ? page : 0) * a.page_stride +
-                           static_cast<int64_t>(there ? p - nth * n.page.d : 0) * a.slot_stride +
-                           head_at;
-        place[i] = at * SIZE | (there ? 0 : 1);
-    }
-
+    const int64_t head_at = static_cast<int64_t>(kv) * a.head_stride * SIZE;
+    const unsigned char *k_cache = static_cast<const unsigned char *>(a.k_cache) + head_at;
+    const unsigned char *v_cache = static_cast<const unsigned char *>(a.v_cache) + head_at;
+    const int row_bytes = a.head_dim * SIZE;
     // The queries' operand: in registers, or, where keys, values and O leave no room for
     // it, in LDS, the same for all waves.
-    constexpr bool SHARED = DIM > 128;
+    constexpr bool SHARED = DIM > 64;
     __shared__ U4 q_lds[SHARED ? STEPS * kRowWave : 1];
     U4 q[STEPS];
+    U4 k[SUBS][STEPS];
+    uint32_t v[MINE][PANELS][WORDS];
+    // Lanes behind the end of a head's row load its first bytes and drop them (times the
+    // queries' zeros, what is not finite would count). The row ends in the second half.
+    constexpr int SURE = !PAD ? STEPS : DIM > 64 ? STEPS / 2 : 0;
+    const unsigned char *k_lane = k_cache + 16 * quarter, *k_end[STEPS];
+    uint32_t keep[STEPS];
+#pragma unroll
+    for (int i = SURE; i < STEPS; ++i) {
+        keep[i] = 64 * i + 16 * quarter < row_bytes ? ~0u : 0u;
+        k_end[i] = k_cache + (keep[i] & (64 * i + 16 * quarter));
+    }
+    const unsigned char *v_lane[PANELS];
+#pragma unroll
+    for (int p = 0; p < PANELS; ++p)
+        v_lane[p] = v_cache + (!PAD || (16 * p + column) * BYTES < row_bytes ? (16 * p + column) * BYTES : 0);
+    const auto load_keys = [&](int tile) {
+#pragma unroll
+        for (int j = 0; j < SUBS; ++j) {
+            const uint64_t at = static_cast<uint64_t>(place[tile * TILE + 16 * j + column]) * (8 * SIZE);
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i)
+                k[j][i] = load_cache<U4, ONCE>(i < SURE ? k_lane + at + 64 * i : k_end[i] + at);
+        }
+    };
+    const auto load_values = [&](int tile) {
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            const uint64_t at =
+                static_cast<uint64_t>(place[tile * TILE + 16 * (j / 4) + 4 * quarter + (j & 3)]) *
+                (8 * SIZE);
+#pragma unroll
+            for (int p = 0; p < PANELS; ++p) {
+                const Words<WORDS> w = load_cache<Words<WORDS>, ONCE>(v_lane[p] + at);
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) v[j][p][i] = w[i];
+            }
+        }
+    };
+
+    const uint32_t page_eights = static_cast<uint32_t>(a.page_stride / 8);
+    const uint32_t slot_eights = static_cast<uint32_t>(a.slot_stride / 8);
+    // The queries' loads go out before the places', and are used behind them.
     {
         const unsigned char *row =
             static_cast<const unsigned char *>(a.q) +
@@ -196,68 +258,59 @@ attend_kernel(const AttendArgs n) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const int at = 64 * i + 16 * quarter;
-            const bool in = !PAD || at < a.head_dim * SIZE;
-            q[i] = *reinterpret_cast<const U4 *>(row + (in ? at : 0));
-            if (column >= heads || !in) q[i] = U4{0, 0, 0, 0};
-            if (SHARED && wave == 0) q_lds[i * kRowWave + lane] = q[i];
+            q[i] = *reinterpret_cast<const U4 *>(row + (!PAD || at < row_bytes ? at : 0));
         }
     }
+    // Where positions lie, in eights of elements from the head's first; a position that is
+    // not there gets the place of the first slot, which is, and its bit.
+    const int tiles = (count + TILE - 1) / TILE;
+    constexpr int EACH_LANE = kMaxChunk / kThreads;
+    int pages[EACH_LANE];  // all loaded before one is used
+    uint32_t slots[EACH_LANE];
+#pragma unroll
+    for (int j = 0; j < EACH_LANE; ++j) {
+        const int i = j * kThreads + static_cast<int>(threadIdx.x);
+        const uint32_t p = static_cast<uint32_t>(s.first + from + (i < count ? i : count - 1));
+        const uint32_t nth = div_u32(p, n.page);
+        slots[j] = p - nth * n.page.d;
+        pages[j] = a.pages[t * a.pages_stride + nth];
+    }
+#pragma unroll
+    for (int j = 0; j < EACH_LANE; ++j) {
+        const int i = j * kThreads + static_cast<int>(threadIdx.x);
+        const bool there = i < count &&
+                           static_cast<uint32_t>(pages[j]) < static_cast<uint32_t>(a.num_pages);
+        const uint64_t at = static_cast<uint64_t>(pages[j]) * page_eights +
+                            static_cast<uint64_t>(slots[j]) * slot_eights;
+        place[i] = there ? static_cast<uint32_t>(at) : 0u;
+        const uint64_t missing = __builtin_amdgcn_ballot_w64(!there);
+        if ((i & 31) == 0) gone[i / 32] = static_cast<uint32_t>(missing >> (i & 63));
+    }
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        const bool in = column < heads && (!PAD || 64 * i + 16 * quarter < row_bytes);
+        q[i] &= in ? ~0u : 0u;
+        if (SHARED && wave == 0) q_lds[i * kRowWave + lane] = q[i];
+    }
     __syncthreads();
-
-    const unsigned char *k_cache = static_cast<const unsigned char *>(a.k_cache);
-    const unsigned char *v_cache = static_cast<const unsigned char *>(a.v_cache);
-    const int row_bytes = a.head_dim * SIZE;
-    U4 k[SUBS][STEPS];
-    uint32_t v[MINE][PANELS][WORDS];
-    const auto load_keys = [&](int tile) {
-#pragma unroll
-        for (int j = 0; j < SUBS; ++j) {
-            const unsigned char *row = k_cache + (place[tile * TILE + 16 * j + column] & ~int64_t{1});
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                const int at = 64 * i + 16 * quarter;
-                k[j][i] = *reinterpret_cast<const U4 *>(row + (!PAD || at < row_bytes ? at : 0));
-            }
-        }
-    };
-    bool gone[MINE];  // positions that are not there
-    bool any_gone;
-    const auto load_values = [&](int tile) {
-        any_gone = false;
-#pragma unroll
-        for (int j = 0; j < MINE; ++j) {
-            const int64_t at = place[tile * TILE + 16 * (j / 4) + 4 * quarter + (j & 3)];
-            gone[j] = at & 1;
-            any_gone |= gone[j];
-            const unsigned char *row = v_cache + (at & ~int64_t{1});
-#pragma unroll
-            for (int p = 0; p < PANELS; ++p) {
-                const int in_row = (16 * p + column) * BYTES;
-                __builtin_memcpy(v[j][p],
-                                 __builtin_assume_aligned(
-                                     row + (!PAD || in_row < row_bytes ? in_row : 0), BYTES),
-                                 BYTES);
-            }
-        }
-    };
 
     float m = kLowest, l = 0.f;
     F4 o[PANELS * EACH];
 #pragma unroll
     for (int i = 0; i < PANELS * EACH; ++i) o[i] = F4{0.f, 0.f, 0.f, 0.f};
 
-    int tile = wave;
-    if (tile < tiles) {
-        load_keys(tile);
-        load_values(tile);
-    }
-    while (tile < tiles) {
-        const int next = tile + kWaves;
+    // A tile's part of the sums; with MORE the wave's next one is loaded on the way. (The
+    // last one stands behind the loop: where its loads were left out by a branch inside,
+    // the registers of values were reused too early, in fp32 heads of 256.)
+    const auto take = [&](int tile, auto more) {
+        constexpr bool MORE = decltype(more)::value;
         if (SHARED) {
             asm volatile("" ::: "memory");  // loaded here, not kept from before the loop
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) q[i] = q_lds[i * kRowWave + lane];
         }
+        uint32_t missing = __builtin_amdgcn_readfirstlane(gone[tile * TILE / 32]);
+        if (TILE == 16) missing = missing >> (16 * (tile & 1)) & 0xFFFFu;
         // S: positions x heads
         F4 x[SUBS];
 #pragma unroll
@@ -265,13 +318,11 @@ attend_kernel(const AttendArgs n) {
             x[j] = F4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                U4 w = k[j][i];
-                // behind the head's elements a lane holds others', which may be NaN
-                if (PAD && 64 * i + 16 * quarter >= row_bytes) w = U4{0, 0, 0, 0};
-                x[j] = mma<D>(w, q[i], x[j]);
+                if (i >= SURE) k[j][i] &= keep[i];
+                x[j] = mma<D>(k[j][i], q[i], x[j]);
             }
         }
-        if (next < tiles) load_keys(next);
+        if constexpr (MORE) load_keys(tile + kWaves);
 
 #pragma unroll
         for (int j = 0; j < SUBS; ++j) {
@@ -284,12 +335,13 @@ attend_kernel(const AttendArgs n) {
                 for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * kLog2e;
             }
         }
-        if (__builtin_amdgcn_ballot_w64(any_gone)) {
+        if (missing) {
 #pragma unroll
             for (int j = 0; j < MINE; ++j) {
-                x[j / 4][j & 3] = gone[j] ? -__builtin_inff() : x[j / 4][j & 3];
+                const bool not_there = missing >> (16 * (j / 4) + 4 * quarter + (j & 3)) & 1;
+                x[j / 4][j & 3] = not_there ? -__builtin_inff() : x[j / 4][j & 3];
                 // weight 0 times what the slot holds would be NaN if that is not finite
-                const uint32_t keep = gone[j] ? 0u : ~0u;
+                const uint32_t keep = not_there ? 0u : ~0u;
 #pragma unroll
                 for (int p = 0; p < PANELS; ++p)
 #pragma unroll
@@ -357,25 +409,32 @@ attend_kernel(const AttendArgs n) {
                     d = mma_half<D>(odd, lo, d);
                 }
         }
-        if (next < tiles) load_values(next);
-        tile = next;
+        if constexpr (MORE) load_values(tile + kWaves);
+    };
+    if (wave < tiles) {
+        int tile = wave;
+        load_keys(tile);
+        load_values(tile);
+        for (; tile + kWaves < tiles; tile += kWaves) take(tile, std::true_type{});
+        take(tile, std::false_type{});
     }
 
     // The waves' sums, joined relative to the largest of their maxima.
+    const int thread = own_thread(), own_column = thread & 15, own_quarter = thread >> 4 & 3;
     const auto add = [](Pair<float> p) { return p.a + p.b; };
     l = add(pair<16>(l));
     l = add(pair<32>(l));
-    if (quarter == 0) {
-        top[wave][column] = m;
-        sum[wave][column] = l;
+    if (own_quarter == 0) {
+        top[wave][own_column] = m;
+        sum[wave][own_column] = l;
     }
     __syncthreads();  // also: no wave reads places any more
-    const int busy = tiles < kWaves ? tiles : kWaves;  // waves that had a tile
-    if (wave < busy && column < heads) {
-        float most = top[0][column];
-        for (int w = 1; w < busy; ++w) most = __builtin_fmaxf(most, top[w][column]);
-        const float share = exp2_of(m - most);
-        float *to = outs + (wave * 16 + column) * ROW;
+    const int busy = count < kWaves * TILE ? (count + TILE - 1) / TILE : kWaves;  // had a tile
+    if (wave < busy && own_column < heads) {
+        float most_of_all = top[0][own_column];
+        for (int w = 1; w < busy; ++w) most_of_all = __builtin_fmaxf(most_of_all, top[w][own_column]);
+        const float scale = exp2_of(m - most_of_all);
+        float *to = outs + (wave * 16 + own_column) * ROW;
 #pragma unroll
         for (int p = 0; p < PANELS; ++p)
 #pragma unroll
@@ -383,33 +442,32 @@ attend_kernel(const AttendArgs n) {
 #pragma unroll
                 for (int i = 0; i < EACH; i += 4) {
                     const int e = p * EACH + i;
-                    *reinterpret_cast<F4 *>(to + p * 16 * EACH + (4 * quarter + r) * EACH + i) =
-                        F4{o[e][r], o[e + 1][r], o[e + 2][r], o[e + 3][r]} * share;
+                    *reinterpret_cast<F4 *>(to + p * 16 * EACH + (4 * own_quarter + r) * EACH + i) =
+                        F4{o[e][r], o[e + 1][r], o[e + 2][r], o[e + 3][r]} * scale;
                 }
     }
     __syncthreads();
-    const int fours = a.head_dim / 4;
-    for (int i = threadIdx.x; i < heads * fours; i += kThreads) {
+    for (int i = thread; i < heads * fours; i += kThreads) {
         const int h = i / fours, at = 4 * (i - h * fours);
-        float most = top[0][h];
-        for (int w = 1; w < busy; ++w) most = __builtin_fmaxf(most, top[w][h]);
+        float most_of_all = top[0][h];
+        for (int w = 1; w < busy; ++w) most_of_all = __builtin_fmaxf(most_of_all, top[w][h]);
         float whole = 0.f;
         F4 f = {0.f, 0.f, 0.f, 0.f};
         for (int w = 0; w < busy; ++w) {
-            whole += sum[w][h] * exp2_of(top[w][h] - most);
+            whole += sum[w][h] * exp2_of(top[w][h] - most_of_all);
             f += *reinterpret_cast<const F4 *>(outs + (w * 16 + h) * ROW + at);
         }
         const int64_t row = t * a.q_heads + first_head + h;
         if (splits > 1) {
             float *ws = static_cast<float *>(a.workspace);
             const int64_t part = row * splits + piece;
-            *reinterpret_cast<F4 *>(ws + n.parts + part * a.head_dim + at) = f;
+            *reinterpret_cast<F4 *>(ws + n.at_outs + part * a.head_dim + at) = f;
             if (at == 0) {
-                ws[2 * part] = most - UP;
+                ws[2 * part] = most_of_all - UP;
                 ws[2 * part + 1] = whole;
             }
         } else {
-            const Close c = close_row(n, first_head + h, most - UP, whole);
+            const Close c = close_row(n, first_head + h, most_of_all - UP, whole);
             store4<D>(a.out, t * a.out_stride + static_cast<int64_t>(first_head + h) * a.head_dim +
                                  at, f * c.inverse);
             if (a.lse && at == 0) a.lse[row] = c.lse;
@@ -417,74 +475,113 @@ attend_kernel(const AttendArgs n) {
     }
 }
 
-// A row's chunks, joined in ascending order: sixteen bytes of the output a lane, chunks
-// dealt to as many groups of lanes as there are.
+// A row's chunks, joined in ascending order: sixteen bytes of the output a lane, `wide`
+// lanes, chunks dealt to as many groups of lanes as there are.
 template <int D>
 __global__ void __launch_bounds__(kThreads) join_kernel(const AttendArgs n, const int wide) {
     __shared__ float part[2 * kWaves];
     __shared__ alignas(16) F4 sums[kThreads];
     const sifar_paged_attention_args &a = n.a;
     const int64_t t = blockIdx.y;
-    const int head = blockIdx.x, wave = threadIdx.x / 64;
-    const int splits = static_cast<int>(n.splits.d);
+    const int head = blockIdx.x, splits = static_cast<int>(n.splits.d);
+    const int wave = threadIdx.x / 64, waves = blockDim.x / 64, threads = blockDim.x;
     const Stretch s = stretch(n, t);
     const int chunks = (s.count + s.chunk - 1) / s.chunk;
     const int64_t row = t * a.q_heads + head;
     const float *ml = static_cast<const float *>(a.workspace) + 2 * row * splits;
-    const float *outs = static_cast<const float *>(a.workspace) + n.parts + row * splits * a.head_dim;
+    const float *outs =
+        static_cast<const float *>(a.workspace) + n.at_outs + row * splits * a.head_dim;
+    const int lane = threadIdx.x & (wide - 1), group = threadIdx.x / wide;
+    const int groups = threads / wide;
+    const int at = 4 * (wide * static_cast<int>(blockIdx.z) + lane);
+    const bool in = at < a.head_dim;
 
-    float m = kLowest;
-    for (int i = threadIdx.x; i < chunks; i += kThreads) m = __builtin_fmaxf(m, ml[2 * i]);
+    // The first chunks' outputs are on their way while the maxima are looked through.
+    constexpr int AHEAD = 4;
+    F4 x[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+        const int i = group + j * groups;
+        x[j] = *reinterpret_cast<const F4 *>(
+            outs + static_cast<int64_t>(i < chunks ? i : 0) * a.head_dim + (in ? at : 0));
+    }
+    float m = kLowest, l = 0.f;
+    for (int i = threadIdx.x; i < chunks; i += threads) m = __builtin_fmaxf(m, ml[2 * i]);
     m = wave_reduce(m, [](float x, float y) { return __builtin_fmaxf(x, y); });
-    if ((threadIdx.x & 63) == 0) part[wave] = m;
-    __syncthreads();
-    m = part[0];
-    for (int w = 1; w < kWaves; ++w) m = __builtin_fmaxf(m, part[w]);
-    float l = 0.f;
-    for (int i = threadIdx.x; i < chunks; i += kThreads) l += ml[2 * i + 1] * exp2_of(ml[2 * i] - m);
+    if (waves > 1) {
+        if ((threadIdx.x & 63) == 0) part[wave] = m;
+        __syncthreads();
+        for (int w = 0; w < waves; ++w) m = __builtin_fmaxf(m, part[w]);
+    }
+    for (int i = threadIdx.x; i < chunks; i += threads) l += ml[2 * i + 1] * exp2_of(ml[2 * i] - m);
     l = wave_reduce(l, Add{});
     if ((threadIdx.x & 63) == 0) part[kWaves + wave] = l;
 
-    const int lane = threadIdx.x & (wide - 1), group = threadIdx.x / wide;
-    const int groups = kThreads / wide;
-    const int at = 4 * lane < a.head_dim ? 4 * lane : 0;
     F4 f = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+        const int i = group + j * groups;
+        if (i < chunks) f += x[j] * exp2_of(ml[2 * i] - m);
+    }
 #pragma unroll 4
-    for (int i = group; i < chunks; i += groups)
-        f += *reinterpret_cast<const F4 *>(outs + static_cast<int64_t>(i) * a.head_dim + at) *
-             exp2_of(ml[2 * i] - m);
+    for (int i = group + AHEAD * groups; i < chunks; i += groups)
+        f += *reinterpret_cast<const F4 *>(outs + static_cast<int64_t>(i) * a.head_dim +
+                                           (in ? at : 0)) * exp2_of(ml[2 * i] - m);
     sums[threadIdx.x] = f;
     __syncthreads();
-    if (group != 0 || 4 * lane >= a.head_dim) return;
+    if (group != 0 || !in) return;
     l = part[kWaves];
-    for (int w = 1; w < kWaves; ++w) l += part[kWaves + w];
+    for (int w = 1; w < waves; ++w) l += part[kWaves + w];
     for (int g = 1; g < groups; ++g) f += sums[g * wide + lane];
     const Close c = close_row(n, head, m, l);
     store4<D>(a.out, t * a.out_stride + static_cast<int64_t>(head) * a.head_dim + at, f * c.inverse);
-    if (a.lse && lane == 0) a.lse[row] = c.lse;
+    if (a.lse && at == 0) a.lse[row] = c.lse;
 }
 
-// The most chunks that a sequence is cut into: as many as fill the GPU, none below
-// kMinChunk positions or above kMaxChunk.
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int64_t tiles_of(int64_t q_heads, int64_t kv_heads) { return ceil_div(q_heads / kv_heads, 16); }
 
-int64_t splits_of(int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t reach) {
+int wide_of(int64_t head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
+
+// The most chunks that a sequence is cut into. At least so many that none is above
+// kMaxChunk; and then as many as full rounds of the workgroups that the GPU holds at once
+// have room for, as long as none is below kMinChunk. A round more is taken where it leaves
+// a tenth less of the places empty.
+int64_t splits_of(int dtype, int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                  int64_t reach) {
+    const int dim = wide_of(head_dim);
+    const int64_t held = kCus * held_by_a_cu(dtype, dim, head_dim != dim);
     const int64_t groups = tokens * kv_heads * tiles_of(q_heads, kv_heads);
-    const int64_t fill = ceil_div(kWorkgroups, groups), fine = ceil_div(reach, kMinChunk),
-                  coarse = ceil_div(reach, kMaxChunk);
-    const int64_t want = fill < fine ? fill : fine;
-    return want > coarse ? want : coarse;
+    // (the smallest chunks only where the next size would not give every CU a workgroup)
+    const int64_t least = groups * ceil_div(reach, 2 * kMinChunk) < kCus ? kMinChunk : 2 * kMinChunk;
+    const int64_t fine = ceil_div(reach, least), coarse = ceil_div(reach, kMaxChunk);
+    const int64_t round = kWaves * tile_of(dtype, dim);
+    int64_t rounds = ceil_div(groups * coarse, held);
+    const int64_t bytes = 2 * head_dim * static_cast<int64_t>(size_of(dtype));  // of a position
+    if (rounds == 1 && groups * reach * bytes < held * kSmall) rounds = 2;
+    int64_t best = coarse;
+    double best_used = 0.0;
+    for (int64_t r = rounds; r < rounds + 2; ++r) {
+        int64_t splits = r * held / groups;
+        splits = splits > fine ? fine : splits;
+        const int64_t chunk = ceil_div(ceil_div(reach, splits), round) * round;
+        const int64_t pieces = ceil_div(reach, chunk);
+        const double used = static_cast<double>(groups * reach) /
+                            static_cast<double>(ceil_div(groups * pieces, held) * held * chunk);
+        if (used > 1.1 * best_used) {
+            best_used = used;
+            best = splits;
+        }
+    }
+    return best;
 }
 
-// Floats of a chunk's row in the workspace: its maximum, its sum, its output.
-int64_t part_floats(int64_t head_dim) { return head_dim + 2; }
-
 template <int D, int DIM>
-void launch_attend(const AttendArgs &n, dim3 grid, hipStream_t s) {
-    if (n.a.head_dim == DIM) attend_kernel<D, DIM, false><<<grid, kThreads, 0, s>>>(n);
-    else attend_kernel<D, DIM, true><<<grid, kThreads, 0, s>>>(n);
+void launch_attend(const AttendArgs &n, bool once, dim3 grid, hipStream_t s) {
+    if (n.a.head_dim != DIM) attend_kernel<D, DIM, true, false><<<grid, kThreads, 0, s>>>(n);
+    else if (once) attend_kernel<D, DIM, false, true><<<grid, kThreads, 0, s>>>(n);
+    else attend_kernel<D, DIM, false, false><<<grid, kThreads, 0, s>>>(n);
 }
 
 int64_t reach_of(const sifar_paged_attention_args &a) {
@@ -499,23 +596,34 @@ int64_t most_of(const sifar_paged_attention_args &a) {
 
 template <int D>
 hipError_t launch(const sifar_paged_attention_args &a, hipStream_t s) {
-    const int64_t splits = splits_of(a.tokens, a.q_heads, a.kv_heads, most_of(a));
+    const int64_t splits = splits_of(a.dtype, a.tokens, a.q_heads, a.kv_heads, a.head_dim, most_of(a));
     AttendArgs n{};
     n.a = a;
     n.page = make_div(static_cast<uint32_t>(a.page_size));
     n.splits = make_div(static_cast<uint32_t>(splits));
     n.group = a.q_heads / a.kv_heads;
     n.reach = static_cast<int32_t>(reach_of(a));
+    n.round = kWaves * tile_of(a.dtype, wide_of(a.head_dim));
     // 16-byte aligned
-    n.parts = (2 * static_cast<int64_t>(a.tokens) * a.q_heads * splits + 3) / 4 * 4;
-    const dim3 grid(a.kv_heads * tiles_of(a.q_heads, a.kv_heads), splits, a.tokens);
-    const int wide = a.head_dim <= 64 ? 64 : a.head_dim <= 128 ? 128 : 256;
-    if (wide == 64) launch_attend<D, 64>(n, grid, s);
-    else if (wide == 128) launch_attend<D, 128>(n, grid, s);
-    else launch_attend<D, 256>(n, grid, s);
+    n.at_outs = (2 * static_cast<int64_t>(a.tokens) * a.q_heads * splits + 3) / 4 * 4;
+    const dim3 grid(splits, a.kv_heads * tiles_of(a.q_heads, a.kv_heads), a.tokens);
+    const int dim = wide_of(a.head_dim);
+    // More keys and values than half of the 256 MB cache behind the L2s, read by one
+    // workgroup each, go past it: 1 x 131072 (32 heads on 8 of 128, bf16) 106 us through
+    // the caches, 96 past them. Those of 34 MB are read again from there (13.4 and 13.9).
+    const bool once = tiles_of(a.q_heads, a.kv_heads) == 1 &&
+                      2 * most_of(a) * a.tokens * a.kv_heads * a.head_dim *
+                              static_cast<int64_t>(size_of(a.dtype)) >= int64_t{1} << 27;
+    if (dim == 64) launch_attend<D, 64>(n, once, grid, s);
+    else if (dim == 128) launch_attend<D, 128>(n, once, grid, s);
+    else launch_attend<D, 256>(n, once, grid, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
-    join_kernel<D><<<dim3(a.q_heads, a.tokens), kThreads, 0, s>>>(n, wide / 4);
+    // Few rows, of many chunks each: their outputs in pieces, with many lanes for the chunks.
+    if (static_cast<int64_t>(a.tokens) * a.q_heads < 256)
+        join_kernel<D><<<dim3(a.q_heads, a.tokens, dim / 32), kThreads, 0, s>>>(n, 8);
+    else
+        join_kernel<D><<<dim3(a.q_heads, a.tokens), kRowWave, 0, s>>>(n, dim / 4);
     return hipGetLastError();
 }
 
@@ -553,7 +661,7 @@ bool good(const sifar_paged_attention_args &a) {
     const int64_t width = static_cast<int64_t>(a.q_heads) * a.head_dim;
     if (!good_stride(a.q_stride, a.tokens, width) || !good_stride(a.out_stride, a.tokens, width))
         return false;
-    const int64_t splits = splits_of(a.tokens, a.q_heads, a.kv_heads, most_of(a));
+    const int64_t splits = splits_of(a.dtype, a.tokens, a.q_heads, a.kv_heads, a.head_dim, most_of(a));
     const int64_t need = sifar_paged_attention_workspace(a.tokens, a.q_heads, a.kv_heads,
                                                          a.head_dim, a.max_length);
     if (splits > 1 && (!a.workspace || a.workspace_bytes < need)) return false;
@@ -586,17 +694,17 @@ extern "C" int64_t sifar_paged_attention_workspace(int32_t tokens, int32_t q_hea
                                                    int32_t max_length) {
     using namespace sifar;
     if (!good_sizes(tokens, q_heads, kv_heads, head_dim, max_length)) return SIFAR_EINVAL;
-    // Chunks of all sequences: no more than fine ones make, nor than fill the GPU and one
-    // for each, or coarse ones make. Each bound grows with tokens and max_length.
+    if (max_length <= kMinChunk || tokens == 0) return 0;
+    // Chunks of all sequences: no more than fine ones make, nor than coarse ones make and
+    // fill the last round of the most workgroups that are ever held. Each grows with tokens
+    // and max_length.
     const int64_t groups = static_cast<int64_t>(tokens) * kv_heads * tiles_of(q_heads, kv_heads);
     const int64_t fine = groups * ceil_div(max_length, kMinChunk);
-    const int64_t fill = kWorkgroups + groups, coarse = groups * ceil_div(max_length, kMaxChunk);
-    const int64_t more = fill > coarse ? fill : coarse;
-    const int64_t chunks = fine < more ? fine : more;
-    if (max_length <= kMinChunk || tokens == 0) return 0;
-    // a group's chunk holds a row for each of its query heads (16 at most)
+    const int64_t full = groups * ceil_div(max_length, kMaxChunk) + kCus * 10;
+    const int64_t chunks = fine < full ? fine : full;
+    // a chunk has a row for each query head of its tile: its maximum, its sum, its output
     const int64_t rows = q_heads / kv_heads < 16 ? q_heads / kv_heads : 16;
-    return (chunks * rows * part_floats(head_dim) + 4) * 4;
+    return (chunks * rows * (head_dim + 2) + 4) * 4;
 }
 
 extern "C" int sifar_paged_attention(const sifar_paged_attention_args *args, void *stream) {

@@ -33,7 +33,8 @@ inline Paged paged(int64_t pages, int64_t slots, int64_t heads, int64_t page_str
 }
 
 // From the first element to behind the last, or 0 where the strides do not keep the
-// elements apart, are not multiples of 8, or lead beyond 2^46 elements.
+// elements apart, are not multiples of 8, or lead beyond
+// SIFAR_CACHE_MAX_ELEMENTS.
 inline int64_t extent(const Paged &p) {
     int64_t e = p.dim;
     for (int i = 0; i < 3; ++i) {
@@ -41,10 +42,10 @@ inline int64_t extent(const Paged &p) {
         if (p.stride[i] < e || p.stride[i] % 8 || p.stride[i] > kMaxStride) return 0;
         const unsigned __int128 more =
             static_cast<unsigned __int128>(p.count[i] - 1) * static_cast<uint64_t>(p.stride[i]);
-        if (more > (static_cast<unsigned __int128>(1) << 46)) return 0;
+        if (more > SIFAR_CACHE_MAX_ELEMENTS) return 0;
         e += static_cast<int64_t>(more);
     }
-    return e;
+    return e <= SIFAR_CACHE_MAX_ELEMENTS ? e : 0;
 }
 
 // Does a cache share an element with one of the same strides whose first element lies

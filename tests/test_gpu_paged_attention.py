@@ -145,6 +145,21 @@ def test_lengths_dims_and_types(D, dtype):
                          4, 2, D, 16, dtype, sinks=D == 80))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_more_than_the_caches_keep(D, dtype):
+    """Tables with room for so much that keys and values are loaded past the caches, and chunks
+    of one tile to a dozen for each wave."""
+    i = inputs(22, [1, 31, 33, 255, 700, 1537, 3001, 9000], 4, 2, D, 512, dtype,
+               width=-(-2 ** 27 // (8 * 2 * 2 * D * 512 * i_size(dtype))) + 1)
+    run_and_check(i)
+    run_and_check(i, window=1200, softcap=20.0)
+
+
+def i_size(dtype):
+    return 4 if dtype == "fp32" else 2
+
+
 @pytest.mark.parametrize("Hq,Hk", [(1, 1), (3, 3), (5, 1), (15, 5), (16, 1), (17, 1), (34, 2),
                                    (64, 1), (48, 16)])
 def test_head_groups(Hq, Hk):
