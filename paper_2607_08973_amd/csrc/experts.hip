@@ -29,6 +29,8 @@ namespace {
 constexpr int kInWaves = 4, kOutWaves = 8;
 constexpr int kInThreads = kInWaves * kRowWave, kOutThreads = kOutWaves * kRowWave;
 constexpr int kRows = 16;
+constexpr int kInAhead = 4, kOutAhead = 4;  // steps of a batch of loads, for 16 columns
+constexpr int kFew = 4;  // columns whose accesses to x are fewer than a turn by way of LDS costs
 constexpr int kMaxSlots = SIFAR_EXPERTS_MAX_SLOTS;
 constexpr int kMaxExperts = SIFAR_ROUTE_MAX_EXPERTS;
 
@@ -46,6 +48,7 @@ struct ExpertsArgs {
     int64_t at_list; // from the workspace's start, in int32: {expert, first, count} of the
                      // n-th behind Plan, then the list
     int64_t at_h;    // in bytes
+    int64_t h_bytes; // of a slot's h, or of its first elements
 };
 
 __device__ __forceinline__ int local_expert(const sifar_experts_args &a, int slot) {
@@ -53,9 +56,29 @@ __device__ __forceinline__ int local_expert(const sifar_experts_args &a, int slo
     return e < static_cast<uint32_t>(a.experts) ? static_cast<int>(e) : -1;
 }
 
+// How h lies in the workspace: slots ordered by expert, then ascending; sixteen of an expert
+// (or what is left) make a tile, whose elements lie as the second product loads them: for
+// each 64 bytes of its rows, for each quarter of them, every column's 16 bytes. So lanes
+// of neighbouring columns read neighbouring bytes: where they read a row each, a load of 64
+// lanes took 64 accesses to the cache instead of 8.
+struct HiddenTile {
+    int64_t at;
+    int columns;
+};
+__device__ __forceinline__ HiddenTile hidden_tile(const ExpertsArgs &n, int before, int count,
+                                                  int nth) {
+    const int first = nth & ~15, left = count - first;
+    return {(before + first) * n.h_bytes, left < 16 ? left : 16};
+}
+// Of element i of a column, from the tile's start, in bytes.
+template <int SIZE>
+__device__ __forceinline__ int hidden_at(int i, int column, int columns) {
+    const int byte = i * SIZE;
+    return (byte & ~15) * columns + 16 * column + (byte & 15);
+}
+
 // 64 bytes of each of 16 rows, a quarter a lane; behind `bytes` of a row zeros.
-__device__ __forceinline__ U4 load_step(const unsigned char *row, int at, int bytes, bool whole) {
-    if (whole) return *reinterpret_cast<const U4 *>(row + at);
+__device__ __forceinline__ U4 load_step(const unsigned char *row, int at, int bytes) {
     const U4 w = *reinterpret_cast<const U4 *>(row + (at < bytes ? at : 0));
     return at < bytes ? w : U4{0, 0, 0, 0};
 }
@@ -68,50 +91,106 @@ __device__ __forceinline__ float act(float g, int activation) {
     return g / (1.f + __builtin_amdgcn_exp2f(y * -0x1.715476p+0f));
 }
 
-// `rows` of 16 weights each (the gate's, the up ones) times up to 16 * TILES columns over
-// the wave's steps of a row.
-template <int D, int TILES, int AHEAD>
+// A batch of x: AHEAD steps of 16 * TILES rows. Read as an operand's lanes need it, each
+// lane a row's 16 bytes, a load of 64 lanes takes 64 accesses to the cache, and the
+// weights' own are as many as it has time for. So lanes of neighbouring bytes read a row,
+// and the wave's part of LDS turns them: 16 bytes of column c and quarter q of step s stand
+// at place c ^ (4 s + q) of the 16 of (s, q), which keeps both sides off each other's banks.
+template <int TILES, int AHEAD>
+struct Turn {
+    static constexpr int ROW = 4 * AHEAD;  // 16-byte pieces of a row
+    static constexpr int LOADS = AHEAD * TILES;
+    static __device__ __forceinline__ int place(int tile, int column, int piece) {
+        return (tile * ROW + piece) * 16 + (column ^ (piece & 15));
+    }
+    static __device__ __forceinline__ void load(const unsigned char *const *rows, int at, int lane,
+                                                U4 (&x)[LOADS]) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int f = i * kRowWave + lane;
+            x[i] = *reinterpret_cast<const U4 *>(rows[f / ROW] + at + f % ROW * 16);
+        }
+    }
+    static __device__ __forceinline__ void put(U4 *lds, int lane, const U4 (&x)[LOADS]) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int f = i * kRowWave + lane, row = f / ROW;
+            lds[place(row / 16, row & 15, f % ROW)] = x[i];
+        }
+    }
+    static __device__ __forceinline__ U4 get(const U4 *lds, int lane, int tile, int step) {
+        return lds[place(tile, lane & 15, 4 * step + (lane >> 4))];
+    }
+};
+
+// Two rows of 16 weights each (the gate's, the up ones) times up to 16 * TILES columns over
+// the wave's steps of a row. TURNED: x by way of `lds`, from the addresses in `rows`.
+template <int D, int TILES, int AHEAD, bool TURNED>
 __device__ __forceinline__ void in_product(const unsigned char *const (&w)[2],
-                                           const unsigned char *const (&x)[TILES], int from, int to,
-                                           int bytes, F4 (&sum)[2][TILES]) {
-    const int at = 16 * ((threadIdx.x & 63) >> 4);
+                                           const unsigned char *const *rows, int from, int to,
+                                           int bytes, U4 *lds, F4 (&sum)[2][TILES]) {
+    const int lane = threadIdx.x & 63, at = 16 * (lane >> 4);
+    const unsigned char *x[TILES];
+#pragma unroll
+    for (int c = 0; c < TILES; ++c) x[c] = rows[16 * c + (lane & 15)];
     int s = from;
     const int whole = to * 64 <= bytes ? to : to - 1;  // steps that no row ends in
     for (; s + AHEAD <= whole; s += AHEAD) {
-        U4 wa[AHEAD][2], xa[AHEAD][TILES];
+        U4 wa[AHEAD][2], xa[AHEAD * TILES];
+        if constexpr (TURNED) Turn<TILES, AHEAD>::load(rows, 64 * s, lane, xa);
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
                 wa[i][j] = *reinterpret_cast<const U4 *>(w[j] + 64 * (s + i) + at);
+            if constexpr (!TURNED)
 #pragma unroll
-            for (int c = 0; c < TILES; ++c)
-                xa[i][c] = *reinterpret_cast<const U4 *>(x[c] + 64 * (s + i) + at);
+                for (int c = 0; c < TILES; ++c)
+                    xa[i * TILES + c] = *reinterpret_cast<const U4 *>(x[c] + 64 * (s + i) + at);
+        }
+        if constexpr (TURNED) {
+            Turn<TILES, AHEAD>::put(lds, lane, xa);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+                for (int c = 0; c < TILES; ++c)
+                    xa[i * TILES + c] = Turn<TILES, AHEAD>::get(lds, lane, c, i);
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int c = 0; c < TILES; ++c) sum[j][c] = mma<D>(wa[i][j], xa[i][c], sum[j][c]);
+                for (int c = 0; c < TILES; ++c)
+                    sum[j][c] = mma<D>(wa[i][j], xa[i * TILES + c], sum[j][c]);
     }
-    for (; s < to; ++s) {
-        U4 wa[2];
+    // what is left, a step in which rows end among it, also in one go
+    for (; s < to; s += AHEAD) {
+        U4 wa[AHEAD][2], xa[AHEAD][TILES];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) wa[j] = load_step(w[j], 64 * s + at, bytes, s < whole);
+        for (int i = 0; i < AHEAD; ++i) {
+            const int step = 64 * (s + i < to ? s + i : to - 1) + at;
 #pragma unroll
-        for (int c = 0; c < TILES; ++c) {
-            const U4 xa = load_step(x[c], 64 * s + at, bytes, s < whole);
+            for (int j = 0; j < 2; ++j) wa[i][j] = load_step(w[j], step, bytes);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) sum[j][c] = mma<D>(wa[j], xa, sum[j][c]);
+            for (int c = 0; c < TILES; ++c) xa[i][c] = load_step(x[c], step, bytes);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (s + i >= to) break;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int c = 0; c < TILES; ++c) sum[j][c] = mma<D>(wa[i][j], xa[i][c], sum[j][c]);
         }
     }
 }
 
 // Columns base.. of the expert's slots: both products, the waves' parts joined, h stored.
-template <int D, int TILES, int AHEAD>
+template <int D, int TILES, int AHEAD, bool TURNED>
 __device__ __forceinline__ void in_columns(const ExpertsArgs &n, int expert, int row, const int *list,
-                                           int base, int count, F4 (*parts)[2][4][kRowWave]) {
+                                           int base, int count, int before, F4 (*parts)[2][4][kRowWave],
+                                           const unsigned char **rows) {
     constexpr int SIZE = D == SIFAR_FP32 ? 4 : 2;
     const sifar_experts_args &a = n.a;
     const int lane = threadIdx.x & 63, column = lane & 15;
@@ -123,13 +202,13 @@ __device__ __forceinline__ void in_columns(const ExpertsArgs &n, int expert, int
     const unsigned char *const w[2] = {
         matrix + static_cast<int64_t>(mine) * bytes,
         matrix + (static_cast<int64_t>(a.inter) + mine) * bytes};
-    const unsigned char *x[TILES];
-#pragma unroll
-    for (int c = 0; c < TILES; ++c) {
-        const int i = base + 16 * c + column;
-        x[c] = static_cast<const unsigned char *>(a.x) +
-               list[i < count ? i : base] / a.topk * a.x_stride * SIZE;
+    // the columns' rows of x; columns behind the last slot repeat the first
+    if (threadIdx.x < 16 * TILES) {
+        const int i = base + static_cast<int>(threadIdx.x);
+        rows[threadIdx.x] = static_cast<const unsigned char *>(a.x) +
+                            list[i < count ? i : base] / a.topk * a.x_stride * SIZE;
     }
+    __syncthreads();
     F4 sum[2][TILES];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -137,7 +216,8 @@ __device__ __forceinline__ void in_columns(const ExpertsArgs &n, int expert, int
         for (int c = 0; c < TILES; ++c) sum[j][c] = F4{0.f, 0.f, 0.f, 0.f};
     const int steps = (bytes + 63) / 64, each = (steps + kInWaves - 1) / kInWaves;
     const int from = wave * each < steps ? wave * each : steps;
-    in_product<D, TILES, AHEAD>(w, x, from, from + each < steps ? from + each : steps, bytes, sum);
+    in_product<D, TILES, AHEAD, TURNED>(w, rows, from, from + each < steps ? from + each : steps,
+                                        bytes, reinterpret_cast<U4 *>(parts[wave]), sum);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -155,28 +235,29 @@ __device__ __forceinline__ void in_columns(const ExpertsArgs &n, int expert, int
         for (int r = 0; r < 4; ++r) h[r] = act(g[r], a.activation) * u[r];
         const int i = base + 16 * wave + column, at = row + 4 * (lane >> 4);
         if (i < count && at < a.inter) {  // inter is a multiple of 8
-            unsigned char *to = static_cast<unsigned char *>(a.workspace) + n.at_h;
-            const int64_t e = static_cast<int64_t>(list[i]) * a.inter + at;
+            const HiddenTile tile = hidden_tile(n, before, count, i);
+            unsigned char *to = static_cast<unsigned char *>(a.workspace) + n.at_h + tile.at +
+                                hidden_at<SIZE>(at, i & 15, tile.columns);
             if constexpr (D == SIFAR_FP32) {
-                *reinterpret_cast<F4 *>(to + 4 * e) = h;
+                *reinterpret_cast<F4 *>(to) = h;
             } else {
                 typedef uint32_t U2 __attribute__((ext_vector_type(2)));
                 const Split p = split<SIFAR_BF16>(h[0], h[1]), q = split<SIFAR_BF16>(h[2], h[3]);
-                *reinterpret_cast<U2 *>(to + 2 * e) = U2{p.high, q.high};
-                to += 2 * static_cast<int64_t>(n.slots) * a.inter;
-                *reinterpret_cast<U2 *>(to + 2 * e) = U2{p.low, q.low};
+                *reinterpret_cast<U2 *>(to) = U2{p.high, q.high};
+                *reinterpret_cast<U2 *>(to + n.slots * n.h_bytes) = U2{p.low, q.low};
             }
         }
     }
-    __syncthreads();  // parts and, behind the last columns, nothing else is written again
+    __syncthreads();  // parts and rows are written again
 }
 
 template <int D>
-__global__ void __launch_bounds__(kInThreads) in_kernel(const ExpertsArgs n) {
+__global__ void __launch_bounds__(kInThreads, 4) in_kernel(const ExpertsArgs n) {
     __shared__ uint32_t bits[kMaxExperts / 32];
     __shared__ int list[kMaxSlots];
-    __shared__ int count, before;
-    __shared__ F4 parts[kInWaves][2][4][kRowWave];
+    __shared__ int here[kMaxSlots / kRowWave], below[kInWaves];
+    __shared__ F4 parts[kInWaves][2][4][kRowWave];  // and, before the sums, x being turned
+    __shared__ const unsigned char *rows[64];
     const sifar_experts_args &a = n.a;
     const int nth = blockIdx.y;
 
@@ -190,7 +271,6 @@ __global__ void __launch_bounds__(kInThreads) in_kernel(const ExpertsArgs n) {
     }
     const int words = (a.experts + 31) / 32;
     if (static_cast<int>(threadIdx.x) < words) bits[threadIdx.x] = 0;
-    if (threadIdx.x == 0) count = before = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
@@ -210,14 +290,32 @@ __global__ void __launch_bounds__(kInThreads) in_kernel(const ExpertsArgs n) {
     if (nth == 0 && blockIdx.x == 0 && threadIdx.x == 0) plan[0] = named;
     if (mine < 0) return;  // the same for the workgroup
 
-    // Its slots, in any order: a column's sums do not depend on where it stands.
+    // Its slots in ascending order, as every workgroup of the expert lists them: h is laid
+    // out by it. And how many slots other experts have before it.
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    uint64_t match[EACH];
+    int lower = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        if (expert[i] == mine)
-            list[atomicAdd(&count, 1)] = i * kInThreads + static_cast<int>(threadIdx.x);
-        else if (expert[i] >= 0 && expert[i] < mine)
-            atomicAdd(&before, 1);
+        match[i] = __builtin_amdgcn_ballot_w64(expert[i] == mine);
+        lower += __builtin_popcountll(
+            __builtin_amdgcn_ballot_w64(expert[i] >= 0 && expert[i] < mine));
+        if (lane == 0) here[i * kInWaves + wave] = __builtin_popcountll(match[i]);
     }
+    if (lane == 0) below[wave] = lower;
+    __syncthreads();
+    int count = 0, before = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+#pragma unroll
+        for (int w = 0; w < kInWaves; ++w) {
+            if (w == wave && expert[i] == mine)
+                list[count + __builtin_popcountll(match[i] & ((uint64_t{1} << lane) - 1))] =
+                    i * kInThreads + static_cast<int>(threadIdx.x);
+            count += here[i * kInWaves + w];
+        }
+#pragma unroll
+    for (int w = 0; w < kInWaves; ++w) before += below[w];
     __syncthreads();
     if (blockIdx.x == 0) {
         int32_t *mark = plan + 4 + 4 * nth;
@@ -229,12 +327,13 @@ __global__ void __launch_bounds__(kInThreads) in_kernel(const ExpertsArgs n) {
         for (int i = threadIdx.x; i < count; i += kInThreads) plan[n.at_list + before + i] = list[i];
     }
 
-    const int row = kRows * blockIdx.x, all = count;
-    for (int base = 0; base < all; base += 64) {
-        const int left = all - base;
-        if (left <= 16) in_columns<D, 1, 8>(n, mine, row, list, base, all, parts);
-        else if (left <= 32) in_columns<D, 2, 4>(n, mine, row, list, base, all, parts);
-        else in_columns<D, 4, 2>(n, mine, row, list, base, all, parts);
+    const int row = kRows * blockIdx.x;
+    for (int base = 0; base < count; base += 64) {
+        const int left = count - base;
+        if (left <= kFew) in_columns<D, 1, 8, false>(n, mine, row, list, base, count, before, parts, rows);
+        else if (left <= 16) in_columns<D, 1, kInAhead, true>(n, mine, row, list, base, count, before, parts, rows);
+        else if (left <= 32) in_columns<D, 2, kInAhead / 2, true>(n, mine, row, list, base, count, before, parts, rows);
+        else in_columns<D, 4, kInAhead / 4, true>(n, mine, row, list, base, count, before, parts, rows);
     }
 }
 
@@ -265,11 +364,22 @@ __device__ __forceinline__ F4 out_mma(const U4 &w, const Hidden<D> &h, F4 c) {
     }
 }
 
+// Where in its steps a wave begins; it goes on from the first behind the last. Rows of
+// weights lie a power of two apart, and workgroups that are all at the same step ask the
+// same few memory channels at every moment; those of an XCD (every eighth) stay together,
+// because they share h in its L2.
+__device__ __forceinline__ int turn_of(int steps, int batch) {
+    const int turns = steps / batch, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int turn = static_cast<int>(blockIdx.x & 7) * turns / 8 + wave * turns / (8 * kOutWaves);
+    return steps > 0 ? turn * batch : 0;
+}
+
 // The columns base.. of an expert's slots over steps from..to of `inter`; each slot's sums
 // go to its row of `rows`.
 template <int D, int TILES, int AHEAD>
 __device__ __forceinline__ void out_columns(const ExpertsArgs &n, int expert, int row,
-                                            const int32_t *list, int base, int count, int from, int to,
+                                            const int32_t *list, int before, int base,
+                                            int count, int from, int to,
                                             float *rows) {
     constexpr int SIZE = D == SIFAR_FP32 ? 4 : 2;
     const sifar_experts_args &a = n.a;
@@ -279,45 +389,95 @@ __device__ __forceinline__ void out_columns(const ExpertsArgs &n, int expert, in
     const unsigned char *w = static_cast<const unsigned char *>(a.w_out) +
                              expert * a.w_out_stride * SIZE + static_cast<int64_t>(mine) * bytes;
     const unsigned char *hidden = static_cast<const unsigned char *>(a.workspace) + n.at_h;
-    const int64_t low = static_cast<int64_t>(n.slots) * bytes;  // behind the first elements
+    const int64_t low = n.slots * n.h_bytes;  // behind the first elements
     const unsigned char *x[TILES];
-    int slot[TILES];
+    int step[TILES], slot[TILES];
 #pragma unroll
     for (int c = 0; c < TILES; ++c) {
         const int i = base + 16 * c + column;
         slot[c] = list[i < count ? i : base];
-        x[c] = hidden + static_cast<int64_t>(slot[c]) * bytes;
+        // behind the last tile, or its last column, the first one's
+        const HiddenTile tile = hidden_tile(n, before, count, base + 16 * c < count ? base + 16 * c : base);
+        x[c] = hidden + tile.at + 16 * (i < count ? column : 0) + at * tile.columns;
+        step[c] = 64 * tile.columns;
     }
     F4 sum[TILES];
 #pragma unroll
     for (int c = 0; c < TILES; ++c) sum[c] = F4{0.f, 0.f, 0.f, 0.f};
-    const auto load_hidden = [&](int c, int s, bool whole) {
+    const auto load_hidden = [&](int c, int s, auto whole) {
         Hidden<D> h;
-        h.v[0] = load_step(x[c], 64 * s + at, bytes, whole);
-        if constexpr (D != SIFAR_FP32) h.v[1] = load_step(x[c] + low, 64 * s + at, bytes, whole);
+        const bool in = decltype(whole)::value || 64 * s + at < bytes;
+        const unsigned char *p = in ? x[c] + static_cast<int64_t>(s) * step[c] : hidden;
+        h.v[0] = *reinterpret_cast<const U4 *>(p);
+        if constexpr (D != SIFAR_FP32) h.v[1] = *reinterpret_cast<const U4 *>(p + low);
+        if (!in) {
+            h.v[0] = U4{0, 0, 0, 0};
+            if constexpr (D != SIFAR_FP32) h.v[1] = U4{0, 0, 0, 0};
+        }
         return h;
     };
-    int s = from;
-    const int whole = to * 64 <= bytes ? to : to - 1;
-    for (; s + AHEAD <= whole; s += AHEAD) {
-        U4 wa[AHEAD];
+    // Two batches of AHEAD steps: one is on its way while the other is multiplied.
+    struct Batch {
+        U4 w[AHEAD];
         Hidden<D> h[AHEAD][TILES];
+    };
+    const auto load = [&](Batch &t, int s) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            wa[i] = *reinterpret_cast<const U4 *>(w + 64 * (s + i) + at);
+            t.w[i] = *reinterpret_cast<const U4 *>(w + 64 * (s + i) + at);
 #pragma unroll
-            for (int c = 0; c < TILES; ++c) h[i][c] = load_hidden(c, s + i, true);
+            for (int c = 0; c < TILES; ++c) t.h[i][c] = load_hidden(c, s + i, std::true_type{});
         }
+    };
+    const auto multiply = [&](const Batch &t) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-            for (int c = 0; c < TILES; ++c) sum[c] = out_mma<D>(wa[i], h[i][c], sum[c]);
-    }
-    for (; s < to; ++s) {
-        const U4 wa = load_step(w, 64 * s + at, bytes, s < whole);
+            for (int c = 0; c < TILES; ++c) sum[c] = out_mma<D>(t.w[i], t.h[i][c], sum[c]);
+    };
+    // From `first` to `last`: whole batches, then what is left in one go, a step in which
+    // rows end among it.
+    const auto steps = [&](int first, int last) {
+        const int whole = last * 64 <= bytes ? last : last - 1;
+        int s = first;
+        if (s + AHEAD <= whole) {
+            Batch one, two;
+            load(one, s);
+            for (s += AHEAD; s + 2 * AHEAD <= whole; s += 2 * AHEAD) {
+                load(two, s);
+                multiply(one);
+                load(one, s + AHEAD);
+                multiply(two);
+            }
+            if (s + AHEAD <= whole) {
+                load(two, s);
+                s += AHEAD;
+                multiply(one);
+                multiply(two);
+            } else {
+                multiply(one);
+            }
+        }
+        for (; s < last; s += AHEAD) {
+            Batch t;
 #pragma unroll
-        for (int c = 0; c < TILES; ++c) sum[c] = out_mma<D>(wa, load_hidden(c, s, s < whole), sum[c]);
-    }
+            for (int i = 0; i < AHEAD; ++i) {
+                const int step = s + i < last ? s + i : last - 1;
+                t.w[i] = load_step(w, 64 * step + at, bytes);
+#pragma unroll
+                for (int c = 0; c < TILES; ++c) t.h[i][c] = load_hidden(c, step, std::false_type{});
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                if (s + i >= last) break;
+#pragma unroll
+                for (int c = 0; c < TILES; ++c) sum[c] = out_mma<D>(t.w[i], t.h[i][c], sum[c]);
+            }
+        }
+    };
+    const int middle = from + turn_of(to - from, AHEAD);
+    steps(middle, to);
+    if (middle > from) steps(from, middle);
 #pragma unroll
     for (int c = 0; c < TILES; ++c)
         if (base + 16 * c + column < count)
@@ -339,22 +499,31 @@ __global__ void __launch_bounds__(kOutThreads) out_kernel(const ExpertsArgs n) {
     const sifar_experts_args &a = n.a;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = kRows * blockIdx.x;
     const int32_t *plan = static_cast<const int32_t *>(a.workspace);
+    // the first experts' marks with the number of them, before one of either is used
+    const int lane = threadIdx.x & 63;
+    int marks[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) marks[i] = plan[4 + 4 * (lane < n.named ? lane : 0) + i];
     const int named = plan[0];
     const int parts = parts_of(named, n.slots);
     const int steps = (a.inter * SIZE + 63) / 64, each = (steps + parts - 1) / parts;
     for (int unit = wave; unit < named * parts; unit += kOutWaves) {
         const int nth = unit / parts, part = unit % parts;
-        const int32_t *mark = plan + 4 + 4 * nth;
-        const int expert = mark[0], count = mark[2];
+        int mark[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            mark[i] = nth < kRowWave ? __builtin_amdgcn_readlane(marks[i], nth)
+                                     : plan[4 + 4 * nth + i];
+        const int count = mark[2];
         const int32_t *list = plan + n.at_list + mark[1];
         const int from = part * each < steps ? part * each : steps;
         const int to = from + each < steps ? from + each : steps;
         float *mine = rows + part * n.slots * kRows;
         for (int base = 0; base < count; base += 64) {
             const int left = count - base;
-            if (left <= 16) out_columns<D, 1, 8>(n, expert, row, list, base, count, from, to, mine);
-            else if (left <= 32) out_columns<D, 2, 4>(n, expert, row, list, base, count, from, to, mine);
-            else out_columns<D, 4, 2>(n, expert, row, list, base, count, from, to, mine);
+            if (left <= 16) out_columns<D, 1, kOutAhead>(n, mark[0], row, list, mark[1], base, count, from, to, mine);
+            else if (left <= 32) out_columns<D, 2, kOutAhead / 2>(n, mark[0], row, list, mark[1], base, count, from, to, mine);
+            else out_columns<D, 4, kOutAhead / 4>(n, mark[0], row, list, mark[1], base, count, from, to, mine);
         }
     }
     __syncthreads();
@@ -385,6 +554,7 @@ hipError_t launch(const sifar_experts_args &a, hipStream_t s) {
     n.named = a.experts < n.slots ? a.experts : n.slots;
     n.at_list = 4 + 4 * static_cast<int64_t>(n.slots);
     n.at_h = (4 * plan_words(n.slots) + 255) / 256 * 256;
+    n.h_bytes = static_cast<int64_t>(a.inter) * size_of(a.dtype);
     in_kernel<D><<<dim3((a.inter + kRows - 1) / kRows, n.named), kInThreads, 0, s>>>(n);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
