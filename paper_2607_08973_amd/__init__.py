@@ -782,8 +782,6 @@ def _heads(fn: str, name: str, t, dtype, shape, dev: int):
     if t is None:
         _refuse(fn, f"no {name}")
     if t.dtype is dtype and t.shape == shape and t.get_device() == dev:
-        if t.is_contiguous():
-            return t.data_ptr(), shape[1] * shape[2]
         at = t.stride()
         if at[2] == 1 and (at[1] == shape[2] or shape[1] == 1):
             return t.data_ptr(), at[0]
@@ -801,9 +799,10 @@ def _caches(fn: str, k_cache, v_cache, dtype, heads: int, dim: int, dev: int):
                     f"[{dim}] with adjacent elements")
     if v_cache.shape != shape or v_cache.stride() != at:
         _refuse(fn, "k_cache and v_cache are not laid out alike")
-    for c in (k_cache, v_cache):
-        if c.dtype is not dtype or c.get_device() != dev:
-            _refuse(fn, f"a cache is {c.dtype} on {c.device}, not {dtype} on the current GPU")
+    if (k_cache.dtype is not dtype or v_cache.dtype is not dtype or k_cache.get_device() != dev
+            or v_cache.get_device() != dev):
+        _refuse(fn, f"the caches are {k_cache.dtype} on {k_cache.device} and {v_cache.dtype} on "
+                    f"{v_cache.device}, not {dtype} on the current GPU")
     if shape[0] > 0x7FFFFFFF or shape[1] > SIFAR_CACHE_MAX_PAGE:
         _refuse(fn, f"{shape[0]} pages of {shape[1]} are too large")
     return shape, at
@@ -811,13 +810,15 @@ def _caches(fn: str, k_cache, v_cache, dtype, heads: int, dim: int, dev: int):
 
 def _table(fn: str, pages, dev: int):
     """Address, rows, columns and row stride of the table of pages."""
-    if pages is None or pages.dim() != 2:
-        _refuse(fn, "no pages" if pages is None else f"pages has {pages.dim()} dimensions, not 2")
-    shape = pages.shape
+    if pages is None:
+        _refuse(fn, "no pages")
+    shape, at = pages.shape, pages.stride()
+    if len(shape) != 2 or pages.dtype is not _I32 or pages.get_device() != dev or at[1] != 1:
+        _refuse(fn, f"pages is {pages.dtype} {tuple(shape)} on {pages.device} at strides {at}, not "
+                    f"{_I32} rows on the current GPU with adjacent elements")
     if shape[0] > 0x7FFFFFFF or shape[1] > 0x7FFFFFFF:
         _refuse(fn, f"a table of {shape[0]} x {shape[1]} pages is too large")
-    at, stride = _operand(fn, "pages", pages, _I32, shape, dev)
-    return at, shape[0], shape[1], stride
+    return pages.data_ptr(), shape[0], shape[1], at[0]
 
 
 def sifar_cache_append(k, v, positions, pages, k_cache, v_cache, q=None, q_out=None, inv_freq=None,

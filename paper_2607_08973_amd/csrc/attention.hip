@@ -28,6 +28,7 @@
 // them.
 #include <hip/hip_runtime.h>
 
+#include "attend_plan.h"
 #include "paged.h"
 #include "rows.h"
 #include "sifar_kernels.h"
@@ -36,12 +37,7 @@
 namespace sifar {
 namespace {
 
-constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kRowWave;
-constexpr int kMinChunk = 128;   // positions of a shared sequence's chunk, at least
-constexpr int kMaxChunk = 1536;  // and at most
-constexpr int kCus = 256;
-constexpr int64_t kSmall = 262144;  // bytes of a workgroup's keys and values
 constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e430p-1f;
 constexpr float kLowest = -0x1.fffffep127f;  // below every finite score
 
@@ -134,16 +130,6 @@ __device__ __forceinline__ int own_thread() {
     int i = threadIdx.x;
     asm volatile("" : "+v"(i));
     return i;
-}
-
-// Positions of a tile.
-constexpr int tile_of(int dtype, int dim) { return dtype == SIFAR_FP32 || dim > 128 ? 16 : 32; }
-
-// Workgroups that a CU holds at once, as the registers allow.
-constexpr int held_by_a_cu(int dtype, int dim, bool padded) {
-    return dim == 64    ? (dtype == SIFAR_FP32 && !padded ? 5 : 4)
-           : dim == 128 ? 3
-                        : (dtype == SIFAR_FP32 ? 1 : 2);
 }
 
 // D: element type. DIM: 64, 128 or 256, head_dim or the next above it (PAD).
@@ -538,45 +524,6 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttendArgs n, cons
     if (a.lse && at == 0) a.lse[row] = c.lse;
 }
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-int64_t tiles_of(int64_t q_heads, int64_t kv_heads) { return ceil_div(q_heads / kv_heads, 16); }
-
-int wide_of(int64_t head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
-
-// The most chunks that a sequence is cut into. At least so many that none is above
-// kMaxChunk; and then as many as full rounds of the workgroups that the GPU holds at once
-// have room for, as long as none is below kMinChunk. A round more is taken where it leaves
-// a tenth less of the places empty.
-int64_t splits_of(int dtype, int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
-                  int64_t reach) {
-    const int dim = wide_of(head_dim);
-    const int64_t held = kCus * held_by_a_cu(dtype, dim, head_dim != dim);
-    const int64_t groups = tokens * kv_heads * tiles_of(q_heads, kv_heads);
-    // (the smallest chunks only where the next size would not give every CU a workgroup)
-    const int64_t least = groups * ceil_div(reach, 2 * kMinChunk) < kCus ? kMinChunk : 2 * kMinChunk;
-    const int64_t fine = ceil_div(reach, least), coarse = ceil_div(reach, kMaxChunk);
-    const int64_t round = kWaves * tile_of(dtype, dim);
-    int64_t rounds = ceil_div(groups * coarse, held);
-    const int64_t bytes = 2 * head_dim * static_cast<int64_t>(size_of(dtype));  // of a position
-    if (rounds == 1 && groups * reach * bytes < held * kSmall) rounds = 2;
-    int64_t best = coarse;
-    double best_used = 0.0;
-    for (int64_t r = rounds; r < rounds + 2; ++r) {
-        int64_t splits = r * held / groups;
-        splits = splits > fine ? fine : splits;
-        const int64_t chunk = ceil_div(ceil_div(reach, splits), round) * round;
-        const int64_t pieces = ceil_div(reach, chunk);
-        const double used = static_cast<double>(groups * reach) /
-                            static_cast<double>(ceil_div(groups * pieces, held) * held * chunk);
-        if (used > 1.1 * best_used) {
-            best_used = used;
-            best = splits;
-        }
-    }
-    return best;
-}
-
 template <int D, int DIM>
 void launch_attend(const AttendArgs &n, bool once, dim3 grid, hipStream_t s) {
     if (n.a.head_dim != DIM) attend_kernel<D, DIM, true, false><<<grid, kThreads, 0, s>>>(n);
@@ -604,8 +551,7 @@ hipError_t launch(const sifar_paged_attention_args &a, hipStream_t s) {
     n.group = a.q_heads / a.kv_heads;
     n.reach = static_cast<int32_t>(reach_of(a));
     n.round = kWaves * tile_of(a.dtype, wide_of(a.head_dim));
-    // 16-byte aligned
-    n.at_outs = (2 * static_cast<int64_t>(a.tokens) * a.q_heads * splits + 3) / 4 * 4;
+    n.at_outs = outs_at(static_cast<int64_t>(a.tokens) * a.q_heads, splits);
     const dim3 grid(splits, a.kv_heads * tiles_of(a.q_heads, a.kv_heads), a.tokens);
     const int dim = wide_of(a.head_dim);
     // More keys and values than half of the 256 MB cache behind the L2s, read by one
@@ -664,7 +610,8 @@ bool good(const sifar_paged_attention_args &a) {
     const int64_t splits = splits_of(a.dtype, a.tokens, a.q_heads, a.kv_heads, a.head_dim, most_of(a));
     const int64_t need = sifar_paged_attention_workspace(a.tokens, a.q_heads, a.kv_heads,
                                                          a.head_dim, a.max_length);
-    if (splits > 1 && (!a.workspace || a.workspace_bytes < need)) return false;
+    const int64_t used = used_bytes(static_cast<int64_t>(a.tokens) * a.q_heads, splits, a.head_dim);
+    if (splits > 1 && (!a.workspace || a.workspace_bytes < need || need < used)) return false;
 
     const uint64_t size = size_of(a.dtype), tokens = static_cast<uint64_t>(a.tokens);
     const Rows q = rows_of(a.q, a.dtype, a.tokens, a.q_stride, width);
@@ -694,17 +641,7 @@ extern "C" int64_t sifar_paged_attention_workspace(int32_t tokens, int32_t q_hea
                                                    int32_t max_length) {
     using namespace sifar;
     if (!good_sizes(tokens, q_heads, kv_heads, head_dim, max_length)) return SIFAR_EINVAL;
-    if (max_length <= kMinChunk || tokens == 0) return 0;
-    // Chunks of all sequences: no more than fine ones make, nor than coarse ones make and
-    // fill the last round of the most workgroups that are ever held. Each grows with tokens
-    // and max_length.
-    const int64_t groups = static_cast<int64_t>(tokens) * kv_heads * tiles_of(q_heads, kv_heads);
-    const int64_t fine = groups * ceil_div(max_length, kMinChunk);
-    const int64_t full = groups * ceil_div(max_length, kMaxChunk) + kCus * 10;
-    const int64_t chunks = fine < full ? fine : full;
-    // a chunk has a row for each query head of its tile: its maximum, its sum, its output
-    const int64_t rows = q_heads / kv_heads < 16 ? q_heads / kv_heads : 16;
-    return (chunks * rows * (head_dim + 2) + 4) * 4;
+    return asked_bytes(tokens, q_heads, kv_heads, head_dim, max_length);
 }
 
 extern "C" int sifar_paged_attention(const sifar_paged_attention_args *args, void *stream) {

@@ -166,7 +166,7 @@ def test_layout_matches_a_c_compiler(name, tmp_path):
 
 def test_workspaces_grow():
     w = S.sifar_paged_attention_workspace
-    assert w(0, 8, 2, 64, 4096) == 0 and w(64, 8, 2, 64, 256) == 0
+    assert w(0, 8, 2, 64, 4096) == 0 and w(64, 8, 2, 64, 100) == 0
     for heads, kv, dim in ((32, 8, 128), (1, 1, 8), (34, 1, 256), (1024, 1024, 64)):
         for length in (1, 257, 1000, 5000, 131072, 1 << 24):
             sizes = [w(t, heads, kv, dim, length) for t in (1, 2, 3, 7, 63, 64, 65, 255, 4096, 32768)]
