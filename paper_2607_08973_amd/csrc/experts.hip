@@ -495,6 +495,9 @@ __device__ __forceinline__ int parts_of(int named, int slots) {
 template <int D>
 __global__ void __launch_bounds__(kOutThreads) out_kernel(const ExpertsArgs n) {
     extern __shared__ __attribute__((aligned(16))) float rows[];  // [parts][slots][kRows]
+    // what each slot adds with, loaded at once here rather than one by one at the end
+    __shared__ float weight[kMaxSlots];
+    __shared__ int8_t here[kMaxSlots];
     constexpr int SIZE = D == SIFAR_FP32 ? 4 : 2;
     const sifar_experts_args &a = n.a;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = kRows * blockIdx.x;
@@ -505,6 +508,10 @@ __global__ void __launch_bounds__(kOutThreads) out_kernel(const ExpertsArgs n) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) marks[i] = plan[4 + 4 * (lane < n.named ? lane : 0) + i];
     const int named = plan[0];
+    for (int i = threadIdx.x; i < n.slots; i += kOutThreads) {
+        weight[i] = a.weights[i];
+        here[i] = local_expert(a, i) >= 0;
+    }
     const int parts = parts_of(named, n.slots);
     const int steps = (a.inter * SIZE + 63) / 64, each = (steps + parts - 1) / parts;
     for (int unit = wave; unit < named * parts; unit += kOutWaves) {
@@ -533,10 +540,10 @@ __global__ void __launch_bounds__(kOutThreads) out_kernel(const ExpertsArgs n) {
         float f = 0.f;
         for (int j = 0; j < a.topk; ++j) {
             const int slot = t * a.topk + j;
-            if (local_expert(a, slot) < 0) continue;
+            if (!here[slot]) continue;
             float y = rows[slot * kRows + r];
             for (int p = 1; p < parts; ++p) y += rows[(p * n.slots + slot) * kRows + r];
-            f = __builtin_fmaf(a.weights[slot], y, f);
+            f = __builtin_fmaf(weight[slot], y, f);
         }
         const int64_t at = t * a.out_stride + row + r;
         if constexpr (D == SIFAR_FP32) static_cast<float *>(a.out)[at] = f;
@@ -572,7 +579,9 @@ bool good_sizes(int64_t tokens, int64_t topk, int64_t inter) {
 bool good(const sifar_experts_args &a) {
     if (!good_dtype(a.dtype) || !good_sizes(a.tokens, a.topk, a.inter)) return false;
     if (a.hidden < 8 || a.hidden > 65536 || a.hidden % 8) return false;
-    if (a.experts < 1 || a.experts > SIFAR_ROUTE_MAX_EXPERTS || a.first_expert < 0) return false;
+    if (a.experts < 1 || a.experts > SIFAR_ROUTE_MAX_EXPERTS || a.first_expert < 0 ||
+        a.first_expert > INT32_MAX - a.experts)
+        return false;
     if (a.activation != SIFAR_EXPERTS_SILU && a.activation != SIFAR_EXPERTS_GELU) return false;
     const int64_t matrix = static_cast<int64_t>(a.inter) * a.hidden;
     if (!good_stride(a.w_in_stride, a.experts, 2 * matrix) ||

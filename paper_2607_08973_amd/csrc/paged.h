@@ -48,6 +48,14 @@ inline int64_t extent(const Paged &p) {
     return e <= SIFAR_CACHE_MAX_ELEMENTS ? e : 0;
 }
 
+// A table of `rows` rows of pages, `stride` apart, whose bytes can be counted.
+inline bool good_table(int64_t rows, int64_t stride) {
+    return stride >= 0 && (rows <= 1 || stride <= kMaxStride / rows);
+}
+inline Rows table_of(const void *p, int64_t rows, int64_t stride, int64_t width) {
+    return span_of(p, 4ull * static_cast<uint64_t>((rows <= 1 ? 0 : (rows - 1) * stride) + width));
+}
+
 // Does a cache share an element with one of the same strides whose first element lies
 // `d` elements away? Exact for strides that extent() accepts: rows of one loop reach at
 // most into the next turn of the loop around it.

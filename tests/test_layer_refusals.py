@@ -75,7 +75,8 @@ BAD_APPEND = [
     dict(positions=5 * MB + 2), dict(sequence=6 * MB + 1), dict(pages=7 * MB + 2),
     dict(inv_freq=8 * MB + 2), dict(q_stride=HQ * D - 8), dict(q_stride=HQ * D + 4),
     dict(q_out_stride=0), dict(k_stride=ROW - 8), dict(k_stride=-ROW), dict(v_stride=ROW + 4),
-    dict(pages_stride=-1), dict(page_stride=PAGE * ROW - 8), dict(slot_stride=ROW - 8),
+    dict(pages_stride=-1), dict(pages_stride=1 << 40), dict(sequences=2 ** 31 - 1, pages_stride=1 << 12),
+    dict(page_stride=PAGE * ROW - 8), dict(slot_stride=ROW - 8),
     dict(slot_stride=ROW + 4), dict(head_stride=D - 8), dict(head_stride=-D), dict(page_stride=0),
     dict(page_stride=1 << 41),
     # outputs over outputs and inputs
@@ -97,7 +98,7 @@ BAD_ATTENTION = [
     dict(workspace=16 * MB + 8), dict(pages=4 * MB + 2), dict(lengths=5 * MB + 1),
     dict(sinks=6 * MB + 2), dict(lse=8 * MB + 2), dict(q_stride=HQ * D - 8),
     dict(q_stride=HQ * D + 4), dict(out_stride=0), dict(page_stride=PAGE * ROW - 8),
-    dict(slot_stride=ROW + 4), dict(head_stride=0), dict(pages_stride=-1),
+    dict(slot_stride=ROW + 4), dict(head_stride=0), dict(pages_stride=-1), dict(pages_stride=1 << 40),
     dict(workspace_bytes=attention_args().workspace_bytes - 1), dict(workspace_bytes=-1),
     dict(out=MB + 2 * D), dict(out=MB, out_stride=2 * HQ * D), dict(out=2 * MB), dict(out=4 * MB),
     dict(out=5 * MB), dict(out=6 * MB), dict(out=8 * MB), dict(out=16 * MB), dict(lse=16 * MB),
@@ -107,6 +108,7 @@ BAD_EXPERTS = [
     dict(dtype=3), dict(tokens=-1), dict(tokens=129), dict(tokens=128, topk=9), dict(hidden=0),
     dict(hidden=12), dict(hidden=65544), dict(inter=0), dict(inter=20), dict(inter=65544),
     dict(experts=0), dict(experts=1025), dict(topk=0), dict(topk=33), dict(first_expert=-1),
+    dict(first_expert=2 ** 31 - 1), dict(first_expert=2 ** 31 - E),
     dict(activation=2), dict(activation=-1), dict(x=None), dict(ids=None), dict(weights=None),
     dict(w_in=None), dict(w_out=None), dict(out=None), dict(workspace=None), dict(x=MB + 8),
     dict(w_in=4 * MB + 8), dict(w_out=5 * MB + 8), dict(out=6 * MB + 8), dict(workspace=7 * MB + 8),
