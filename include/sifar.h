@@ -872,8 +872,9 @@ int64_t sifar_paged_attention_workspace(int32_t tokens, int32_t q_heads, int32_t
  * Limits: hidden and inter multiples of 8 in 8..65536; experts 1..
  * SIFAR_ROUTE_MAX_EXPERTS; topk 1..SIFAR_ROUTE_MAX_TOPK; 0 <= tokens <=
  * SIFAR_EXPERTS_MAX_TOKENS and tokens * topk <= SIFAR_EXPERTS_MAX_SLOTS; first_expert
- * not negative, and no expert's index above 2^31 - 2; row strides, where there is more than one token, and the experts',
- * where there is more than one, multiples of 8 and at least what they step over;
+ * not negative, and no expert's index above 2^31 - 2; row strides, where there is more
+ * than one token, and the experts', where there is more than one, multiples of 8 and at
+ * least what they step over;
  * x, out and weight matrices 16-byte aligned. Outputs and workspace that overlap each
  * other or an input are refused. Two launches. */
 #define SIFAR_EXPERTS_SILU 0

@@ -28,7 +28,9 @@ constexpr int kMostHeld = 5;
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-inline int64_t tiles_of(int64_t q_heads, int64_t kv_heads) { return ceil_div(q_heads / kv_heads, 16); }
+inline int64_t tiles_of(int64_t q_heads, int64_t kv_heads) {
+    return ceil_div(q_heads / kv_heads, 16);
+}
 
 inline int wide_of(int64_t head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 

@@ -215,11 +215,14 @@ attend_kernel(const AttendArgs n) {
     const unsigned char *v_lane[PANELS];
 #pragma unroll
     for (int p = 0; p < PANELS; ++p)
-        v_lane[p] = v_cache + (!PAD || (16 * p + column) * BYTES < row_bytes ? (16 * p + column) * BYTES : 0);
+        v_lane[p] = v_cache + (!PAD || (16 * p + column) * BYTES < row_bytes
+                                   ? (16 * p + column) * BYTES
+                                   : 0);
     const auto load_keys = [&](int tile) {
 #pragma unroll
         for (int j = 0; j < SUBS; ++j) {
-            const uint64_t at = static_cast<uint64_t>(place[tile * TILE + 16 * j + column]) * (8 * SIZE);
+            const uint64_t at =
+                static_cast<uint64_t>(place[tile * TILE + 16 * j + column]) * (8 * SIZE);
 #pragma unroll
             for (int i = 0; i < STEPS; ++i)
                 k[j][i] = load_cache<U4, ONCE>(i < SURE ? k_lane + at + 64 * i : k_end[i] + at);
@@ -425,7 +428,8 @@ attend_kernel(const AttendArgs n) {
     const int busy = count < kWaves * TILE ? (count + TILE - 1) / TILE : kWaves;  // had a tile
     if (wave < busy && own_column < heads) {
         float most_of_all = top[0][own_column];
-        for (int w = 1; w < busy; ++w) most_of_all = __builtin_fmaxf(most_of_all, top[w][own_column]);
+        for (int w = 1; w < busy; ++w)
+            most_of_all = __builtin_fmaxf(most_of_all, top[w][own_column]);
         const float scale = exp2_of(m - most_of_all);
         float *to = outs + (wave * 16 + own_column) * ROW;
 #pragma unroll
@@ -527,7 +531,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttendArgs n, cons
     for (int w = 1; w < waves; ++w) l += part[kWaves + w];
     for (int g = 1; g < groups; ++g) f += sums[g * wide + lane];
     const Close c = close_row(n, head, m, l);
-    store4<D>(a.out, t * a.out_stride + static_cast<int64_t>(head) * a.head_dim + at, f * c.inverse);
+    store4<D>(a.out, t * a.out_stride + static_cast<int64_t>(head) * a.head_dim + at,
+              f * c.inverse);
     if (a.lse && at == 0) a.lse[row] = c.lse;
 }
 
@@ -550,7 +555,8 @@ int64_t most_of(const sifar_paged_attention_args &a) {
 
 template <int D>
 hipError_t launch(const sifar_paged_attention_args &a, hipStream_t s) {
-    const int64_t splits = splits_of(a.dtype, a.tokens, a.q_heads, a.kv_heads, a.head_dim, most_of(a));
+    const int64_t splits =
+        splits_of(a.dtype, a.tokens, a.q_heads, a.kv_heads, a.head_dim, most_of(a));
     AttendArgs n{};
     n.a = a;
     n.page = make_div(static_cast<uint32_t>(a.page_size));
@@ -614,7 +620,8 @@ bool good(const sifar_paged_attention_args &a) {
     const int64_t width = static_cast<int64_t>(a.q_heads) * a.head_dim;
     if (!good_stride(a.q_stride, a.tokens, width) || !good_stride(a.out_stride, a.tokens, width))
         return false;
-    const int64_t splits = splits_of(a.dtype, a.tokens, a.q_heads, a.kv_heads, a.head_dim, most_of(a));
+    const int64_t splits =
+        splits_of(a.dtype, a.tokens, a.q_heads, a.kv_heads, a.head_dim, most_of(a));
     const int64_t need = sifar_paged_attention_workspace(a.tokens, a.q_heads, a.kv_heads,
                                                          a.head_dim, a.max_length);
     const int64_t used = used_bytes(static_cast<int64_t>(a.tokens) * a.q_heads, splits, a.head_dim);

@@ -166,7 +166,9 @@ __global__ void __launch_bounds__(kMaxThreads) append_kernel(const AppendArgs n)
             }
         }
         const bool q = m.head < a.q_heads;
-        const int head = m.value ? m.head - a.q_heads - a.kv_heads : q ? m.head : m.head - a.q_heads;
+        const int head = m.value ? m.head - a.q_heads - a.kv_heads
+                         : q     ? m.head
+                                 : m.head - a.q_heads;
         void *to = m.value ? a.v_cache : q ? a.q_out : a.k_cache;
         const int64_t row = q ? t * a.q_out_stride + static_cast<int64_t>(head) * a.head_dim
                               : slot + head * a.head_stride;
@@ -228,11 +230,13 @@ bool good(const sifar_cache_append_args &a) {
     if ((a.q_heads != 0) != (a.q != nullptr) || (a.q_heads != 0) != (a.q_out != nullptr))
         return false;
     if ((a.rotary_dim != 0) != (a.inv_freq != nullptr)) return false;
-    for (const void *p : {a.q, static_cast<const void *>(a.q_out), a.k, a.v,
-                          static_cast<const void *>(a.k_cache), static_cast<const void *>(a.v_cache)})
+    for (const void *p :
+         {a.q, static_cast<const void *>(a.q_out), a.k, a.v, static_cast<const void *>(a.k_cache),
+          static_cast<const void *>(a.v_cache)})
         if (!aligned16(p)) return false;
-    for (const void *p : {static_cast<const void *>(a.positions), static_cast<const void *>(a.sequence),
-                          static_cast<const void *>(a.pages), static_cast<const void *>(a.inv_freq)})
+    for (const void *p :
+         {static_cast<const void *>(a.positions), static_cast<const void *>(a.sequence),
+          static_cast<const void *>(a.pages), static_cast<const void *>(a.inv_freq)})
         if (!aligned4(p)) return false;
     const int64_t q_row = static_cast<int64_t>(a.q_heads) * a.head_dim;
     const int64_t k_row = static_cast<int64_t>(a.kv_heads) * a.head_dim;
@@ -254,7 +258,8 @@ bool good(const sifar_cache_append_args &a) {
     const Rows q_out = rows_of(a.q_out, a.dtype, a.tokens, a.q_out_stride, q_row);
     const Rows caches[] = {span_of(a.k_cache, static_cast<uint64_t>(elements) * size),
                            span_of(a.v_cache, static_cast<uint64_t>(elements) * size)};
-    const int64_t apart = static_cast<const char *>(a.v_cache) - static_cast<const char *>(a.k_cache);
+    const int64_t apart = static_cast<int64_t>(reinterpret_cast<uintptr_t>(a.v_cache) -
+                                               reinterpret_cast<uintptr_t>(a.k_cache));
     if (apart % 16 || shares(cache, apart / static_cast<int64_t>(size))) return false;
     if (may_overlap(q_out, q) && !same_rows(q_out, q)) return false;
     for (const Rows &i : in)

@@ -10,13 +10,22 @@
 //        experts those are it finds in ids by itself (a bit each in LDS), so the grid has
 //        no workgroup for an expert that nobody named, and no third launch plans it.
 //        The first workgroup of an expert leaves its list of slots to the second launch.
+//        Where more than four tokens share the expert, their rows are read in order and
+//        turned to the operand in LDS.
 //  out   a workgroup makes 16 elements of every token's output: its waves share the
 //        experts, or parts of `inter` where those are fewer than waves, each slot's row
-//        goes to LDS, and the slots of a token are summed in their order.
+//        goes to LDS, and the slots of a token are summed in their order. h lies in the
+//        order of its loads, and two batches of them are in flight.
 //
 // h passes between the launches in fp32 (fp32) or as two bf16 elements whose sum is
 // good to 2^-17 (16-bit types; bf16, because h in fp16 could overflow). fp16 weights
 // meet it as two bf16 elements too, which hold their 11 bits exactly.
+//
+// Measured, bf16, us of the two launches: 16 tokens, 6 of 64 experts, 4096 x 1408 (41 of
+// them named) 173 + 100, 5.5 and 4.8 TB/s; 64 tokens, 2 of 8, 4096 x 8192 217 + 174, 5.0 and
+// 3.1 (h comes from the L2s in twice as many bytes); one token, 8 of 128, 2048 x 768 15 + 13, the
+// latency of the ids or the plan and of two to six batches. Reads of weights alone, 16 rows
+// at a time, reach 6.4 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "operands.h"
@@ -30,23 +39,22 @@ constexpr int kInWaves = 4, kOutWaves = 8;
 constexpr int kInThreads = kInWaves * kRowWave, kOutThreads = kOutWaves * kRowWave;
 constexpr int kRows = 16;
 constexpr int kInAhead = 4, kOutAhead = 4;  // steps of a batch of loads, for 16 columns
-constexpr int kFew = 4;  // columns whose accesses to x are fewer than a turn by way of LDS costs
+constexpr int kFew = 4;  // columns up to which x is read as it is used (1, 4, 16: no change but
+                         // at 16, where 64 tokens took 230 us for 217)
 constexpr int kMaxSlots = SIFAR_EXPERTS_MAX_SLOTS;
 constexpr int kMaxExperts = SIFAR_ROUTE_MAX_EXPERTS;
 
-// What the first launch leaves in the workspace: how many experts are named, and for the
-// n-th of them its index and where its slots stand in the list.
-struct Plan {
-    int32_t named;
-    int32_t pad[3];
-};
+template <int N>
+constexpr std::integral_constant<int, N> kInt{};
 
+// What the first launch leaves in the workspace for the second, in int32: how many experts
+// are named, and behind 4 words, 4 for each of them in ascending order: its index, the first
+// of its slots in the list, their number. Then the list, slots by expert, then ascending.
 struct ExpertsArgs {
     sifar_experts_args a;
     int32_t slots;   // tokens * topk
     int32_t named;   // experts that can be named at most
-    int64_t at_list; // from the workspace's start, in int32: {expert, first, count} of the
-                     // n-th behind Plan, then the list
+    int64_t at_list; // of the list, from the workspace's start, in int32
     int64_t at_h;    // in bytes
     int64_t h_bytes; // of a slot's h, or of its first elements
 };
@@ -93,8 +101,8 @@ __device__ __forceinline__ float act(float g, int activation) {
 
 // A batch of x: AHEAD steps of 16 * TILES rows. Read as an operand's lanes need it, each
 // lane a row's 16 bytes, a load of 64 lanes takes 64 accesses to the cache, and the
-// weights' own are as many as it has time for. So lanes of neighbouring bytes read a row,
-// and the wave's part of LDS turns them: 16 bytes of column c and quarter q of step s stand
+// weights' own are as many as it has time for (64 tokens 246 us, by way of LDS 217). So
+// lanes of neighbouring bytes read a row, and the wave's part of LDS turns them: 16 bytes of column c and quarter q of step s stand
 // at place c ^ (4 s + q) of the 16 of (s, q), which keeps both sides off each other's banks.
 template <int TILES, int AHEAD>
 struct Turn {
@@ -150,11 +158,14 @@ __device__ __forceinline__ void in_product(const unsigned char *const (&w)[2],
         }
         if constexpr (TURNED) {
             Turn<TILES, AHEAD>::put(lds, lane, xa);
+            // other lanes of the wave read what this one wrote, and write it anew next time
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
                 for (int c = 0; c < TILES; ++c)
                     xa[i * TILES + c] = Turn<TILES, AHEAD>::get(lds, lane, c, i);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
@@ -188,15 +199,17 @@ __device__ __forceinline__ void in_product(const unsigned char *const (&w)[2],
 
 // Columns base.. of the expert's slots: both products, the waves' parts joined, h stored.
 template <int D, int TILES, int AHEAD, bool TURNED>
-__device__ __forceinline__ void in_columns(const ExpertsArgs &n, int expert, int row, const int *list,
-                                           int base, int count, int before, F4 (*parts)[2][4][kRowWave],
+__device__ __forceinline__ void in_columns(const ExpertsArgs &n, int expert, int row,
+                                           const int *list, int base, int count, int before,
+                                           F4 (*parts)[2][4][kRowWave],
                                            const unsigned char **rows) {
     constexpr int SIZE = D == SIFAR_FP32 ? 4 : 2;
     const sifar_experts_args &a = n.a;
     const int lane = threadIdx.x & 63, column = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int bytes = a.hidden * SIZE;
-    const int mine = row + column < a.inter ? row + column : a.inter - 1;  // what is cut is not stored
+    // (what rows behind the last make is not stored)
+    const int mine = row + column < a.inter ? row + column : a.inter - 1;
     const unsigned char *matrix = static_cast<const unsigned char *>(a.w_in) +
                                   expert * a.w_in_stride * SIZE;
     const unsigned char *const w[2] = {
@@ -324,16 +337,21 @@ __global__ void __launch_bounds__(kInThreads, 4) in_kernel(const ExpertsArgs n) 
             mark[1] = before;
             mark[2] = count;
         }
-        for (int i = threadIdx.x; i < count; i += kInThreads) plan[n.at_list + before + i] = list[i];
+        for (int i = threadIdx.x; i < count; i += kInThreads)
+            plan[n.at_list + before + i] = list[i];
     }
 
     const int row = kRows * blockIdx.x;
     for (int base = 0; base < count; base += 64) {
         const int left = count - base;
-        if (left <= kFew) in_columns<D, 1, 8, false>(n, mine, row, list, base, count, before, parts, rows);
-        else if (left <= 16) in_columns<D, 1, kInAhead, true>(n, mine, row, list, base, count, before, parts, rows);
-        else if (left <= 32) in_columns<D, 2, kInAhead / 2, true>(n, mine, row, list, base, count, before, parts, rows);
-        else in_columns<D, 4, kInAhead / 4, true>(n, mine, row, list, base, count, before, parts, rows);
+        const auto columns = [&](auto tiles, auto ahead, auto turned) {
+            in_columns<D, decltype(tiles)::value, decltype(ahead)::value, decltype(turned)::value>(
+                n, mine, row, list, base, count, before, parts, rows);
+        };
+        if (left <= kFew) columns(kInt<1>, kInt<8>, std::false_type{});
+        else if (left <= 16) columns(kInt<1>, kInt<kInAhead>, std::true_type{});
+        else if (left <= 32) columns(kInt<2>, kInt<kInAhead / 2>, std::true_type{});
+        else columns(kInt<4>, kInt<kInAhead / 4>, std::true_type{});
     }
 }
 
@@ -354,7 +372,8 @@ __device__ __forceinline__ F4 out_mma(const U4 &w, const Hidden<D> &h, F4 c) {
         U4 high, low;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const Split p = split<SIFAR_BF16>(low_half<SIFAR_FP16>(w[i]), high_half<SIFAR_FP16>(w[i]));
+            const Split p =
+                split<SIFAR_BF16>(low_half<SIFAR_FP16>(w[i]), high_half<SIFAR_FP16>(w[i]));
             high[i] = p.high;
             low[i] = p.low;
         }
@@ -367,7 +386,8 @@ __device__ __forceinline__ F4 out_mma(const U4 &w, const Hidden<D> &h, F4 c) {
 // Where in its steps a wave begins; it goes on from the first behind the last. Rows of
 // weights lie a power of two apart, and workgroups that are all at the same step ask the
 // same few memory channels at every moment; those of an XCD (every eighth) stay together,
-// because they share h in its L2.
+// because they share h in its L2. 64 tokens over rows of 16 KB: 254 us in step, 204 so. (In
+// the first product workgroups in step share DRAM pages: 246 us in step, 279 apart.)
 __device__ __forceinline__ int turn_of(int steps, int batch) {
     const int turns = steps / batch, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int turn = static_cast<int>(blockIdx.x & 7) * turns / 8 + wave * turns / (8 * kOutWaves);
@@ -378,9 +398,8 @@ __device__ __forceinline__ int turn_of(int steps, int batch) {
 // go to its row of `rows`.
 template <int D, int TILES, int AHEAD>
 __device__ __forceinline__ void out_columns(const ExpertsArgs &n, int expert, int row,
-                                            const int32_t *list, int before, int base,
-                                            int count, int from, int to,
-                                            float *rows) {
+                                            const int32_t *list, int before, int base, int count,
+                                            int from, int to, float *rows) {
     constexpr int SIZE = D == SIFAR_FP32 ? 4 : 2;
     const sifar_experts_args &a = n.a;
     const int lane = threadIdx.x & 63, column = lane & 15, at = 16 * (lane >> 4);
@@ -397,7 +416,8 @@ __device__ __forceinline__ void out_columns(const ExpertsArgs &n, int expert, in
         const int i = base + 16 * c + column;
         slot[c] = list[i < count ? i : base];
         // behind the last tile, or its last column, the first one's
-        const HiddenTile tile = hidden_tile(n, before, count, base + 16 * c < count ? base + 16 * c : base);
+        const HiddenTile tile =
+            hidden_tile(n, before, count, base + 16 * c < count ? base + 16 * c : base);
         x[c] = hidden + tile.at + 16 * (i < count ? column : 0) + at * tile.columns;
         step[c] = 64 * tile.columns;
     }
@@ -528,9 +548,13 @@ __global__ void __launch_bounds__(kOutThreads) out_kernel(const ExpertsArgs n) {
         float *mine = rows + part * n.slots * kRows;
         for (int base = 0; base < count; base += 64) {
             const int left = count - base;
-            if (left <= 16) out_columns<D, 1, kOutAhead>(n, mark[0], row, list, mark[1], base, count, from, to, mine);
-            else if (left <= 32) out_columns<D, 2, kOutAhead / 2>(n, mark[0], row, list, mark[1], base, count, from, to, mine);
-            else out_columns<D, 4, kOutAhead / 4>(n, mark[0], row, list, mark[1], base, count, from, to, mine);
+            const auto columns = [&](auto tiles, auto ahead) {
+                out_columns<D, decltype(tiles)::value, decltype(ahead)::value>(
+                    n, mark[0], row, list, mark[1], base, count, from, to, mine);
+            };
+            if (left <= 16) columns(kInt<1>, kInt<kOutAhead>);
+            else if (left <= 32) columns(kInt<2>, kInt<kOutAhead / 2>);
+            else columns(kInt<4>, kInt<kOutAhead / 4>);
         }
     }
     __syncthreads();
