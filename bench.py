@@ -193,7 +193,7 @@ def parse():
     ap.add_argument("--workload", default="llama8b-decode",
                     choices=["llama8b-decode", "smoke-n2", "spec-stress", "sweep", "moe-rmsnorm",
                              "ablation", "retry-curve", "reduce-cold", "litmus", "misspec-vs-tp",
-                             "row-ops"],
+                             "row-ops", "layer-ops"],
                     help="llama8b-decode is the headline line; the others print one "
                          "JSON line per configuration")
     ap.add_argument("--wpg", type=int, default=1, choices=[1, 2, 4, 8, 16],
@@ -548,6 +548,75 @@ def torch_sum_reference(w, scrub, reps=30):
     return res
 
 
+def graph_us(call, reps=20):
+    """Microseconds per call of a captured graph of `reps` calls, launches included."""
+    import torch
+
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        for _ in range(reps):
+            call()
+    g.replay()
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    for _ in range(10):
+        g.replay()
+    b.record()
+    torch.cuda.synchronize()
+    return a.elapsed_time(b) * 1e3 / (10 * reps)
+
+
+def layer_ops_points():
+    """The blocks of a decode layer (sifar_cache_append, sifar_paged_attention, sifar_experts)
+    at decode batches: microseconds per call of a captured graph, and the rate of the bytes a
+    call has to move. Small calls' operands stay in the caches between calls."""
+    import torch
+
+    import paper_2607_08973_amd as S
+
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(260708973)
+    bf16 = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda:0").normal_(generator=gen)
+    i32 = lambda t: t.to(torch.int32)
+    HQ, HK, D, PAGE = 32, 8, 128, 64
+    inv_freq = (10000.0 ** (-torch.arange(0, D, 2, device="cuda:0").double() / D)).float()
+    for T, lengths in ((1, (512, 8192, 131072)), (8, (512, 8192, 32768)), (64, (512, 8192))):
+        for L in lengths:
+            width = -(-L // PAGE)
+            pages = i32(torch.randperm(T * width, generator=gen, device="cuda:0").view(T, width))
+            kc, vc = bf16(T * width, PAGE, HK, D), bf16(T * width, PAGE, HK, D)
+            x, q = bf16(T, HQ + 2 * HK, D), bf16(T, HQ, D)
+            out = torch.empty_like(q)
+            n = i32(torch.full((T,), L, device="cuda:0"))
+            at = n - 1
+            ws = torch.empty(S.sifar_paged_attention_workspace(T, HQ, HK, D, L),
+                             dtype=torch.uint8, device="cuda:0")
+            if L == lengths[0]:
+                us = graph_us(lambda: S.sifar_cache_append(
+                    x[:, HQ:HQ + HK], x[:, HQ + HK:], at, pages, kc, vc, q=x[:, :HQ], q_out=q,
+                    inv_freq=inv_freq))
+                yield {"op": "cache_append", "tokens": T, "heads": f"{HQ}x{HK}x{D}",
+                       "us_per_call": us, "bytes": 4 * T * (HQ + 2 * HK) * D}
+            us = graph_us(lambda: S.sifar_paged_attention(q, kc, vc, pages, n, out, ws))
+            yield {"op": "paged_attention", "tokens": T, "length": L, "heads": f"{HQ}x{HK}x{D}",
+                   "us_per_call": us, "bytes": 4 * T * (L * HK + HQ) * D}
+            del kc, vc
+    E, K, H, I = 64, 8, 4096, 1024
+    w_in, w_out = bf16(E, 2 * I, H), bf16(E, H, I)
+    for T in (1, 8, 64):
+        x = bf16(T, H)
+        out, ids = torch.empty_like(x), torch.empty((T, K), dtype=torch.int32, device="cuda:0")
+        w = torch.empty((T, K), device="cuda:0")
+        S.sifar_route(torch.randn((T, E), generator=gen, device="cuda:0"), ids, w)
+        ws = torch.empty(S.sifar_experts_workspace(T, K, I), dtype=torch.uint8, device="cuda:0")
+        us = graph_us(lambda: S.sifar_experts(x, ids, w, w_in, w_out, out, ws))
+        named = int(ids.unique().numel())
+        yield {"op": "experts", "tokens": T, "topk": K, "named": named, "hidden": H, "inter": I,
+               "us_per_call": us, "bytes": 6 * named * H * I + 4 * T * H}
+
+
 def row_ops_points(reps=20):
     """The row operators of a decode step (sifar_block_norm, sifar_route, sifar_sample) at
     decode batches and a prefill's, each as a captured graph of `reps` calls: microseconds
@@ -556,22 +625,7 @@ def row_ops_points(reps=20):
 
     import paper_2607_08973_amd as S
 
-    def timed(call):
-        call()
-        torch.cuda.synchronize()
-        g = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(g):
-            for _ in range(reps):
-                call()
-        g.replay()
-        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-        a.record()
-        for _ in range(10):
-            g.replay()
-        b.record()
-        torch.cuda.synchronize()
-        return a.elapsed_time(b) * 1e3 / (10 * reps)
-
+    timed = lambda call: graph_us(call, reps)
     gen = torch.Generator(device="cuda:0")
     gen.manual_seed(260708973)
     rand = lambda *s: torch.randn(s, generator=gen, device="cuda:0")
@@ -623,10 +677,10 @@ def suite(args):
             print(json.dumps({k: (round(v, 4) if isinstance(v, float) else v)
                               for k, v in p.items()}), flush=True)
         return
-    if args.workload == "row-ops":
-        for p in row_ops_points():
+    if args.workload in ("row-ops", "layer-ops"):
+        for p in row_ops_points() if args.workload == "row-ops" else layer_ops_points():
             p["gbs"] = p["bytes"] / p["us_per_call"] / 1e3
-            print(json.dumps({"workload": "row-ops", **{
+            print(json.dumps({"workload": args.workload, **{
                 k: (round(v, 3) if isinstance(v, float) else v) for k, v in p.items()}}),
                 flush=True)
         return
