@@ -21,6 +21,9 @@
 // P is split into two 16-bit elements (what the first leaves goes into the second), so
 // weights are good to 2^-17 and the output's one rounding is its last; the second
 // product costs matrix time that the bytes leave free.
+// Infinite values would meet the second elements' zeros and signs: where a wave's sums are
+// not finite, it takes its tiles once more and gives those values a product of their own.
+// (Looking costs 0.1 us a call: 1 x 33 in a graph 4.8 and 4.9.)
 //
 // A workgroup takes one cache head of one sequence, or a chunk of its positions where that
 // leaves too few workgroups or too uneven ones; its four waves take every fourth tile and
@@ -139,6 +142,44 @@ __device__ __forceinline__ int own_thread() {
     return i;
 }
 
+// What is infinite or NaN in a tile of 16-bit values, added to the sums and taken out of the
+// tile. A weight's second element is often zero or of the other sign, and an infinity times
+// it NaN: so those values meet the weights' signs alone, in a product of their own (1 where
+// there is weight; zero and NaN as they are). Sums that they leave finite keep their bits.
+template <int D, int SUBS, int MINE, int PANELS, int WORDS, int SUMS>
+__device__ __forceinline__ void take_strange(const F4 (&x)[SUBS],
+                                             uint32_t (&v)[MINE][PANELS][WORDS],
+                                             F4 (&o)[SUMS]) {
+    constexpr uint32_t kExponent = D == SIFAR_BF16 ? 0x7F80u : 0x7C00u;
+    const auto strange = [](uint32_t w) {  // all bits of the halves whose exponent is full
+        return ((w & kExponent) == kExponent ? 0xFFFFu : 0u) |
+               ((w >> 16 & kExponent) == kExponent ? 0xFFFF0000u : 0u);
+    };
+    const auto sign = [](float w) { return w > 0.f ? 1.f : w; };
+    Half<MINE / 2> s;
+#pragma unroll
+    for (int j = 0; j < MINE / 2; ++j)
+        s.w[j] = pack16<D>(sign(x[j / 2][2 * (j & 1)]), sign(x[j / 2][2 * (j & 1) + 1]));
+#pragma unroll
+    for (int p = 0; p < PANELS; ++p)
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            Half<MINE / 2> even, odd;
+#pragma unroll
+            for (int j = 0; j < MINE / 2; ++j) {
+                uint32_t &a = v[2 * j][p][i], &b = v[2 * j + 1][p][i];
+                const uint32_t keep_a = ~strange(a), keep_b = ~strange(b);
+                even.w[j] = __builtin_amdgcn_perm(b & ~keep_b, a & ~keep_a, 0x05040100u);
+                odd.w[j] = __builtin_amdgcn_perm(b & ~keep_b, a & ~keep_a, 0x07060302u);
+                a &= keep_a;
+                b &= keep_b;
+            }
+            F4 &e = o[p * 2 * WORDS + 2 * i], &d = o[p * 2 * WORDS + 2 * i + 1];
+            e = mma_half<D>(even, s, e);
+            d = mma_half<D>(odd, s, d);
+        }
+}
+
 // D: element type. DIM: 64, 128 or 256, head_dim or the next above it (PAD).
 template <int D, int DIM, bool PAD, bool ONCE>
 __global__ void __launch_bounds__(kThreads, held_by_a_cu(D, DIM, PAD))
@@ -146,7 +187,7 @@ attend_kernel(const AttendArgs n) {
     constexpr int SIZE = D == SIFAR_FP32 ? 4 : 2;
     constexpr int STEPS = DIM * SIZE / 64;          // of 64 bytes of a row of keys
     // positions: half as many where keys, values and O would not fit the registers
-        constexpr int TILE = tile_of(D, DIM);
+    constexpr int TILE = tile_of(D, DIM);
     constexpr int SUBS = TILE / 16;
     constexpr int MINE = TILE / 4;                  // positions whose values a lane loads
     // 16 lanes hold a row of values in panels, up to 16 bytes a lane each
@@ -298,8 +339,8 @@ attend_kernel(const AttendArgs n) {
     // A tile's part of the sums; with MORE the wave's next one is loaded on the way. (The
     // last one stands behind the loop: where its loads were left out by a branch inside,
     // the registers of values were reused too early, in fp32 heads of 256.)
-    const auto take = [&](int tile, auto more) {
-        constexpr bool MORE = decltype(more)::value;
+    const auto take = [&](int tile, auto more, auto strange) {
+        constexpr bool MORE = decltype(more)::value, STRANGE = decltype(strange)::value;
         if (SHARED) {
             asm volatile("" ::: "memory");  // loaded here, not kept from before the loop
 #pragma unroll
@@ -379,6 +420,7 @@ attend_kernel(const AttendArgs n) {
                         o[p * EACH + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(
                             __uint_as_float(v[j][p][i]), x[0][j], o[p * EACH + i], 0, 0, 0);
         } else {
+            if constexpr (STRANGE) take_strange<D>(x, v, o);
             Half<MINE / 2> hi, lo;
 #pragma unroll
             for (int j = 0; j < MINE / 2; ++j) {
@@ -407,12 +449,31 @@ attend_kernel(const AttendArgs n) {
         }
         if constexpr (MORE) load_values(tile + kWaves);
     };
-    if (wave < tiles) {
+    const auto take_all = [&](auto strange) {
         int tile = wave;
         load_keys(tile);
         load_values(tile);
-        for (; tile + kWaves < tiles; tile += kWaves) take(tile, std::true_type{});
-        take(tile, std::false_type{});
+        for (; tile + kWaves < tiles; tile += kWaves) take(tile, std::true_type{}, strange);
+        take(tile, std::false_type{}, strange);
+    };
+    if (wave < tiles) {
+        take_all(std::false_type{});
+        // Values of 16 bits that are not finite need a product of their own: only where a sum
+        // shows that there may be some are the tiles taken once more, with it.
+        if constexpr (D != SIFAR_FP32) {
+            F4 all = o[0];
+#pragma unroll
+            for (int i = 1; i < PANELS * EACH; ++i) all += o[i];
+            const float any = __builtin_fabsf(all[0] + all[1] + (all[2] + all[3]));
+            if (__builtin_amdgcn_ballot_w64(!(any < __builtin_inff()))) {
+                asm volatile("" ::: "memory");  // loaded again, not kept
+                m = kLowest;
+                l = 0.f;
+#pragma unroll
+                for (int i = 0; i < PANELS * EACH; ++i) o[i] = F4{0.f, 0.f, 0.f, 0.f};
+                take_all(std::true_type{});
+            }
+        }
     }
 
     // The waves' sums, joined relative to the largest of their maxima.
