@@ -99,6 +99,17 @@ __device__ __forceinline__ float act(float g, int activation) {
     return g / (1.f + __builtin_amdgcn_exp2f(y * -0x1.715476p+0f));
 }
 
+// h as two bf16 elements. Above bf16's largest the first stays finite, so that the second,
+// and with it what is infinite in fp32 or NaN, is all of the rest.
+__device__ __forceinline__ Split split_h(float a, float b) {
+    constexpr float most = 0x1.fep127f;
+    const auto within = [](float f) { return __builtin_fminf(__builtin_fmaxf(f, -most), most); };
+    Split s;
+    s.high = pack16<SIFAR_BF16>(within(a), within(b));
+    s.low = pack16<SIFAR_BF16>(a - low_half<SIFAR_BF16>(s.high), b - high_half<SIFAR_BF16>(s.high));
+    return s;
+}
+
 // A batch of x: AHEAD steps of 16 * TILES rows. Read as an operand's lanes need it, each
 // lane a row's 16 bytes, a load of 64 lanes takes 64 accesses to the cache, and the
 // weights' own are as many as it has time for (64 tokens 246 us, by way of LDS 217). So
@@ -255,7 +266,7 @@ __device__ __forceinline__ void in_columns(const ExpertsArgs &n, int expert, int
                 *reinterpret_cast<F4 *>(to) = h;
             } else {
                 typedef uint32_t U2 __attribute__((ext_vector_type(2)));
-                const Split p = split<SIFAR_BF16>(h[0], h[1]), q = split<SIFAR_BF16>(h[2], h[3]);
+                const Split p = split_h(h[0], h[1]), q = split_h(h[2], h[3]);
                 *reinterpret_cast<U2 *>(to) = U2{p.high, q.high};
                 *reinterpret_cast<U2 *>(to + n.slots * n.h_bytes) = U2{p.low, q.low};
             }
