@@ -406,9 +406,9 @@ __device__ __forceinline__ int turn_of(int steps, int batch) {
 }
 
 // The columns base.. of an expert's slots over steps from..to of `inter`; each slot's sums
-// go to its row of `rows`.
+// go to its row of `rows`. Is one of them not finite?
 template <int D, int TILES, int AHEAD>
-__device__ __forceinline__ void out_columns(const ExpertsArgs &n, int expert, int row,
+__device__ __forceinline__ bool out_columns(const ExpertsArgs &n, int expert, int row,
                                             const int32_t *list, int before, int base, int count,
                                             int from, int to, float *rows) {
     constexpr int SIZE = D == SIFAR_FP32 ? 4 : 2;
@@ -513,6 +513,58 @@ __device__ __forceinline__ void out_columns(const ExpertsArgs &n, int expert, in
     for (int c = 0; c < TILES; ++c)
         if (base + 16 * c + column < count)
             *reinterpret_cast<F4 *>(rows + slot[c] * kRows + 4 * (lane >> 4)) = sum[c];
+    F4 all = sum[0];
+#pragma unroll
+    for (int c = 1; c < TILES; ++c) all += sum[c];
+    const float any = __builtin_fabsf(all[0] + all[1] + (all[2] + all[3]));
+    return __builtin_amdgcn_ballot_w64(!(any < __builtin_inff())) != 0;
+}
+
+// The columns' sums that are not finite, anew (16-bit types): an infinite weight, or in fp16
+// its second element, meets the zeros and signs of second elements in the matrix
+// instructions. Here weights and h are whole again; a lane takes four rows of its column.
+template <int D>
+__device__ __forceinline__ void strange_columns(const ExpertsArgs &n, int expert, int row,
+                                                const int32_t *list, int before, int base,
+                                                int count, int from, int to, float *rows) {
+    const sifar_experts_args &a = n.a;
+    const int column = threadIdx.x & 15, first = row + 4 * (threadIdx.x >> 4 & 3);
+    const int bytes = a.inter * 2, end = 64 * to < bytes ? 64 * to : bytes;
+    const unsigned char *w =
+        static_cast<const unsigned char *>(a.w_out) + expert * a.w_out_stride * 2;
+    const unsigned char *hidden = static_cast<const unsigned char *>(a.workspace) + n.at_h;
+    const int last = base + 64 < count ? base + 64 : count;
+#pragma unroll 1
+    for (int tile = base; tile < last; tile += 16) {
+        const bool in = tile + column < last;
+        float *sums = rows + list[in ? tile + column : tile] * kRows + 4 * (threadIdx.x >> 4 & 3);
+        const HiddenTile h = hidden_tile(n, before, count, tile);
+        const unsigned char *x = hidden + h.at + 16 * (in ? column : 0);
+#pragma unroll 1
+        for (int r = 0; r < 4; ++r) {
+            const int i = first + r < a.hidden ? first + r : a.hidden - 1;
+            const unsigned char *mine = w + static_cast<int64_t>(i) * bytes;
+            const bool odd = in && !(__builtin_fabsf(sums[r]) < __builtin_inff());
+            float f = 0.f;
+#pragma unroll 1
+            for (int at = 64 * from; at < end; at += 16) {
+                if (!__builtin_amdgcn_ballot_w64(odd && f == f)) break;  // NaN stays
+                const unsigned char *p = x + static_cast<int64_t>(at) * h.columns;
+                const U4 y = *reinterpret_cast<const U4 *>(mine + at);
+                const U4 high = *reinterpret_cast<const U4 *>(p);
+                const U4 low = *reinterpret_cast<const U4 *>(p + n.slots * n.h_bytes);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    f = __builtin_fmaf(low_half<D>(y[k]),
+                                       low_half<SIFAR_BF16>(high[k]) + low_half<SIFAR_BF16>(low[k]), f);
+                    f = __builtin_fmaf(high_half<D>(y[k]),
+                                       high_half<SIFAR_BF16>(high[k]) + high_half<SIFAR_BF16>(low[k]),
+                                       f);
+                }
+            }
+            if (odd) sums[r] = f;
+        }
+    }
 }
 
 // Parts that `inter` is cut into: waves that the experts leave idle, as long as all slots'
@@ -560,12 +612,15 @@ __global__ void __launch_bounds__(kOutThreads) out_kernel(const ExpertsArgs n) {
         for (int base = 0; base < count; base += 64) {
             const int left = count - base;
             const auto columns = [&](auto tiles, auto ahead) {
-                out_columns<D, decltype(tiles)::value, decltype(ahead)::value>(
+                return out_columns<D, decltype(tiles)::value, decltype(ahead)::value>(
                     n, mark[0], row, list, mark[1], base, count, from, to, mine);
             };
-            if (left <= 16) columns(kInt<1>, kInt<kOutAhead>);
-            else if (left <= 32) columns(kInt<2>, kInt<kOutAhead / 2>);
-            else columns(kInt<4>, kInt<kOutAhead / 4>);
+            const bool strange = left <= 16   ? columns(kInt<1>, kInt<kOutAhead>)
+                                 : left <= 32 ? columns(kInt<2>, kInt<kOutAhead / 2>)
+                                              : columns(kInt<4>, kInt<kOutAhead / 4>);
+            if constexpr (D != SIFAR_FP32)
+                if (strange)
+                    strange_columns<D>(n, mark[0], row, list, mark[1], base, count, from, to, mine);
         }
     }
     __syncthreads();

@@ -35,6 +35,22 @@ def check(got, want, i):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("T,E,topk", [(1, 1, 1), (3, 9, 4), (13, 2, 1), (30, 1, 1), (64, 4, 2),
+                                      (70, 1, 1)])
+@pytest.mark.parametrize("H,I", [(24, 8), (72, 520), (40, 1096)])
+def test_infinite_weights_of_the_second_product(dtype, T, E, topk, H, I):
+    i = experts_test.inputs(5000, T, E, topk, H, I, dtype)
+    want = experts_test.run(i)
+    e = int(i["ids"][0, 0])
+    i["w_out"][e, 1, 0] = INF
+    i["w_out"][e, 5, I - 1] = -INF
+    i["w_out"][e, H - 1, I // 2] = INF
+    i["w_out"][e, 6, 1], i["w_out"][e, 6, 2] = INF, -INF  # NaN or infinite, as the signs of h are
+    i["w_out"][e, 9, 3] = NAN
+    check(experts_test.run(i), want, i)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("T", [1, 4, 9, 40])
 @pytest.mark.parametrize("I", [8, 136, 1096])
 def test_infinite_h(dtype, T, I):
@@ -70,3 +86,15 @@ def test_h_above_the_largest_of_16_bits(T):
     got = experts_test.run(i)
     assert torch.isfinite(got).all()
     experts_test.check(i, got)
+
+
+def test_a_token_that_is_nan_beside_others():
+    """The other tokens of its tile keep their bits, those with infinite outputs too."""
+    i = experts_test.inputs(5003, 20, 2, 1, 72, 264, ids=np.zeros((20, 1)))
+    i["w_out"][0, 3, 9] = INF
+    want = experts_test.run(i)
+    i["x"][7] = NAN
+    got = experts_test.run(i)
+    assert got[7].isnan().all()
+    keep = [t for t in range(20) if t != 7]
+    assert torch.equal(got[keep], want[keep]) and torch.isinf(got[keep, 3]).all()
