@@ -124,11 +124,15 @@ struct Close {
 };
 __device__ __forceinline__ Close close_row(const AttendArgs &n, int head, float m, float l) {
     if (n.a.sinks) {
-        const float sink = n.a.sinks[head] * kLog2e;
+        const float natural = n.a.sinks[head], two = natural * kLog2e;
+        // one that has no place in base 2 keeps one at its end
+        const float sink =
+            natural < kLowest ? natural : __builtin_fminf(__builtin_fmaxf(two, kLowest), -kLowest);
         const float top = sink > m ? sink : m;
         const float scale = exp2_of(m - top);
         const float whole = l * scale + exp2_of(sink - top);
-        return {whole == 0.f ? 0.f : scale / whole, (top + log2_of(whole)) * kLn2};
+        return {whole == 0.f ? 0.f : scale / whole,
+                sink >= m ? natural + log2_of(whole) * kLn2 : (top + log2_of(whole)) * kLn2};
     }
     return {l == 0.f ? 0.f : 1.f / l, (l == 0.f ? -__builtin_inff() : (m + log2_of(l)) * kLn2)};
 }
