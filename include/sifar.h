@@ -788,7 +788,7 @@ int sifar_cache_append(const sifar_cache_append_args *a, void *stream);
  * lengths counts the new token, once it was appended. Products, sums and weights are
  * in fp32; out is rounded once. A row without any position has out 0 and lse -inf
  * (with a sink: the sink). A position whose score is -inf has no weight; a score that
- * is NaN or +inf makes its row NaN. An infinite value v_p makes its element of out
+ * is NaN or +inf makes its row NaN; scores of 2^127 and beyond may count as infinite. An infinite value v_p makes its element of out
  * infinite, of its sign; NaN where both signs meet or its weight, relative to the
  * row's largest, is below fp32's normal numbers. What the cache holds in slots that are
  * not read (behind a length, outside the window) has no influence, NaN included.

@@ -50,6 +50,7 @@ namespace {
 constexpr int kThreads = kWaves * kRowWave;
 constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e430p-1f;
 constexpr float kLowest = -0x1.fffffep127f;  // below every finite score
+constexpr float kFar = 0x1p127f;  // times log2(e) still finite
 
 struct AttendArgs {
     sifar_paged_attention_args a;
@@ -58,6 +59,7 @@ struct AttendArgs {
     int32_t group;  // query heads of a cache head
     int32_t reach;  // lengths are cut to this
     int32_t round;  // chunks are multiples of this, a power of two
+    float unit;     // log2(e), or 1 where the scale or softcap leaves fp32 times it: then last
     int64_t at_outs;  // the chunks' outputs from the workspace's start, in floats
 };
 
@@ -370,11 +372,15 @@ attend_kernel(const AttendArgs n) {
             if (a.softcap > 0.f) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    x[j][r] = a.softcap * kLog2e * tanh_of(x[j][r] * a.scale / a.softcap);
+                    x[j][r] = a.softcap * n.unit * tanh_of(x[j][r] * a.scale / a.softcap);
             } else {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * kLog2e;
+                for (int r = 0; r < 4; ++r) x[j][r] *= a.scale * n.unit;
             }
+        }
+        if (n.unit == 1.f) {
+#pragma unroll
+            for (int j = 0; j < SUBS; ++j) x[j] *= kLog2e;
         }
         if (missing) {
 #pragma unroll
@@ -629,6 +635,7 @@ hipError_t launch(const sifar_paged_attention_args &a, hipStream_t s) {
     n.group = a.q_heads / a.kv_heads;
     n.reach = static_cast<int32_t>(reach_of(a));
     n.round = kWaves * tile_of(a.dtype, wide_of(a.head_dim));
+    n.unit = __builtin_fabsf(a.scale) > kFar || a.softcap > kFar ? 1.f : kLog2e;
     n.at_outs = outs_at(static_cast<int64_t>(a.tokens) * a.q_heads, splits);
     const dim3 grid(splits, a.kv_heads * tiles_of(a.q_heads, a.kv_heads), a.tokens);
     const int dim = wide_of(a.head_dim);
