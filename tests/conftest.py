@@ -42,3 +42,30 @@ def grid(request, monkeypatch):
     if request.param == "unpadded":
         _load_fallbacks(monkeypatch)
     return request.param
+
+
+def ordered(row_stream):
+    """The binding's look-up of a call's stream; one that is passed waits for the current one."""
+
+    def look_up(stream, dev):
+        if stream is not None:
+            import torch
+
+            stream.wait_stream(torch.cuda.current_stream())
+        return row_stream(stream, dev)
+
+    return look_up
+
+
+# whose run() fills outputs and workspaces on the current stream before it calls on another
+FILL_FIRST = {"test_gpu_experts", "test_gpu_paged_attention"}
+
+
+@pytest.fixture(autouse=True)
+def streams_wait_for_fills(request, monkeypatch):
+    """Without the wait a late fill could overwrite an output, or the experts' plan between the
+    two launches, which would then be read as indices."""
+    if request.module.__name__.rpartition(".")[2] in FILL_FIRST:
+        import paper_2607_08973_amd as S
+
+        monkeypatch.setattr(S, "_row_stream", ordered(S._row_stream))
