@@ -72,6 +72,13 @@ inline int64_t splits_of(int dtype, int64_t tokens, int64_t q_heads, int64_t kv_
     return best;
 }
 
+// Positions of a chunk, of a sequence whose even share is `share`; `round` is a power of two
+// that kMaxChunk is a multiple of.
+constexpr int chunk_of(int share, int round) {
+    const int chunk = (share + round - 1) & -round;
+    return chunk < kMinChunk ? kMinChunk : chunk;
+}
+
 // The workspace: each row's chunks' maxima and sums, then, 16-byte aligned, their outputs.
 inline int64_t outs_at(int64_t rows, int64_t splits) { return (2 * rows * splits + 3) / 4 * 4; }
 

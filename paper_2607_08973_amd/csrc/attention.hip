@@ -73,10 +73,9 @@ __device__ __forceinline__ Stretch stretch(const AttendArgs &n, int64_t t) {
     Stretch s;
     s.first = n.a.window > 0 && length > n.a.window ? length - n.a.window : 0;
     s.count = length - s.first;
-    const int share =
-        static_cast<int>(div_u32(static_cast<uint32_t>(s.count) + n.splits.d - 1, n.splits));
-    s.chunk = (share + n.round - 1) & -n.round;
-    if (s.chunk < kMinChunk) s.chunk = kMinChunk;
+    s.chunk = chunk_of(
+        static_cast<int>(div_u32(static_cast<uint32_t>(s.count) + n.splits.d - 1, n.splits)),
+        n.round);
     return s;
 }
 
