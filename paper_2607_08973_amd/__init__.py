@@ -797,7 +797,8 @@ def _caches(fn: str, k_cache, v_cache, dtype, heads: int, dim: int, dev: int):
     if len(shape) != 4 or shape[2:] != (heads, dim) or at[3] != 1:
         _refuse(fn, f"k_cache is {tuple(shape)} at strides {at}, not [pages][page_size][{heads}]"
                     f"[{dim}] with adjacent elements")
-    if v_cache.shape != shape or v_cache.stride() != at:
+    if v_cache.shape != shape or v_cache.stride() != at and any(
+            n > 1 and a != b for n, a, b in zip(shape, at, v_cache.stride())):
         _refuse(fn, "k_cache and v_cache are not laid out alike")
     if (k_cache.dtype is not dtype or v_cache.dtype is not dtype or k_cache.get_device() != dev
             or v_cache.get_device() != dev):
@@ -813,7 +814,8 @@ def _table(fn: str, pages, dev: int):
     if pages is None:
         _refuse(fn, "no pages")
     shape, at = pages.shape, pages.stride()
-    if len(shape) != 2 or pages.dtype is not _I32 or pages.get_device() != dev or at[1] != 1:
+    if (len(shape) != 2 or pages.dtype is not _I32 or pages.get_device() != dev
+            or at[1] != 1 and shape[1] > 1):
         _refuse(fn, f"pages is {pages.dtype} {tuple(shape)} on {pages.device} at strides {at}, not "
                     f"{_I32} rows on the current GPU with adjacent elements")
     if shape[0] > 0x7FFFFFFF or shape[1] > 0x7FFFFFFF:
