@@ -799,7 +799,8 @@ int sifar_cache_append(const sifar_cache_append_args *a, void *stream);
  *   sinks    [q_heads] fp32, finite or -inf, or NULL;  lse [tokens][q_heads] fp32, or NULL
  *   max_length  what no length exceeds, known to the host: sizes, with the window, how
  *            many workgroups share a sequence, and the workspace. The caches' capacity
- *            is always right; calls that are to give equal bits need equal ones.
+ *            is always right, and slower than a bound near the lengths where these are
+ *            far below it; calls that are to give equal bits need equal ones.
  *   workspace   at least sifar_paged_attention_workspace(...) bytes, 16-byte aligned,
  *            caller-owned, in any state before and after; NULL where that is 0. Calls
  *            that may run at the same time need one each.

@@ -37,17 +37,23 @@ inline int wide_of(int64_t head_dim) { return head_dim <= 64 ? 64 : head_dim <= 
 // The most chunks that a sequence is cut into. At least so many that none is above
 // kMaxChunk; and then as many as full rounds of the workgroups that the GPU holds at once
 // have room for, as long as none is below kMinChunk. A round more is taken where it leaves
-// a tenth less of the places empty: 64 x 4096 (64 heads on 8 of 128, bf16) takes 196 us in 3
-// chunks (two rounds), 210 in 4 (2.7 rounds) and 202 in 2 (1.3). One round is not enough where
-// its workgroups have so little to read that they all start and end together: 16 x 2000 (16
-// heads of 64, fp32) 57 us in one, 51 in two.
+// a tenth less of the places empty: 64 x 4096 (64 heads on 8 of 128, bf16) takes 190 us in 3
+// chunks (two rounds), 204 in 4 (2.7 rounds). Two rounds are taken where the workgroups of one
+// have so little to read that they all start and end together: 16 x 2000 (16 heads of 64) in
+// bf16 34.2 us in one, 33.2 in two. (In fp32, where five workgroups a CU make one round of 5
+// chunks, it is the other way about: 46.9 and 52.0.)
+//
+// All of it goes by the most that a length may be: where lengths are far below that, a
+// sequence is in smaller chunks than its own length would make, down to kMinChunk, and most
+// workgroups read a length and leave. 64 x 1000 (64 heads on 8 of 128, bf16) takes 60 us under
+// a max_length of 1024, 69 under 32768, 76 under 131072; 8 x 1000 13, 16 and 30.
 inline int64_t splits_of(int dtype, int64_t tokens, int64_t q_heads, int64_t kv_heads,
                          int64_t head_dim, int64_t reach) {
     const int dim = wide_of(head_dim);
     const int64_t held = kCus * held_by_a_cu(dtype, dim, head_dim != dim);
     const int64_t groups = tokens * kv_heads * tiles_of(q_heads, kv_heads);
     // The smallest chunks only where twice as long ones would not give every CU a workgroup:
-    // 1 x 2048 takes 10.5 and 12.4 us with 128 and 256, 8 x 4096 35 and 33 (32 heads on 8).
+    // 1 x 2048 takes 9.9 and 10.9 us with 128 and 256, 8 x 4096 33.1 and 32.0 (32 heads on 8).
     const int64_t least =
         groups * ceil_div(reach, 2 * kMinChunk) < kCus ? kMinChunk : 2 * kMinChunk;
     const int64_t fine = ceil_div(reach, least), coarse = ceil_div(reach, kMaxChunk);

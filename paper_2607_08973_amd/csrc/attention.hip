@@ -23,17 +23,17 @@
 // product costs matrix time that the bytes leave free.
 // Infinite values would meet the second elements' zeros and signs: where a wave's sums are
 // not finite, it takes its tiles once more and gives those values a product of their own.
-// (Looking costs 0.1 us a call: 1 x 33 in a graph 4.8 and 4.9.)
+// (Looking costs 0.1 us a call: 1 x 33 in a graph 4.7 and 4.8.)
 //
 // A workgroup takes one cache head of one sequence, or a chunk of its positions where that
 // leaves too few workgroups or too uneven ones; its four waves take every fourth tile and
 // join in LDS. Chunks' sums go to the workspace, not yet divided, and a second launch joins
 // them.
 //
-// Measured, bf16, heads of 128: 1 x 131072 (32 heads on 8) 91 us a call, 5.9 TB/s, which is
-// what loads in this pattern reach that compute nothing; 64 x 4096 (64 on 8) 200 us, 5.4; 64
-// sequences of 1 to 8192 223 us, 5.0 (the rest are chunks of unequal length, the last of
-// which leave CUs idle); 1 x 33 in a graph 5.0 us. Left out, the matrix products and the
+// Measured, bf16, heads of 128: 1 x 131072 (32 heads on 8) 91.5 us a call, 5.9 TB/s, which is
+// what loads in this pattern reach that compute nothing; 64 x 4096 (64 on 8) 190 us, 5.7; 64
+// sequences of 1 to 8192 (1056 MB) 227 us, 4.6 (the rest are chunks of unequal length, the
+// last of which leave CUs idle); 1 x 33 in a graph 4.8 us. Left out, the matrix products and the
 // softmax change none of the long ones by a percent; nor do coalesced keys, or a third
 // less or more workgroups a CU.
 #include <hip/hip_runtime.h>
@@ -639,8 +639,9 @@ hipError_t launch(const sifar_paged_attention_args &a, hipStream_t s) {
     const dim3 grid(splits, a.kv_heads * tiles_of(a.q_heads, a.kv_heads), a.tokens);
     const int dim = wide_of(a.head_dim);
     // More keys and values than half of the 256 MB cache behind the L2s, read by one
-    // workgroup each, go past it: 1 x 131072 (32 heads on 8 of 128, bf16) 106 us through
-    // the caches, 96 past them. Those of 34 MB are read again from there (13.4 and 13.9).
+    // workgroup each, go past it: 1 x 131072 (32 heads on 8 of 128, bf16) took 106 us through
+    // the caches and 96 past them. Those of 34 MB are read again from there (13.4 and 13.9).
+    // Padded heads have no such variant: 64 x 8192 at heads of 96 runs at 4.9 TB/s.
     const bool once = tiles_of(a.q_heads, a.kv_heads) == 1 &&
                       2 * most_of(a) * a.tokens * a.kv_heads * a.head_dim *
                               static_cast<int64_t>(size_of(a.dtype)) >= int64_t{1} << 27;

@@ -7,7 +7,7 @@
 // their way. Each input is read once and each output written once. Bound: HBM bytes for
 // many tokens; for a few the launch and two dependent round trips (the position, then
 // its page). Measured: 8192 tokens of 32 + 2 x 8 heads of 128, bf16, 39.7 us a call, 5.1
-// TB/s, the rate of a copy; in a graph 1 token 4.4 us, 77 tokens 3.9.
+// TB/s, the rate of a copy; in a graph 1 token 3.0 us, 77 tokens (12 + 2 x 4 heads of 96) 3.2.
 //
 // Angles: position times frequency is formed in 64 bits and reduced to a quadrant there,
 // so that a position of a million is as exact as one of ten; what remains of the angle,

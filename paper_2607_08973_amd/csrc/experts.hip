@@ -22,9 +22,10 @@
 // meet it as two bf16 elements too, which hold their 11 bits exactly.
 //
 // Measured, bf16, us of the two launches: 16 tokens, 6 of 64 experts, 4096 x 1408 (41 of
-// them named) 173 + 100, 5.5 and 4.8 TB/s; 64 tokens, 2 of 8, 4096 x 8192 217 + 174, 5.0 and
+// them named) 171 + 98, 5.5 and 4.8 TB/s; 64 tokens, 2 of 8, 4096 x 8192 220 + 174, 4.9 and
 // 3.1 (h comes from the L2s in twice as many bytes); one token, 8 of 128, 2048 x 768 15 + 13, the
-// latency of the ids or the plan and of two to six batches. Reads of weights alone, 16 rows
+// latency of the ids or the plan and of two to six batches, and in the second launch the
+// half of the CUs that its 128 workgroups leave idle. Reads of weights alone, 16 rows
 // at a time, reach 6.4 TB/s.
 #include <hip/hip_runtime.h>
 
@@ -113,8 +114,9 @@ __device__ __forceinline__ Split split_h(float a, float b) {
 // A batch of x: AHEAD steps of 16 * TILES rows. Read as an operand's lanes need it, each
 // lane a row's 16 bytes, a load of 64 lanes takes 64 accesses to the cache, and the
 // weights' own are as many as it has time for (64 tokens 246 us, by way of LDS 217). So
-// lanes of neighbouring bytes read a row, and the wave's part of LDS turns them: 16 bytes of column c and quarter q of step s stand
-// at place c ^ (4 s + q) of the 16 of (s, q), which keeps both sides off each other's banks.
+// lanes of neighbouring bytes read a row, and the wave's part of LDS turns them: 16 bytes of
+// column c and quarter q of step s stand at place c ^ (4 s + q) of the 16 of (s, q), which
+// keeps both sides off each other's banks.
 template <int TILES, int AHEAD>
 struct Turn {
     static constexpr int ROW = 4 * AHEAD;  // 16-byte pieces of a row
