@@ -525,6 +525,8 @@ __device__ __forceinline__ bool out_columns(const ExpertsArgs &n, int expert, in
 // The columns' sums that are not finite, anew (16-bit types): an infinite weight, or in fp16
 // its second element, meets the zeros and signs of second elements in the matrix
 // instructions. Here weights and h are whole again; a lane takes four rows of its column.
+// Sums that turn NaN end it at once; where all stay infinite, 64 tokens (2 of 8, 4096 x 8192)
+// take 3.8 ms instead of 0.36.
 template <int D>
 __device__ __forceinline__ void strange_columns(const ExpertsArgs &n, int expert, int row,
                                                 const int32_t *list, int before, int base,
@@ -557,11 +559,11 @@ __device__ __forceinline__ void strange_columns(const ExpertsArgs &n, int expert
                 const U4 low = *reinterpret_cast<const U4 *>(p + n.slots * n.h_bytes);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
+                    const uint32_t p0 = high[k], p1 = low[k];
                     f = __builtin_fmaf(low_half<D>(y[k]),
-                                       low_half<SIFAR_BF16>(high[k]) + low_half<SIFAR_BF16>(low[k]), f);
+                                       low_half<SIFAR_BF16>(p0) + low_half<SIFAR_BF16>(p1), f);
                     f = __builtin_fmaf(high_half<D>(y[k]),
-                                       high_half<SIFAR_BF16>(high[k]) + high_half<SIFAR_BF16>(low[k]),
-                                       f);
+                                       high_half<SIFAR_BF16>(p0) + high_half<SIFAR_BF16>(p1), f);
                 }
             }
             if (odd) sums[r] = f;
